@@ -246,6 +246,105 @@ mx_status mx_layer_step(const mx_batch* batch, const mx_layer_cfg* cfg, const vo
                         const uint16_t* x, uint16_t* y, uint16_t* k_pool, uint16_t* v_pool,
                         void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------- 8-bit cache
+ *
+ * A layer's keys and values in 8 bits: twice the tokens in the same memory, half
+ * the bytes for a decode to read.  Pages, page tables and batches are those of the
+ * bf16 cache above; a page of a pool holds, for each KV head, 16 tokens as e4m3
+ * codes (OCP: largest 448, no infinity), and one scale belongs to the page's keys
+ * of that head and one to its values:
+ *   k_pool[pool_pages][n_kv_heads][head_dim / 64][16][64]  (element (slot s, dim e)
+ *                          of a page's head at (e / 64) * 1024 + s * 64 + e % 64)
+ *   v_pool[pool_pages][n_kv_heads][head_dim][16]           (transposed)
+ *   k_scale, v_scale[pool_pages][n_kv_heads]               fp32 powers of two
+ * The cached value is code * scale.  Scales are powers of two, as mx_kv_append_f8
+ * writes them; the attention reads a scale's exponent only.
+ *   weight[pool_pages][n_kv_heads][16]                     fp32, or NULL
+ * is the attention weight that each cached token has received so far (below); with
+ * weight == NULL nothing is accumulated and nothing can be evicted by it.
+ *
+ * The calls below read host staging buffers like all others of this library, and
+ * refuse a stream that is being captured into a graph (MX_ERR_UNSUPPORTED).
+ */
+typedef struct {
+  uint8_t *k_pool, *v_pool;
+  float *k_scale, *v_scale;
+  float *weight;
+} mx_cache_f8;
+
+/*
+ * mx_kv_append into the 8-bit cache: k_new, v_new [T][n_kv_heads][head_dim] bf16.
+ * For every page and KV head that new tokens touch, keys and values apart:
+ *   need  = the least power of two 2^e, -100 <= e <= 119, with max |x| <= 448 * 2^e
+ *           over the finite elements x of the page's new tokens;
+ *   scale = need where the page's first new token has slot 0, else max(old scale, need);
+ *   the new tokens' codes are x / scale rounded to nearest even (beyond +-448, which
+ *           only the bound on e can leave: +-448; x infinite or NaN: NaN);
+ *   the codes of the older tokens in the page (slots below the first new one) become
+ *           code * old / new scale, rounded to nearest even: exact but for codes that
+ *           end below the smallest normal one.
+ * Slots behind the last new token keep their bytes.  weight, where given, is set to 0
+ * for the new tokens.  Errors as mx_kv_append, and MX_ERR_INVALID where two requests'
+ * new tokens share a page (its scale would be written twice).  No workspace.
+ */
+mx_status mx_kv_append_f8(const mx_batch* batch, const mx_attn_shape* shape,
+                          const uint16_t* k_new, const uint16_t* v_new, const mx_cache_f8* cache,
+                          hipStream_t stream);
+
+/*
+ * mx_paged_attn over the 8-bit cache, with K_r[j] and V_r[j] = code * scale.  Where
+ * cache->weight is given, every key's attention weight is accumulated beside it: with
+ * p[t][h][j] = softmax_j of the call, for every request r, KV head g and position j
+ *   weight[slot of j][g] += sum over r's new tokens t and the q heads h of group g of
+ *                           p[t][h][j].
+ * Sums are in fp32.  A page that several requests of the batch share receives the sum
+ * over all of them (in no fixed order; every other weight, and every output, is the
+ * same from run to run).  Sizes of the workspace: mx_workspace_bytes_f8_for, with
+ * track != 0 where cache->weight is given (it holds the decodes' scores then); its
+ * upper bound for any batch of at most max_tokens new tokens, max_reqs requests and
+ * max_pages page-table entries in total: mx_workspace_bytes_f8.
+ */
+size_t mx_workspace_bytes_f8_for(const mx_batch* batch, const mx_attn_shape* shape, int32_t track);
+size_t mx_workspace_bytes_f8(const mx_attn_shape* shape, int32_t track, int32_t max_tokens,
+                             int32_t max_reqs, int64_t max_pages);
+mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape* shape, const uint16_t* q,
+                           const mx_cache_f8* cache, uint16_t* out, void* ws, size_t ws_bytes,
+                           hipStream_t stream);
+
+/* One request of an eviction. */
+typedef struct {
+  int32_t len;                /* cached tokens */
+  int32_t keep;               /* tokens that stay: 0 .. len */
+  int32_t recent;             /* of these, the last ones, whatever their weight: 0 .. keep */
+  int32_t n_pages;            /* entries in pages[]: >= ceil(len / 16) */
+  int32_t n_dst_pages;        /* entries in dst_pages[]: >= ceil(keep / 16) */
+  const int32_t* pages;       /* [host] page ids in [0, pool_pages) */
+  const int32_t* dst_pages;   /* [host] free pages for the tokens that stay */
+} mx_evict_request;
+
+/*
+ * Eviction by accumulated attention weight.  For every request and KV head by itself:
+ * the last `recent` tokens stay, and of the others the (keep - recent) with the largest
+ * weight (equal weights: the lower index first; a NaN counts as larger than any
+ * number).  The tokens that stay are copied, in their order, to tokens 0 .. keep - 1 of
+ * dst_pages, codes, scales and weights; a destination page's scale is the largest of
+ * the scales its tokens come from, and codes of a smaller one become
+ * code * source / destination scale, rounded to nearest even.  The indices that stay go
+ * to kept (int32): request r's at n_kv_heads * (keep of the requests before it),
+ * [n_kv_heads][keep], ascending.  The source pages keep what they hold (a shared prefix
+ * may be a source of several requests); the caller frees them, goes on with dst_pages
+ * and ctx_len = keep, and counts positions by itself where they matter (rotary angles
+ * are in the keys already).  Slots of the last destination page behind keep keep their
+ * bytes.  A destination page must not be another's destination or any request's source
+ * (MX_ERR_INVALID).  cache->weight must be given.  The workspace:
+ * mx_kv_evict_f8_ws_bytes (0 and mx_last_error on invalid requests).
+ */
+size_t mx_kv_evict_f8_ws_bytes(int32_t num_reqs, const mx_evict_request* reqs,
+                               const mx_attn_shape* shape);
+mx_status mx_kv_evict_f8(int32_t num_reqs, const mx_evict_request* reqs,
+                         const mx_attn_shape* shape, const mx_cache_f8* cache, int32_t* kept,
+                         void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------------- inspection */
 
 /* Byte offsets, inside the workspace of mx_layer_step for this batch, of the

@@ -31,7 +31,8 @@ EXPORTED = [
     "mx_debug_gather", "mx_debug_gemm_ws_bytes", "mx_debug_gemm", "mx_debug_gemm_config",
     "mx_debug_gemm_tiled", "mx_debug_gemm_plan", "mx_debug_gemm_rows",
     "mx_debug_reduce_residual_rmsnorm", "mx_paged_attn_static", "mx_paged_attn_static_max_bytes",
-    "mx_profile_enable", "mx_profile_read",
+    "mx_profile_enable", "mx_profile_read", "mx_kv_append_f8", "mx_workspace_bytes_f8_for",
+    "mx_workspace_bytes_f8", "mx_paged_attn_f8", "mx_kv_evict_f8_ws_bytes", "mx_kv_evict_f8",
 ]
 
 
@@ -61,6 +62,17 @@ class LayerCfg(ctypes.Structure):
                 ("rms_eps", ctypes.c_float), ("rope_theta", ctypes.c_float)]
 
 
+class _CacheF8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pool", "v_pool", "k_scale", "v_scale", "weight")]
+
+
+class _EvictRequest(ctypes.Structure):
+    _fields_ = [("len", ctypes.c_int32), ("keep", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("n_dst_pages", ctypes.c_int32),
+                ("pages", ctypes.POINTER(ctypes.c_int32)),
+                ("dst_pages", ctypes.POINTER(ctypes.c_int32))]
+
+
 class _Weights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("ln1_g", "w_qkv", "w_o", "ln2_g", "w_gate_up", "w_down")]
 
@@ -80,6 +92,7 @@ def _load() -> ctypes.CDLL:
     BP = ctypes.POINTER(_Batch)
     SP = ctypes.POINTER(AttnShape)
     CP = ctypes.POINTER(LayerCfg)
+    FP, EP = ctypes.POINTER(_CacheF8), ctypes.POINTER(_EvictRequest)
     sig = {
         "mx_status_str": ([ctypes.c_int], ctypes.c_char_p),
         "mx_last_error": ([], ctypes.c_char_p),
@@ -94,6 +107,12 @@ def _load() -> ctypes.CDLL:
         "mx_layer_step": ([BP, CP, P, P, P, P, P, P, SZ, P], ctypes.c_int),
         "mx_paged_attn_static": ([BP, SP, P, P, P, P, P], ctypes.c_int),
         "mx_paged_attn_static_max_bytes": ([], SZ),
+        "mx_kv_append_f8": ([BP, SP, P, P, FP, P], ctypes.c_int),
+        "mx_workspace_bytes_f8_for": ([BP, SP, I32], SZ),
+        "mx_workspace_bytes_f8": ([SP, I32, I32, I32, I64], SZ),
+        "mx_paged_attn_f8": ([BP, SP, P, FP, P, P, SZ, P], ctypes.c_int),
+        "mx_kv_evict_f8_ws_bytes": ([I32, EP, SP], SZ),
+        "mx_kv_evict_f8": ([I32, EP, SP, FP, P, P, SZ, P], ctypes.c_int),
         "mx_layer_workspace_offsets": ([BP, CP, ctypes.POINTER(SZ)], ctypes.c_int),
         "mx_debug_token_map": ([BP, SP, P, P, P, P, SZ, P], ctypes.c_int),
         "mx_debug_gather": ([BP, SP, I32, P, P, P, P, P, SZ, P], ctypes.c_int),
@@ -160,6 +179,59 @@ class Batch:
     @property
     def ptr(self):
         return ctypes.byref(self._batch)
+
+
+class CacheF8:
+    """A layer's 8-bit cache: device tensors in the layouts of mx_cache_f8, the pools
+    one byte per element (uint8 or float8_e4m3fn), scales and weight float32.  Holds
+    the tensors alive."""
+
+    def __init__(self, k_pool, v_pool, k_scale, v_scale, weight=None):
+        for name, t, size in (("k_pool", k_pool, 1), ("v_pool", v_pool, 1), ("k_scale", k_scale, 4),
+                              ("v_scale", v_scale, 4), ("weight", weight, 4)):
+            if t is not None and (t.element_size() != size or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous, {size} byte(s) per element")
+        heads, d = tuple(k_scale.shape), v_pool.shape[2]  # (pages, KV heads), head_dim
+        for name, t, shape in (("k_pool", k_pool, heads + (d // 64, 16, 64)),
+                               ("v_pool", v_pool, heads + (d, 16)), ("v_scale", v_scale, heads),
+                               ("weight", weight, heads + (16,))):
+            if t is not None and tuple(t.shape) != shape:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+        self.k_pool, self.v_pool, self.k_scale, self.v_scale = k_pool, v_pool, k_scale, v_scale
+        self.weight = weight
+        self._cache = _CacheF8(*(_ptr(t) for t in (k_pool, v_pool, k_scale, v_scale, weight)))
+
+    def ptr(self, shape: AttnShape):
+        """The C struct, for calls of `shape`."""
+        pages, heads = self.k_scale.shape
+        if (pages, heads, self.v_pool.shape[2]) != (shape.pool_pages, shape.n_kv_heads, shape.head_dim):
+            raise ValueError("the cache is not of this attention shape")
+        return ctypes.byref(self._cache)
+
+
+class EvictBatch:
+    """The requests of an eviction in the C layout: each from `length` cached tokens in
+    the pages of page_tables to its `keep` in those of dst_tables, the last `recent`
+    among them.  Holds the host arrays alive while in use."""
+
+    def __init__(self, length: Sequence[int], keep: Sequence[int], recent: Sequence[int],
+                 page_tables: Sequence[Sequence[int]], dst_tables: Sequence[Sequence[int]]):
+        R = len(length)
+        self._tables = [np.ascontiguousarray(t, dtype=np.int32)
+                        for r in range(R) for t in (page_tables[r], dst_tables[r])]
+        self._reqs = (_EvictRequest * max(R, 1))()
+        for r in range(R):
+            q, src, dst = self._reqs[r], self._tables[2 * r], self._tables[2 * r + 1]
+            q.len, q.keep, q.recent = int(length[r]), int(keep[r]), int(recent[r])
+            q.n_pages, q.n_dst_pages = len(src), len(dst)
+            q.pages = src.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)) if len(src) else None
+            q.dst_pages = dst.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)) if len(dst) else None
+        self.R = R
+        self.total_keep = int(sum(int(k) for k in keep))
+
+    @property
+    def ptr(self):
+        return self._reqs
 
 
 def attn_shape(n_q_heads, n_kv_heads, head_dim, pool_pages, scale=0.0, page_size=16) -> AttnShape:
@@ -254,6 +326,51 @@ def mx_layer_step(batch: Batch, cfg: LayerCfg, packed, x, y, k_pool, v_pool, ws,
                   stream=None) -> None:
     _check(_lib.mx_layer_step(batch.ptr, ctypes.byref(cfg), _ptr(packed), _ptr(x), _ptr(y),
                               _ptr(k_pool), _ptr(v_pool), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def mx_kv_append_f8(batch: Batch, shape: AttnShape, k_new, v_new, cache: CacheF8,
+                    stream=None) -> None:
+    """The new tokens' keys and values into the 8-bit cache."""
+    _check(_lib.mx_kv_append_f8(batch.ptr, ctypes.byref(shape), _ptr(k_new), _ptr(v_new),
+                                cache.ptr(shape), _stream(stream)))
+
+
+def mx_workspace_bytes_f8_for(batch: Batch, shape: AttnShape, track: bool = False) -> int:
+    """Workspace of mx_paged_attn_f8 for this batch (track: the cache has a weight)."""
+    n = _lib.mx_workspace_bytes_f8_for(batch.ptr, ctypes.byref(shape), int(track))
+    if n == 0:
+        raise MxError(MX_ERR_INVALID, last_error())
+    return int(n)
+
+
+def mx_workspace_bytes_f8(shape: AttnShape, track: bool, max_tokens: int, max_reqs: int,
+                          max_pages: int) -> int:
+    n = _lib.mx_workspace_bytes_f8(ctypes.byref(shape), int(track), max_tokens, max_reqs, max_pages)
+    if n == 0:
+        raise MxError(MX_ERR_INVALID, last_error())
+    return int(n)
+
+
+def mx_paged_attn_f8(batch: Batch, shape: AttnShape, q, cache: CacheF8, out, ws,
+                     stream=None) -> None:
+    """Attention over the 8-bit cache; adds to cache.weight where it has one."""
+    _check(_lib.mx_paged_attn_f8(batch.ptr, ctypes.byref(shape), _ptr(q), cache.ptr(shape), _ptr(out),
+                                 _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def mx_kv_evict_f8_ws_bytes(batch: EvictBatch, shape: AttnShape) -> int:
+    n = _lib.mx_kv_evict_f8_ws_bytes(batch.R, batch.ptr, ctypes.byref(shape))
+    if n == 0:
+        raise MxError(MX_ERR_INVALID, last_error())
+    return int(n)
+
+
+def mx_kv_evict_f8(batch: EvictBatch, shape: AttnShape, cache: CacheF8, kept, ws,
+                   stream=None) -> None:
+    """Copies the tokens that stay to the destination pages; kept (int32, n_kv_heads *
+    batch.total_keep elements) receives their indices."""
+    _check(_lib.mx_kv_evict_f8(batch.R, batch.ptr, ctypes.byref(shape), cache.ptr(shape), _ptr(kept),
+                               _ptr(ws), ws.numel(), _stream(stream)))
 
 
 def mx_layer_workspace_offsets(batch: Batch, cfg: LayerCfg) -> dict:

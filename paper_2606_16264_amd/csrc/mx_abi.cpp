@@ -9,6 +9,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <exception>
 #include <initializer_list>
 #include <map>
 #include <mutex>
@@ -194,7 +195,8 @@ struct Plan {
 // decodes over 1000-2000 tokens: 18.8 -> 17.2 us).
 constexpr int64_t kMinSplitPages = 16, kUnsplitPages = 32, kUnsplitPagesFull = 64, kCUs = 256;
 
-int choose_split_pages(const mx_batch* b, const mx_attn_shape* s) {
+// (step: pages that a wave takes at a time; splits are whole steps)
+int choose_split_pages(const mx_batch* b, const mx_attn_shape* s, int step) {
   const int group = s->n_q_heads / s->n_kv_heads;
   const int64_t sub = s->n_kv_heads * ceil_div(group, 16);
   int64_t total = 0, longest = 0, decodes = 0;
@@ -210,15 +212,18 @@ int choose_split_pages(const mx_batch* b, const mx_attn_shape* s) {
   sp = std::max(kMinSplitPages, std::min<int64_t>(sp, 4096));
   const int64_t whole = decodes * sub >= kCUs ? kUnsplitPagesFull : kUnsplitPages;
   if (longest <= whole) sp = std::max(sp, longest);
-  sp = (sp + 1) / 2 * 2;
+  sp = ceil_div(sp, step) * step;
   return (int)sp;
 }
 
-void build_plan(const mx_batch* b, const mx_attn_shape* s, bool with_items, Plan& p) {
+constexpr int kStepPages = 2, kStepPagesF8 = 4;
+
+void build_plan(const mx_batch* b, const mx_attn_shape* s, bool with_items, Plan& p,
+                int step = kStepPages) {
   p.batch = b;
   p.R = b->num_reqs;
   p.group = s->n_q_heads / s->n_kv_heads;
-  p.split_pages = choose_split_pages(b, s);
+  p.split_pages = choose_split_pages(b, s, step);
   p.reqs.resize(p.R);
   const int nq = s->n_q_heads;
   const int64_t sub = s->n_kv_heads * ceil_div(p.group, 16);  // decode items per split
@@ -697,6 +702,7 @@ AttnParams attn_params(const Plan& p, const Layout& L, const mx_attn_shape* s, v
   a.split_pages = p.split_pages;
   a.scale_log2 = eff_scale(s) * 1.4426950408889634f;
   a.decode_only = p.has_prefill ? 0 : 1;
+  a.lse = nullptr;
   return a;
 }
 
@@ -792,7 +798,7 @@ MX_EXPORT const char* mx_status_str(mx_status s) {
 
 MX_EXPORT const char* mx_last_error(void) { return g_err.c_str(); }
 
-MX_EXPORT uint32_t mx_version(void) { return (1u << 16) | 0u; }
+MX_EXPORT uint32_t mx_version(void) { return (1u << 16) | 1u; }
 
 // Device tensors are read and written with 16-byte vector accesses.
 static mx_status check_aligned(std::initializer_list<const void*> ptrs) {
@@ -896,6 +902,29 @@ static mx_status check_ws(const Layout& L, void* ws, size_t ws_bytes) {
   return MX_OK;
 }
 
+// The runs of a batch's new tokens, one per page that a request's touch.
+static int64_t count_runs(const mx_batch* batch) {
+  int64_t n = 0;
+  for (int r = 0; r < batch->num_reqs; r++) {
+    const mx_request& q = batch->reqs[r];
+    n += (q.ctx_len + q.n_new - 1) / 16 - q.ctx_len / 16 + 1;
+  }
+  return n;
+}
+static void pack_runs(const mx_batch* batch, AppendRun* run) {
+  int32_t tok = 0;
+  for (int r = 0; r < batch->num_reqs; r++) {
+    const mx_request& q = batch->reqs[r];
+    const int end = q.ctx_len + q.n_new;
+    for (int pos = q.ctx_len; pos < end;) {
+      const int n = std::min(16 - pos % 16, end - pos);
+      *run++ = AppendRun{tok, n, (int64_t)q.pages[pos / 16] * 16 + pos % 16};
+      tok += n;
+      pos += n;
+    }
+  }
+}
+
 MX_EXPORT mx_status mx_kv_append(const mx_batch* batch, const mx_attn_shape* shape,
                                  const uint16_t* k_new, const uint16_t* v_new, uint16_t* k_pool,
                                  uint16_t* v_pool, void* ws, size_t ws_bytes, hipStream_t stream) {
@@ -906,31 +935,15 @@ MX_EXPORT mx_status mx_kv_append(const mx_batch* batch, const mx_attn_shape* sha
   if (T == 0) return MX_OK;
   if (!k_new || !v_new || !k_pool || !v_pool) return fail(MX_ERR_NULL, "tensor pointer is NULL");
   if ((st = check_aligned({k_new, v_new, k_pool, v_pool, ws})) != MX_OK) return st;
-  // one run per page that a request's new tokens touch
-  int64_t n_pages = 0, n_runs = 0;
-  for (int r = 0; r < batch->num_reqs; r++) {
-    const mx_request& q = batch->reqs[r];
-    n_pages += ceil_div((int64_t)q.ctx_len + q.n_new, 16);
-    n_runs += (q.ctx_len + q.n_new - 1) / 16 - q.ctx_len / 16 + 1;
-  }
+  int64_t n_pages = 0;
+  for (int r = 0; r < batch->num_reqs; r++)
+    n_pages += ceil_div((int64_t)batch->reqs[r].ctx_len + batch->reqs[r].n_new, 16);
+  const int64_t n_runs = count_runs(batch);
   const Layout L = make_layout(batch->num_reqs, T, n_pages, 0, 0, 0, shape, nullptr, 0);
   if ((st = check_ws(L, ws, ws_bytes)) != MX_OK) return st;
   return staged(
       n_runs * sizeof(AppendRun), stream,
-      [&](char* h) {
-        AppendRun* run = reinterpret_cast<AppendRun*>(h);
-        int32_t tok = 0;
-        for (int r = 0; r < batch->num_reqs; r++) {
-          const mx_request& q = batch->reqs[r];
-          const int end = q.ctx_len + q.n_new;
-          for (int pos = q.ctx_len; pos < end;) {
-            const int n = std::min(16 - pos % 16, end - pos);
-            *run++ = AppendRun{tok, n, (int64_t)q.pages[pos / 16] * 16 + pos % 16};
-            tok += n;
-            pos += n;
-          }
-        }
-      },
+      [&](char* h) { pack_runs(batch, reinterpret_cast<AppendRun*>(h)); },
       [&](const void* dev) {
         return launch_kv_append(k_new, v_new, k_pool, v_pool, static_cast<const AppendRun*>(dev),
                                 n_runs, shape->n_kv_heads, shape->head_dim, stream);
@@ -1158,6 +1171,353 @@ MX_EXPORT mx_status mx_layer_step(const mx_batch* batch, const mx_layer_cfg* cfg
   }
 #undef MX_CK
   return MX_OK;
+}
+
+// ------------------------------------------------------------------ 8-bit cache
+namespace {
+
+mx_status check_cache(const mx_cache_f8* c) {
+  if (!c) return fail(MX_ERR_NULL, "cache is NULL");
+  if (!c->k_pool || !c->v_pool || !c->k_scale || !c->v_scale)
+    return fail(MX_ERR_NULL, "cache pointer is NULL");
+  return check_aligned({c->k_pool, c->v_pool, c->k_scale, c->v_scale, c->weight});
+}
+
+CacheF8 cache_args(const mx_cache_f8* c) {
+  return CacheF8{c->k_pool, c->v_pool, c->k_scale, c->v_scale, c->weight};
+}
+
+// The calls below plan in host containers: what those throw ends here.
+template <typename R, typename F>
+R no_throw(R failed, F&& f) {
+  try {
+    return f();
+  } catch (const std::exception& e) {
+    (void)fail(MX_ERR_TOO_LARGE, "planning on the host: %s", e.what());
+    return failed;
+  }
+}
+
+// These calls read host staging buffers that later calls write again, so a captured
+// one would read whatever lies there at its replay.
+mx_status check_not_capturing(hipStream_t stream) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &st) != hipSuccess) {
+    (void)hipGetLastError();
+    return MX_OK;
+  }
+  if (st != hipStreamCaptureStatusNone)
+    return fail(MX_ERR_UNSUPPORTED, "the call cannot be captured into a graph");
+  return MX_OK;
+}
+
+// The first page that two runs of the batch's new tokens touch, -1 if none: a page's
+// scale is written once per call.
+int64_t page_touched_twice(const mx_batch* b) {
+  std::vector<int32_t> touched;
+  for (int r = 0; r < b->num_reqs; r++) {
+    const mx_request& q = b->reqs[r];
+    for (int64_t pg = q.ctx_len / 16; pg <= ((int64_t)q.ctx_len + q.n_new - 1) / 16; pg++)
+      touched.push_back(q.pages[pg]);
+  }
+  std::sort(touched.begin(), touched.end());
+  const auto it = std::adjacent_find(touched.begin(), touched.end());
+  return it == touched.end() ? -1 : *it;
+}
+
+// Workspace of mx_paged_attn_f8: the metadata as for mx_paged_attn, then, where
+// weights are accumulated, where each request's scores start and the work items of
+// the two accumulation kernels; the split partials, the rows' sums of exponentials
+// and the decodes' scores.
+struct LayoutF8 {
+  Layout base;  // reqs, pages, items, merges, part_o, part_ml
+  size_t score_base = 0, dec = 0, pre = 0, meta_end = 0, lse = 0, scores = 0, total = 0;
+};
+
+LayoutF8 make_layout_f8(int64_t R, int64_t T, int64_t n_pages, int64_t n_items, int64_t n_merges,
+                        int64_t n_parts, int64_t n_dec, int64_t n_pre, int64_t n_scores,
+                        const mx_attn_shape* s, bool track) {
+  LayoutF8 F;
+  Layout& L = F.base;
+  size_t o = 0;
+  L.reqs = o; o = align_up(o + R * sizeof(ReqDev));
+  L.pages = o; o = align_up(o + n_pages * sizeof(int32_t));
+  L.items = o; o = align_up(o + n_items * sizeof(AttnItem));
+  L.merges = o; o = align_up(o + n_merges * sizeof(MergeItem));
+  L.meta_end = o;
+  if (track) {
+    F.score_base = o; o = align_up(o + R * sizeof(int64_t));
+    F.dec = o; o = align_up(o + n_dec * sizeof(WeightItem));
+    F.pre = o; o = align_up(o + n_pre * sizeof(WeightItem));
+  }
+  F.meta_end = o;
+  L.part_o = o; o = align_up(o + n_parts * s->head_dim * 4);
+  L.part_ml = o; o = align_up(o + n_parts * 8);
+  if (track) {
+    F.lse = o; o = align_up(o + T * s->n_q_heads * 4);
+    F.scores = o; o = align_up(o + n_scores * 4);
+  }
+  F.total = o;
+  return F;
+}
+
+struct PlanF8 {
+  Plan p;
+  int64_t n_dec = 0, n_pre = 0, n_scores = 0;
+  LayoutF8 L;
+};
+
+void build_plan_f8(const mx_batch* b, const mx_attn_shape* s, bool track, PlanF8& f) {
+  build_plan(b, s, true, f.p, kStepPagesF8);
+  if (track)
+    for (const ReqDev& d : f.p.reqs) {
+      if (d.phase == MX_DECODE) {
+        f.n_dec += ceil_div(d.n_pages, kWeightDecodePages);
+        f.n_scores += (int64_t)s->n_q_heads * 16 * d.n_pages;
+      } else {
+        f.n_pre += ceil_div(d.n_pages, kWeightPrefillPages);
+      }
+    }
+  f.L = make_layout_f8(f.p.R, f.p.T, f.p.n_pages, f.p.n_items, (int64_t)f.p.merges.size(),
+                       f.p.n_parts, f.n_dec, f.n_pre, f.n_scores, s, track);
+}
+
+void pack_meta_f8(const PlanF8& f, const mx_attn_shape* s, bool track, char* h) {
+  pack_meta(f.p, f.L.base, s, h);
+  if (!track) return;
+  int64_t* base = (int64_t*)(h + f.L.score_base);
+  WeightItem* dec = (WeightItem*)(h + f.L.dec);
+  WeightItem* pre = (WeightItem*)(h + f.L.pre);
+  int64_t at = 0;
+  for (int r = 0; r < f.p.R; r++) {
+    const ReqDev& d = f.p.reqs[r];
+    base[r] = at;
+    if (d.phase == MX_DECODE) {
+      at += (int64_t)s->n_q_heads * 16 * d.n_pages;
+      for (int pg = 0; pg < d.n_pages; pg += kWeightDecodePages) *dec++ = WeightItem{r, pg};
+    } else {
+      for (int pg = 0; pg < d.n_pages; pg += kWeightPrefillPages) *pre++ = WeightItem{r, pg};
+    }
+  }
+}
+
+}  // namespace
+
+MX_EXPORT size_t mx_workspace_bytes_f8_for(const mx_batch* batch, const mx_attn_shape* shape,
+                                           int32_t track) {
+  g_err.clear();
+  return no_throw((size_t)0, [&]() -> size_t {
+    if (validate_batch(batch, shape, nullptr) != MX_OK) return 0;
+    PlanF8 f;
+    build_plan_f8(batch, shape, track != 0, f);
+    return std::max(f.L.total, kAlign);
+  });
+}
+
+MX_EXPORT size_t mx_workspace_bytes_f8(const mx_attn_shape* shape, int32_t track,
+                                       int32_t max_tokens, int32_t max_reqs, int64_t max_pages) {
+  g_err.clear();
+  if (validate_shape(shape) != MX_OK) return 0;
+  if (max_tokens < 0 || max_reqs < 0 || max_pages < 0) {
+    fail(MX_ERR_INVALID, "negative bound");
+    return 0;
+  }
+  const int64_t nq = shape->n_q_heads, nkv = shape->n_kv_heads, group = nq / nkv;
+  const int64_t splits = max_pages / 8 + max_reqs;  // as in mx_workspace_bytes
+  const int64_t items =
+      splits * nkv * ceil_div(group, 16) + (max_tokens / kPrefillTileRows + max_reqs) * nq;
+  return std::max(make_layout_f8(max_reqs, max_tokens, max_pages, items, max_reqs, splits * nq,
+                                 max_pages / kWeightDecodePages + max_reqs,
+                                 max_pages / kWeightPrefillPages + max_reqs, nq * 16 * max_pages,
+                                 shape, track != 0)
+                      .total,
+                  kAlign);
+}
+
+MX_EXPORT mx_status mx_kv_append_f8(const mx_batch* batch, const mx_attn_shape* shape,
+                                    const uint16_t* k_new, const uint16_t* v_new,
+                                    const mx_cache_f8* cache, hipStream_t stream) {
+  g_err.clear();
+  return no_throw(MX_ERR_TOO_LARGE, [&]() -> mx_status {
+    int64_t T;
+    mx_status st = validate_batch(batch, shape, &T);
+    if (st != MX_OK) return st;
+    if ((st = check_cache(cache)) != MX_OK) return st;
+    if (T == 0) return MX_OK;
+    if (!k_new || !v_new) return fail(MX_ERR_NULL, "tensor pointer is NULL");
+    if ((st = check_aligned({k_new, v_new})) != MX_OK) return st;
+    if (const int64_t pg = page_touched_twice(batch); pg >= 0)
+      return fail(MX_ERR_INVALID, "two requests append to page %lld", (long long)pg);
+    if ((st = check_not_capturing(stream)) != MX_OK) return st;
+    const int64_t n_runs = count_runs(batch);
+    return staged(
+        n_runs * sizeof(AppendRun), stream,
+        [&](char* h) { pack_runs(batch, reinterpret_cast<AppendRun*>(h)); },
+        [&](const void* dev) {
+          return launch_kv_append_f8(k_new, v_new, cache_args(cache),
+                                     static_cast<const AppendRun*>(dev), n_runs, shape->n_kv_heads,
+                                     shape->head_dim, stream);
+        });
+  });
+}
+
+MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape* shape,
+                                     const uint16_t* q, const mx_cache_f8* cache, uint16_t* out,
+                                     void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_err.clear();
+  return no_throw(MX_ERR_TOO_LARGE, [&]() -> mx_status {
+    int64_t T;
+    mx_status st = validate_batch(batch, shape, &T);
+    if (st != MX_OK) return st;
+    if ((st = check_cache(cache)) != MX_OK) return st;
+    if (T == 0) return MX_OK;
+    if (!q || !out) return fail(MX_ERR_NULL, "tensor pointer is NULL");
+    if ((st = check_aligned({q, out, ws})) != MX_OK) return st;
+    const bool track = cache->weight != nullptr;
+    PlanF8 f;
+    build_plan_f8(batch, shape, track, f);
+    const LayoutF8& L = f.L;
+    if (!ws) return fail(MX_ERR_NULL, "workspace is NULL");
+    if (ws_bytes < L.total)
+      return fail(MX_ERR_TOO_LARGE, "workspace %zu bytes < %zu needed", ws_bytes, L.total);
+    if ((st = check_not_capturing(stream)) != MX_OK) return st;
+    st = staged(
+        L.meta_end, stream, [&](char* h) { pack_meta_f8(f, shape, track, h); },
+        [&](const void* dev) { return launch_upload(dev, ws, L.meta_end, stream); });
+    if (st != MX_OK) return st;
+    AttnF8Params a;
+    a.a = attn_params(f.p, L.base, shape, ws, q, (int64_t)shape->n_q_heads * shape->head_dim,
+                      nullptr, nullptr, out);
+    a.a.lse = track ? at<float>(ws, L.lse) : nullptr;
+    a.k8 = cache->k_pool;
+    a.v8 = cache->v_pool;
+    a.k_scale = cache->k_scale;
+    a.v_scale = cache->v_scale;
+    a.weight = cache->weight;
+    a.scores = at<float>(ws, L.scores);
+    a.score_base = at<int64_t>(ws, L.score_base);
+    const hipError_t e = timed("paged_attn_f8", stream, [&] {
+      return launch_paged_attn_f8(a, (int)f.p.n_items, at<MergeItem>(ws, L.base.merges),
+                                  (int)f.p.merges.size(), at<WeightItem>(ws, L.dec), (int)f.n_dec,
+                                  at<WeightItem>(ws, L.pre), (int)f.n_pre, shape->head_dim, stream);
+    });
+    if (e != hipSuccess) return hip_fail(e, "attention launch");
+    return MX_OK;
+  });
+}
+
+namespace {
+
+struct EvictPlan {
+  int64_t src_pages = 0, dst_pages = 0;
+  size_t pages = 0, items = 0, total = 0;  // offsets after the requests
+};
+
+mx_status validate_evict(int32_t R, const mx_evict_request* reqs, const mx_attn_shape* s,
+                         EvictPlan& p) {
+  mx_status st = validate_shape(s);
+  if (st != MX_OK) return st;
+  if (R < 0) return fail(MX_ERR_INVALID, "num_reqs %d < 0", R);
+  if (R > 0 && !reqs) return fail(MX_ERR_NULL, "reqs is NULL");
+  std::vector<int32_t> dst;
+  for (int r = 0; r < R; r++) {
+    const mx_evict_request& q = reqs[r];
+    if (q.len < 0 || q.keep < 0 || q.keep > q.len || q.recent < 0 || q.recent > q.keep)
+      return fail(MX_ERR_INVALID, "request %d: need 0 <= recent %d <= keep %d <= len %d", r,
+                  q.recent, q.keep, q.len);
+    if (q.len > INT32_MAX - 16) return fail(MX_ERR_TOO_LARGE, "request %d: context too long", r);
+    const int64_t ns = ceil_div(q.len, 16), nd = ceil_div(q.keep, 16);
+    if (q.n_pages < ns || q.n_dst_pages < nd)
+      return fail(MX_ERR_NO_SPACE, "request %d: %d pages and %d destination pages (need %lld, %lld)",
+                  r, q.n_pages, q.n_dst_pages, (long long)ns, (long long)nd);
+    if ((ns > 0 && !q.pages) || (nd > 0 && !q.dst_pages))
+      return fail(MX_ERR_NULL, "request %d: pages is NULL", r);
+    for (int64_t i = 0; i < ns + nd; i++) {
+      const int32_t pg = i < ns ? q.pages[i] : q.dst_pages[i - ns];
+      if (pg < 0 || pg >= s->pool_pages)
+        return fail(MX_ERR_INVALID, "request %d: page id %d outside [0, %lld)", r, pg,
+                    (long long)s->pool_pages);
+    }
+    dst.insert(dst.end(), q.dst_pages, q.dst_pages + nd);
+    p.src_pages += ns;
+    p.dst_pages += nd;
+    if (p.src_pages + p.dst_pages > INT32_MAX / 2) return fail(MX_ERR_TOO_LARGE, "too many pages");
+  }
+  // destination pages are nobody else's: neither another destination nor a source
+  std::sort(dst.begin(), dst.end());
+  const auto twice = std::adjacent_find(dst.begin(), dst.end());
+  if (twice != dst.end())
+    return fail(MX_ERR_INVALID, "page %d is the destination of two", *twice);
+  if (!dst.empty())
+    for (int r = 0; r < R; r++)
+      for (int64_t i = 0, ns = ceil_div(reqs[r].len, 16); i < ns; i++)
+        if (std::binary_search(dst.begin(), dst.end(), reqs[r].pages[i]))
+          return fail(MX_ERR_INVALID, "page %d is a source and a destination", reqs[r].pages[i]);
+  size_t o = align_up(R * sizeof(EvictReq));
+  p.pages = o; o = align_up(o + (p.src_pages + p.dst_pages) * sizeof(int32_t));
+  p.items = o; o = align_up(o + p.dst_pages * sizeof(EvictPage));
+  p.total = o;
+  return MX_OK;
+}
+
+}  // namespace
+
+MX_EXPORT size_t mx_kv_evict_f8_ws_bytes(int32_t num_reqs, const mx_evict_request* reqs,
+                                         const mx_attn_shape* shape) {
+  g_err.clear();
+  return no_throw((size_t)0, [&]() -> size_t {
+    EvictPlan p;
+    if (validate_evict(num_reqs, reqs, shape, p) != MX_OK) return 0;
+    return std::max(p.total, kAlign);
+  });
+}
+
+MX_EXPORT mx_status mx_kv_evict_f8(int32_t num_reqs, const mx_evict_request* reqs,
+                                   const mx_attn_shape* shape, const mx_cache_f8* cache,
+                                   int32_t* kept, void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_err.clear();
+  return no_throw(MX_ERR_TOO_LARGE, [&]() -> mx_status {
+    EvictPlan p;
+    mx_status st = validate_evict(num_reqs, reqs, shape, p);
+    if (st != MX_OK) return st;
+    if ((st = check_cache(cache)) != MX_OK) return st;
+    if (p.dst_pages == 0) return MX_OK;
+    if (!cache->weight) return fail(MX_ERR_NULL, "the cache has no weights");
+    if (!kept) return fail(MX_ERR_NULL, "kept is NULL");
+    if ((st = check_aligned({kept, ws})) != MX_OK) return st;
+    if (!ws) return fail(MX_ERR_NULL, "workspace is NULL");
+    if (ws_bytes < p.total)
+      return fail(MX_ERR_TOO_LARGE, "workspace %zu bytes < %zu needed", ws_bytes, p.total);
+    if ((st = check_not_capturing(stream)) != MX_OK) return st;
+    st = staged(
+        p.total, stream,
+        [&](char* h) {
+          EvictReq* er = (EvictReq*)h;
+          int32_t* pages = (int32_t*)(h + p.pages);
+          EvictPage* item = (EvictPage*)(h + p.items);
+          int64_t at_kept = 0;
+          int32_t pg = 0;
+          for (int r = 0; r < num_reqs; r++) {
+            const mx_evict_request& q = reqs[r];
+            const int32_t ns = (int32_t)ceil_div(q.len, 16), nd = (int32_t)ceil_div(q.keep, 16);
+            er[r] = EvictReq{q.len, q.keep, q.recent, pg, pg + ns, 0, at_kept};
+            if (ns) memcpy(pages + pg, q.pages, ns * sizeof(int32_t));
+            if (nd) memcpy(pages + pg + ns, q.dst_pages, nd * sizeof(int32_t));
+            for (int32_t i = 0; i < nd; i++) *item++ = EvictPage{r, 16 * i};
+            pg += ns + nd;
+            at_kept += (int64_t)shape->n_kv_heads * q.keep;
+          }
+        },
+        [&](const void* dev) { return launch_upload(dev, ws, p.total, stream); });
+    if (st != MX_OK) return st;
+    const hipError_t e = timed("kv_evict_f8", stream, [&] {
+      return launch_kv_evict_f8(at<EvictReq>(ws, 0), num_reqs, at<int32_t>(ws, p.pages),
+                                at<EvictPage>(ws, p.items), p.dst_pages, cache_args(cache), kept,
+                                shape->n_kv_heads, shape->head_dim, stream);
+    });
+    if (e != hipSuccess) return hip_fail(e, "eviction launch");
+    return MX_OK;
+  });
 }
 
 MX_EXPORT mx_status mx_layer_workspace_offsets(const mx_batch* batch, const mx_layer_cfg* cfg,

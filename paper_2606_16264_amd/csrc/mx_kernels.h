@@ -24,10 +24,63 @@ struct AttnParams {
   int32_t nq, nkv, group, split_pages;
   float scale_log2;        // softmax scale * log2(e)
   int32_t decode_only;     // no prefill items: decode keys and values are read non-temporally
+  float* lse;              // [T][nq] log2 of the row's sum of exponentials, or null
 };
 
 hipError_t launch_paged_attn(const AttnParams& p, int n_items, const MergeItem* merges,
                              int n_merges, int head_dim, hipStream_t stream);
+// The merge of the key splits alone (part of launch_paged_attn).
+hipError_t launch_attn_merge(const AttnParams& p, const MergeItem* merges, int n_merges,
+                             int head_dim, hipStream_t stream);
+
+// The 8-bit cache of a layer, as the ABI's mx_cache_f8.
+struct CacheF8 {
+  uint8_t *k, *v;           // [pages][nkv][d / 64][16][64] and [pages][nkv][d][16] e4m3 codes
+  float *k_scale, *v_scale; // [pages][nkv] powers of two
+  float* weight;            // [pages][nkv][16] accumulated attention weight, or null
+};
+
+// Keys of one request whose attention weight a workgroup accumulates: pages start ..
+// of its table, kWeightDecodePages of a decode's, kWeightPrefillPages of a chunk's.
+constexpr int kWeightDecodePages = 64, kWeightPrefillPages = 4;
+struct WeightItem {
+  int32_t req, start;
+};
+
+struct AttnF8Params {
+  AttnParams a;               // k_pool and v_pool unused; lse set where weight is
+  const uint8_t *k8, *v8;
+  const float *k_scale, *v_scale;
+  float* weight;              // null: weights are not accumulated
+  float* scores;              // decodes' scores in log2 units, [nq][16 n_pages] per request
+  const int64_t* score_base;  // [R] first score of the request
+};
+// The attention of the items, the merge of the key splits and, where p.weight is
+// set, the accumulation of the weights.
+hipError_t launch_paged_attn_f8(const AttnF8Params& p, int n_items, const MergeItem* merges,
+                                int n_merges, const WeightItem* dec, int n_dec,
+                                const WeightItem* pre, int n_pre, int head_dim,
+                                hipStream_t stream);
+
+// Append to the 8-bit cache, one run per page that new tokens touch (runs as for
+// launch_kv_append; no two of one page).
+hipError_t launch_kv_append_f8(const uint16_t* k_new, const uint16_t* v_new, const CacheF8& cache,
+                               const AppendRun* runs, int64_t n_runs, int nkv, int d,
+                               hipStream_t stream);
+
+// Eviction: src and dst are offsets of a request's page tables in the flat page
+// array, kept that of its first index in the kept array ([nkv][keep] per request).
+struct EvictReq {
+  int32_t len, keep, recent, src, dst, pad;
+  int64_t kept;
+};
+// A destination page: tokens start .. of the request's kept ones.
+struct EvictPage {
+  int32_t req, start;
+};
+hipError_t launch_kv_evict_f8(const EvictReq* reqs, int n_reqs, const int32_t* pages,
+                              const EvictPage* items, int64_t n_items, const CacheF8& cache,
+                              int32_t* kept, int nkv, int d, hipStream_t stream);
 
 // Copies `bytes` (a multiple of 16, both ends 16-byte aligned) from pinned host
 // memory, given by its device mapping, into device memory.  A kernel on the

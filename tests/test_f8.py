@@ -1,0 +1,226 @@
+"""CPU checks of the 8-bit cache's calls: every malformed argument is refused on the
+host with the documented status, before any device work; workspace sizes and their
+bounds; what the calls launch."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_16264_amd as mx
+from test_host_runtime import fake_hip, run  # noqa: F401  (fake_hip is a fixture)
+
+POOL = 64
+
+
+def shape(nq=4, nkv=2, d=64, pool=POOL):
+    return mx.attn_shape(nq, nkv, d, pool)
+
+
+def cache(s, weight=True):
+    P, g, d = s.pool_pages, s.n_kv_heads, s.head_dim
+    z = lambda *n, t=torch.uint8: torch.zeros(n, dtype=t)  # noqa: E731
+    return mx.CacheF8(z(P, g, d // 64, 16, 64), z(P, g, d, 16), z(P, g, t=torch.float32),
+                      z(P, g, t=torch.float32), z(P, g, 16, t=torch.float32) if weight else None)
+
+
+class Raw:
+    """A made-up device tensor."""
+
+    def __init__(self, ptr=0x100000, n=1 << 40):
+        self.p, self.n = ptr, n
+
+    def data_ptr(self):
+        return self.p
+
+    def numel(self):
+        return self.n
+
+
+def raw_cache(**changed):
+    c = {n: 0x200000 for n in ("k_pool", "v_pool", "k_scale", "v_scale", "weight")}
+    c.update(changed)
+    return mx._CacheF8(*(c[n] for n in ("k_pool", "v_pool", "k_scale", "v_scale", "weight")))
+
+
+def one(phase=mx.MX_PREFILL, n_new=4, ctx=0, pages=(1,)):
+    return mx.Batch([phase], [n_new], [ctx], [pages])
+
+
+def append(b, s, c, k=0x100000, v=0x100000):
+    return mx.lib().mx_kv_append_f8(b.ptr, ctypes.byref(s), k, v, ctypes.byref(c) if c else None, None)
+
+
+def attn(b, s, c, q=0x100000, out=0x110000, ws=0x120000, n=1 << 40):
+    return mx.lib().mx_paged_attn_f8(b.ptr, ctypes.byref(s), q, ctypes.byref(c) if c else None, out,
+                                     ws, n, None)
+
+
+def evict(e, s, c, kept=0x100000, ws=0x120000, n=1 << 40):
+    return mx.lib().mx_kv_evict_f8(e.R, e.ptr, ctypes.byref(s), ctypes.byref(c) if c else None, kept,
+                                   ws, n, None)
+
+
+BAD_BATCHES = [
+    (mx.Batch([7], [1], [5], [[0]]), mx.MX_ERR_INVALID),
+    (one(n_new=0), mx.MX_ERR_INVALID),
+    (one(mx.MX_DECODE, 1, 0), mx.MX_ERR_INVALID),
+    (one(n_new=2, ctx=15), mx.MX_ERR_NO_SPACE),
+    (one(pages=[POOL]), mx.MX_ERR_INVALID),
+    (one(pages=[-1]), mx.MX_ERR_INVALID),
+    (mx.Batch([0, 1], [3, 1], [0, 2], [[5], [5]]), mx.MX_ERR_INVALID),
+]
+
+
+@pytest.mark.parametrize("b,status", BAD_BATCHES)
+def test_bad_batches(b, status):
+    for call in (append, attn):
+        assert call(b, shape(), raw_cache()) == status
+        assert mx.last_error()
+
+
+@pytest.mark.parametrize("s,status", [
+    (shape(4, 3), mx.MX_ERR_INVALID),
+    (shape(d=96), mx.MX_ERR_UNSUPPORTED),
+    (shape(pool=0), mx.MX_ERR_INVALID),
+])
+def test_bad_shapes(s, status):
+    e = mx.EvictBatch([4], [2], [1], [[1]], [[2]])
+    assert append(one(), s, raw_cache()) == status
+    assert attn(one(), s, raw_cache()) == status
+    assert evict(e, s, raw_cache()) == status
+    assert mx.lib().mx_workspace_bytes_f8(ctypes.byref(s), 1, 10, 10, 10) == 0
+    assert mx.lib().mx_kv_evict_f8_ws_bytes(e.R, e.ptr, ctypes.byref(s)) == 0
+
+
+def test_bad_caches_and_pointers():
+    e = mx.EvictBatch([4], [2], [1], [[1]], [[2]])
+    for call in (lambda c: append(one(), shape(), c), lambda c: attn(one(), shape(), c),
+                 lambda c: evict(e, shape(), c)):
+        assert call(None) == mx.MX_ERR_NULL
+        for name in ("k_pool", "v_pool", "k_scale", "v_scale"):
+            assert call(raw_cache(**{name: None})) == mx.MX_ERR_NULL
+            assert call(raw_cache(**{name: 0x200008})) == mx.MX_ERR_INVALID
+        assert call(raw_cache(weight=0x200004)) == mx.MX_ERR_INVALID
+    c = raw_cache()
+    assert append(one(), shape(), c, k=None) == mx.MX_ERR_NULL
+    assert append(one(), shape(), c, v=0x100002) == mx.MX_ERR_INVALID
+    for kw, status in ((dict(q=None), mx.MX_ERR_NULL), (dict(out=None), mx.MX_ERR_NULL),
+                       (dict(ws=None), mx.MX_ERR_NULL), (dict(q=0x100008), mx.MX_ERR_INVALID),
+                       (dict(ws=0x120004), mx.MX_ERR_INVALID), (dict(n=255), mx.MX_ERR_TOO_LARGE)):
+        assert attn(one(), shape(), c, **kw) == status, kw
+    for kw, status in ((dict(kept=None), mx.MX_ERR_NULL), (dict(ws=None), mx.MX_ERR_NULL),
+                       (dict(kept=0x100004), mx.MX_ERR_INVALID), (dict(n=255), mx.MX_ERR_TOO_LARGE)):
+        assert evict(e, shape(), c, **kw) == status, kw
+    assert evict(e, shape(), raw_cache(weight=None)) == mx.MX_ERR_NULL
+
+
+def test_append_refuses_a_page_of_two_requests():
+    # distinct slots of one page: fine for a byte copy, not for a page with one scale
+    b = mx.Batch([1, 1], [1, 1], [3, 4], [[5], [5]])
+    assert mx.mx_batch_validate(b, shape()) == mx.MX_OK
+    assert append(b, shape(), raw_cache()) == mx.MX_ERR_INVALID
+    assert "page 5" in mx.last_error()
+    # a shared prefix page that only one of them writes is fine as far as the host sees
+    b = mx.Batch([1, 1], [1, 1], [16, 3], [[5, 6], [7]])
+    assert append(b, shape(), raw_cache()) in (mx.MX_OK, mx.MX_ERR_HIP)
+
+
+@pytest.mark.parametrize("args,status", [
+    (([4], [5], [0], [[1]], [[2]]), mx.MX_ERR_INVALID),          # keep > len
+    (([4], [-1], [0], [[1]], [[2]]), mx.MX_ERR_INVALID),
+    (([-1], [0], [0], [[1]], [[2]]), mx.MX_ERR_INVALID),
+    (([4], [2], [3], [[1]], [[2]]), mx.MX_ERR_INVALID),          # recent > keep
+    (([4], [2], [-1], [[1]], [[2]]), mx.MX_ERR_INVALID),
+    (([17], [2], [1], [[1]], [[2]]), mx.MX_ERR_NO_SPACE),
+    (([40], [17], [1], [[1, 3, 4]], [[2]]), mx.MX_ERR_NO_SPACE),
+    (([4], [2], [1], [[]], [[2]]), mx.MX_ERR_NO_SPACE),
+    (([4], [2], [1], [[POOL]], [[2]]), mx.MX_ERR_INVALID),
+    (([4], [2], [1], [[1]], [[-2]]), mx.MX_ERR_INVALID),
+    (([4], [2], [1], [[1]], [[1]]), mx.MX_ERR_INVALID),          # its own source
+    (([4, 4], [2, 2], [1, 1], [[1], [2]], [[3], [3]]), mx.MX_ERR_INVALID),
+    (([4, 4], [2, 2], [1, 1], [[1], [2]], [[3], [1]]), mx.MX_ERR_INVALID),  # another's source
+    (([40], [20], [1], [[1, 3, 4]], [[2, 2]]), mx.MX_ERR_INVALID),
+])
+def test_bad_evictions(args, status):
+    e = mx.EvictBatch(*args)
+    assert evict(e, shape(), raw_cache()) == status
+    assert mx.last_error()
+    assert mx.lib().mx_kv_evict_f8_ws_bytes(e.R, e.ptr, ctypes.byref(shape())) == 0
+
+
+def test_empty_calls_are_no_ops():
+    s, c = shape(), raw_cache()
+    empty = mx.Batch([], [], [], [])
+    assert append(empty, s, c) == attn(empty, s, c) == mx.MX_OK
+    assert evict(mx.EvictBatch([], [], [], [], []), s, c) == mx.MX_OK
+    assert evict(mx.EvictBatch([20, 0], [0, 0], [0, 0], [[1, 2], []], [[], []]), s, c) == mx.MX_OK
+    # a shared prefix is a source of two requests, only destinations are their own
+    e = mx.EvictBatch([4, 4], [2, 2], [1, 1], [[1], [1]], [[3], [4]])
+    assert mx.mx_kv_evict_f8_ws_bytes(e, s) > 0
+    assert mx.mx_workspace_bytes_f8_for(empty, s) > 0
+
+
+def test_binding_checks_the_cache():
+    s = shape()
+    c = cache(s)
+    with pytest.raises(ValueError):  # heads of another shape
+        mx.mx_kv_append_f8(one(), shape(4, 4), Raw(), Raw(), c, stream=0)
+    with pytest.raises(ValueError):  # pages the tensors do not have
+        mx.mx_paged_attn_f8(one(), shape(pool=POOL + 1), Raw(), c, Raw(), Raw(), stream=0)
+    with pytest.raises(ValueError):
+        mx.CacheF8(c.k_pool, c.v_pool, c.k_scale, c.v_scale.double())
+    with pytest.raises(ValueError):
+        mx.CacheF8(c.k_pool.transpose(3, 4), c.v_pool, c.k_scale, c.v_scale)
+    with pytest.raises(ValueError):
+        mx.CacheF8(c.k_pool, c.v_pool[1:], c.k_scale, c.v_scale)
+    with pytest.raises(ValueError):
+        mx.CacheF8(c.k_pool, c.v_pool, c.k_scale, c.v_scale, c.weight[:, :1].contiguous())
+
+
+@pytest.mark.parametrize("track", [False, True])
+def test_workspace_bound_covers_batches(track):
+    rng = np.random.default_rng(5)
+    for _ in range(60):
+        nkv = int(rng.choice([1, 2, 8]))
+        s = shape(nkv * int(rng.choice([1, 4, 20])), nkv, int(rng.choice([64, 128])), 1 << 20)
+        R = int(rng.integers(1, 9))
+        dec = rng.random(R) < 0.6
+        ctx = rng.integers(1, rng.choice([20, 300, 40000]), R)
+        new = np.where(dec, 1, rng.integers(1, 400, R))
+        need = -(-(ctx + new) // 16)
+        at = np.cumsum(np.concatenate([[0], need]))
+        b = mx.Batch(dec.astype(int), new, ctx, [np.arange(at[r], at[r + 1]) for r in range(R)])
+        exact = mx.mx_workspace_bytes_f8_for(b, s, track)
+        assert exact <= mx.mx_workspace_bytes_f8(s, track, int(new.sum()), R, int(need.sum()))
+
+
+def test_launches(fake_hip):  # noqa: F811
+    """The kernels of each call, and staging buffers that outlive their readers."""
+    r = run(fake_hip, """
+        import ctypes
+        s = mx.attn_shape(8, 2, 128, 1 << 20)
+        c = lambda w: ctypes.byref(mx._CacheF8(1 << 20, 2 << 20, 3 << 20, 4 << 20, w))
+        calls = {
+            "append": lambda st: mx.lib().mx_kv_append_f8(batch(3, 20).ptr, ctypes.byref(s), A(0), A(1), c(None), st),
+            "attn": lambda st: mx.lib().mx_paged_attn_f8(batch(3, 20).ptr, ctypes.byref(s), A(0), c(None), A(1), A(2), BIG, st),
+            "track": lambda st: mx.lib().mx_paged_attn_f8(batch(3, 20).ptr, ctypes.byref(s), A(0), c(5 << 20), A(1), A(2), BIG, st),
+        }
+        e = mx.EvictBatch([40, 3], [20, 0], [4, 0], [[1, 2, 3], [4]], [[5, 6], []])
+        calls["evict"] = lambda st: mx.lib().mx_kv_evict_f8(2, e.ptr, ctypes.byref(s), c(5 << 20), A(0), A(2), BIG, st)
+        kernels, st = {}, []
+        for name, f in calls.items():
+            n = len(log())
+            st.append(f(None))
+            kernels[name] = [l[0] for l in log()[n:]]
+        for i in range(60):
+            st += [f([None, None, A(30), None, A(31)][i % 5]) for f in calls.values()]
+        print(json.dumps(dict(kernels=kernels, st=st, bad=fake.fake_violations())))
+        """)
+    assert set(r["st"]) == {0} and r["bad"] == 0
+    got = {k: [next(n for n in ("upload", "kv_append_f8", "paged_attn_f8", "weight_decode",
+                                "weight_prefill", "evict_select", "evict_move") if n in x)
+               for x in v] for k, v in r["kernels"].items()}
+    assert got == {"append": ["kv_append_f8"], "attn": ["upload", "paged_attn_f8"],
+                   "track": ["upload", "paged_attn_f8", "weight_decode", "weight_prefill"],
+                   "evict": ["upload", "evict_select", "evict_move"]}
