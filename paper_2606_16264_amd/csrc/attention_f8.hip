@@ -21,13 +21,6 @@ namespace mx {
 
 namespace {
 
-template <int HD>
-struct Chunk8 {
-  u32x4 k[4][HD / 64];  // key codes: 16 dims of one key per lane per (score block, 64 dims)
-  u32x4 v[HD / 16];     // value codes: the 16 tokens of a page per lane per 16 dims
-  float ks, vs;         // scales of the lane's key page and of its value page
-};
-
 // Eight codes times a power of two as bf16 (exact).  The instruction reads the
 // scale's exponent only.
 __device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b, float scale) {
@@ -39,37 +32,11 @@ __device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b, float scale) {
                          __builtin_bit_cast(uint32_t, w2), __builtin_bit_cast(uint32_t, w3)});
 }
 
-// The keys of the step that starts at page pi: page ids of this lane's key and
-// value pages (past the range: its last page, whose keys are masked there).
-struct PageIds {
-  int k, v;
-};
-__device__ __forceinline__ PageIds page_ids(const int32_t* ptab, int pi, int page_end, int col,
-                                            int g4) {
-  return PageIds{ptab[min(pi + (col >> 2), page_end - 1)], ptab[min(pi + g4, page_end - 1)]};
-}
-
 template <bool NT>
 __device__ __forceinline__ u32x4 load16(const uint8_t* ptr) {
   const u32x4* q = reinterpret_cast<const u32x4*>(ptr);
   if constexpr (NT) return __builtin_nontemporal_load(q);
   else return *q;
-}
-
-template <int HD, bool NT>
-__device__ __forceinline__ void load_chunk(Chunk8<HD>& c, const AttnF8Params& p, int kvh,
-                                           const PageIds& id, int col, int g4) {
-  const int64_t kp = (int64_t)id.k * p.a.nkv + kvh, vp = (int64_t)id.v * p.a.nkv + kvh;
-  const uint8_t* k = p.k8 + kp * (16 * HD) + (col & 3) * 64 + 16 * g4;
-  const uint8_t* v = p.v8 + vp * (16 * HD) + col * 16;
-  c.ks = p.k_scale[kp];
-  c.vs = p.v_scale[vp];
-#pragma unroll
-  for (int b = 0; b < 4; b++)
-#pragma unroll
-    for (int h = 0; h < HD / 64; h++) c.k[b][h] = load16<NT>(k + h * 1024 + b * 256);
-#pragma unroll
-  for (int db = 0; db < HD / 16; db++) c.v[db] = load16<true>(v + db * 256);
 }
 
 // This lane's part of a query row as the first product's B operands: 8 dims
@@ -99,19 +66,20 @@ __device__ __forceinline__ f32x4 score_block(const u32x4 (&k)[HD / 64], float ks
   return s;
 }
 
-// This lane's 16 raw scores of the step (keys past the range or after the row's
-// position masked to kNegBig by select) and their max.
-template <bool MASK>
-__device__ __forceinline__ float masked_scores(const f32x4 (&s)[4], float (&sv)[4][4], int page,
-                                               int page_end, int row_pos) {
+// Keys past the range or after the row's position: their scores become kNegBig.
+__device__ __forceinline__ void mask_scores(f32x4 (&s)[4], int page, int page_end, int row_pos) {
+  const int n = page < page_end ? row_pos - page * 16 : -1;  // the page's last key that counts
+#pragma unroll
+  for (int b = 0; b < 4; b++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) s[b][i] = 4 * b + i <= n ? s[b][i] : kNegBig;
+}
+__device__ __forceinline__ float scores_max(const f32x4 (&s)[4]) {
   float mx = kNegBig;
 #pragma unroll
   for (int b = 0; b < 4; b++)
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      sv[b][i] = (!MASK || (page < page_end && page * 16 + 4 * b + i <= row_pos)) ? s[b][i] : kNegBig;
-      mx = fmaxf(mx, sv[b][i]);
-    }
+    for (int i = 0; i < 4; i++) mx = fmaxf(mx, s[b][i]);
   return mx;
 }
 
@@ -122,7 +90,7 @@ __device__ __forceinline__ float masked_scores(const f32x4 (&s)[4], float (&sv)[
 // which the accumulated weights need: theirs is an fp32 result, and the rounded
 // sum of a row is off by up to 2^-9.
 template <bool EXACT>
-__device__ __forceinline__ void probs(const float (&sv)[4][4], RowState& r, float scale_log2,
+__device__ __forceinline__ void probs(const f32x4 (&sv)[4], RowState& r, float scale_log2,
                                       bf16x8 (&pb)[2]) {
   const mx_bf16x2 ones = __builtin_bit_cast(mx_bf16x2, 0x3F803F80u);
 #pragma unroll
@@ -164,101 +132,107 @@ __device__ __forceinline__ void value_keep(int page, int page_end, int kv_len,
 }
 
 // O^T += V^T P^T over the output blocks DB0 .. DB0 + NDB - 1 (16 head dims each).
-template <int HD, int DB0, int NDB, bool MASK>
-__device__ __forceinline__ void values_part(const u32x4 (&vf)[NDB], float vs, f32x4 (&o)[HD / 16],
-                                            const bf16x8 (&pb)[2], const uint32_t (&keep)[4]) {
+template <int HD, int DB0, int NDB>
+__device__ __forceinline__ void values_part(const u32x4 (&v)[NDB], float vs, f32x4 (&o)[HD / 16],
+                                            const bf16x8 (&pb)[2]) {
 #pragma unroll
   for (int e = 0; e < NDB; e++) {
-    u32x4 v = vf[e];
-    if constexpr (MASK) {
-#pragma unroll
-      for (int w = 0; w < 4; w++) v[w] &= keep[w];
-    }
-    o[DB0 + e] = mfma16(widen(v[0], v[1], vs), pb[0], o[DB0 + e]);
-    o[DB0 + e] = mfma16(widen(v[2], v[3], vs), pb[1], o[DB0 + e]);
+    o[DB0 + e] = mfma16(widen(v[e][0], v[e][1], vs), pb[0], o[DB0 + e]);
+    o[DB0 + e] = mfma16(widen(v[e][2], v[e][3], vs), pb[1], o[DB0 + e]);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// What a wave's 16 query rows scan: pages first, first + step .. of those below
-// page_end, 64 keys each (four pages), up to the row's own position.
-struct Scan {
-  int first, step, page_end, row_pos, first_row_pos, kv_len;
-};
-
-// One 64-key step of the online softmax for this lane's query row.  scores: where
-// to leave the lane's 16 scores in log2 units, or null.
-template <int HD, bool MASK, bool TRACK>
-__device__ __forceinline__ void process_chunk(const Chunk8<HD>& c, const bf16x8 (&qf)[HD / 32],
-                                              f32x4 (&o)[HD / 16], RowState& r, int pi,
-                                              const Scan& sc, float scale_log2, float inv_scale,
-                                              int g4, float* scores) {
-  f32x4 s[4];
-#pragma unroll
-  for (int b = 0; b < 4; b++) s[b] = score_block<HD>(c.k[b], c.ks, qf);
-  float sv[4][4];
-  const int page = pi + g4;
-  const float mx = masked_scores<MASK>(s, sv, page, sc.page_end, sc.row_pos);
-  if constexpr (TRACK) {
-    if (scores && (!MASK || page < sc.page_end)) {
-#pragma unroll
-      for (int b = 0; b < 4; b++)
-        *reinterpret_cast<f32x4*>(scores + page * 16 + 4 * b) =
-            f32x4{sv[b][0], sv[b][1], sv[b][2], sv[b][3]} * scale_log2;
-    }
-  }
-  if (__any(mx > r.thr)) raise_max(r, mx, scale_log2, inv_scale, o);
-  bf16x8 pb[2];
-  probs<TRACK>(sv, r, scale_log2, pb);
-  uint32_t keep[4];
-  value_keep(page, sc.page_end, sc.kv_len, keep);
-  values_part<HD, 0, HD / 16, MASK>(c.v, c.vs, o, pb, keep);
-}
-
-// The scan from global memory: two chunk buffers used in turn, the next chunk's
-// loads in flight while the current one is processed, page ids fetched one chunk
-// ahead of their loads.  Unrolled by two so that no buffer is ever copied.
+// The scan of a decode: the wave's 64-key steps at pages pi, pi + 16 .. below
+// page_end.  One register buffer for the keys of a step and one for its values, each
+// filled again for the next step as soon as its products have been taken: the next
+// keys are in flight during the softmax and the value products, the next values
+// during the next score products.  (Two buffers of both, in turn, took more than the
+// 256 registers of a wave, and a spilled register comes back behind every load in
+// flight: 256 decodes of the 8B heads 651 us.)  Only a wave's last step can hold keys
+// that do not count.  The loads are unconditional on every path, so that the waits
+// cover exactly what they need.
 template <int HD, bool NT, bool TRACK>
-__device__ __forceinline__ void scan_rows(const AttnF8Params& p, const int32_t* ptab, int kvh,
-                                          const Scan& sc, const bf16x8 (&qf)[HD / 32],
-                                          f32x4 (&o)[HD / 16], RowState& r, int col, int g4,
-                                          float* scores) {
-  const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
-  auto ids = [&](int pi) { return page_ids(ptab, pi, sc.page_end, col, g4); };
-  auto proc = [&](const Chunk8<HD>& c, int pi) {
-    // all 64 keys count for every row of the wave: no mask is needed
-    if (pi + 3 < sc.page_end && pi * 16 + 63 <= sc.first_row_pos)
-      process_chunk<HD, false, TRACK>(c, qf, o, r, pi, sc, scale, inv_scale, g4, scores);
-    else
-      process_chunk<HD, true, TRACK>(c, qf, o, r, pi, sc, scale, inv_scale, g4, scores);
-  };
-  int pi = sc.first;
-  if (pi >= sc.page_end) return;
-  Chunk8<HD> ca, cb;
-  PageIds n = ids(pi + sc.step);
-  load_chunk<HD, NT>(ca, p, kvh, ids(pi), col, g4);
-  while (true) {
-    int pn = pi + sc.step;
-    if (pn >= sc.page_end) {
-      proc(ca, pi);
-      break;
-    }
-    PageIds nn = ids(pn + sc.step);
-    load_chunk<HD, NT>(cb, p, kvh, n, col, g4);
-    proc(ca, pi);
-    pi = pn;
-    n = nn;
-    pn = pi + sc.step;
-    if (pn >= sc.page_end) {
-      proc(cb, pi);
-      break;
-    }
-    nn = ids(pn + sc.step);
-    load_chunk<HD, NT>(ca, p, kvh, n, col, g4);
-    proc(cb, pi);
-    pi = pn;
-    n = nn;
+struct DecodeScan {
+  const AttnF8Params& p;
+  const int32_t* ptab;
+  int kvh, page_end, row_pos, kv_len, col, g4;
+  float scale, inv_scale;
+  float* scores;  // where to leave the lane's scores in log2 units, or null
+  u32x4 k[4][HD / 64], v[HD / 16];
+  float ks, vs;
+
+  // the lane's key and value pages (past the range: its last page, masked there)
+  __device__ __forceinline__ int key_page(int pi) const { return ptab[min(pi + (col >> 2), page_end - 1)]; }
+  __device__ __forceinline__ int value_page(int pi) const { return ptab[min(pi + g4, page_end - 1)]; }
+  __device__ __forceinline__ void load_keys(int page) {
+    const int64_t at = (int64_t)page * p.a.nkv + kvh;
+    const uint8_t* src = p.k8 + at * (16 * HD) + (col & 3) * 64 + 16 * g4;
+    ks = p.k_scale[at];
+#pragma unroll
+    for (int b = 0; b < 4; b++)
+#pragma unroll
+      for (int h = 0; h < HD / 64; h++) k[b][h] = load16<NT>(src + h * 1024 + b * 256);
   }
-}
+  __device__ __forceinline__ void load_values(int page) {
+    const int64_t at = (int64_t)page * p.a.nkv + kvh;
+    const uint8_t* src = p.v8 + at * (16 * HD) + col * 16;
+    vs = p.v_scale[at];
+#pragma unroll
+    for (int db = 0; db < HD / 16; db++) v[db] = load16<true>(src + db * 256);
+  }
+  __device__ __forceinline__ void score(const bf16x8 (&qf)[HD / 32], f32x4 (&s)[4]) {
+#pragma unroll
+    for (int b = 0; b < 4; b++) {
+      s[b] = score_block<HD>(k[b], ks, qf);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  template <bool LAST>
+  __device__ __forceinline__ void softmax(f32x4 (&s)[4], int pi, RowState& r, f32x4 (&o)[HD / 16],
+                                          bf16x8 (&pb)[2]) {
+    const int page = pi + g4;
+    if constexpr (LAST) mask_scores(s, page, page_end, row_pos);
+    if constexpr (TRACK) {
+      if (scores && (!LAST || page < page_end)) {
+#pragma unroll
+        for (int b = 0; b < 4; b++)
+          *reinterpret_cast<f32x4*>(scores + page * 16 + 4 * b) = s[b] * scale;
+      }
+    }
+    const float mx = scores_max(s);
+    if (__any(mx > r.thr)) raise_max(r, mx, scale, inv_scale, o);
+    probs<TRACK>(s, r, scale, pb);
+  }
+  __device__ __forceinline__ void run(int pi, const bf16x8 (&qf)[HD / 32], f32x4 (&o)[HD / 16],
+                                      RowState& r) {
+    if (pi >= page_end) return;
+    f32x4 s[4];
+    bf16x8 pb[2];
+    load_keys(key_page(pi));
+    load_values(value_page(pi));
+    int kn = key_page(pi + 16), vn = value_page(pi + 16);
+    for (; pi + 16 < page_end; pi += 16) {
+      score(qf, s);
+      const int kn2 = key_page(pi + 32), vn2 = value_page(pi + 32);
+      load_keys(kn);
+      softmax<false>(s, pi, r, o, pb);
+      values_part<HD, 0, HD / 16>(v, vs, o, pb);
+      load_values(vn);
+      kn = kn2;
+      vn = vn2;
+    }
+    score(qf, s);
+    softmax<true>(s, pi, r, o, pb);
+    uint32_t keep[4];
+    value_keep(pi + g4, page_end, kv_len, keep);
+#pragma unroll
+    for (int db = 0; db < HD / 16; db++)
+#pragma unroll
+      for (int w = 0; w < 4; w++) v[db][w] &= keep[w];
+    values_part<HD, 0, HD / 16>(v, vs, o, pb);
+  }
+};
 
 // Decode item: the q heads it.head .. it.head + nrows - 1 (one per lane row) of the
 // request's single token, over pages it.start .. of its table; the four waves
@@ -267,7 +241,7 @@ template <int HD, bool NT, bool TRACK>
 __device__ __forceinline__ void decode_item(const AttnF8Params& p, const AttnItem& it,
                                             const ReqDev& rq, char* smem) {
   const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15;  // q head of this lane (relative to it.head)
   const int g4 = lane >> 4;   // lane group
   const bool row_valid = col < it.nrows;
@@ -279,18 +253,15 @@ __device__ __forceinline__ void decode_item(const AttnF8Params& p, const AttnIte
   for (int db = 0; db < HD / 16; db++) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   bf16x8 qf[HD / 32];
   load_q<HD>(p, qtok, qhead, row_valid, g4, qf);
-  Scan sc;
-  sc.first = it.start + 4 * wave;
-  sc.step = 16;
-  sc.page_end = min(it.start + p.a.split_pages, rq.n_pages);
-  sc.row_pos = sc.first_row_pos = rq.kv_len - 1;
-  sc.kv_len = rq.kv_len;
   float* scores = nullptr;
   if constexpr (TRACK) {
     if (row_valid) scores = p.scores + p.score_base[it.req] + (int64_t)qhead * 16 * rq.n_pages;
   }
-  scan_rows<HD, NT, TRACK>(p, p.a.pages + rq.page_start, it.head / p.a.group, sc, qf, o, r, col, g4,
-                           scores);
+  DecodeScan<HD, NT, TRACK> scan{p, p.a.pages + rq.page_start, it.head / p.a.group,
+                                 min(it.start + p.a.split_pages, rq.n_pages), rq.kv_len - 1,
+                                 rq.kv_len, col, g4, p.a.scale_log2, 1.f / p.a.scale_log2, scores,
+                                 {}, {}, 0.f, 0.f};
+  scan.run(it.start + 4 * wave, qf, o, r);
 
   float(*s_o)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(smem);
   float(*s_m)[16] = reinterpret_cast<float(*)[16]>(smem + 4 * 16 * (HD + 4) * 4);
@@ -345,61 +316,372 @@ __device__ __forceinline__ void decode_item(const AttnF8Params& p, const AttnIte
   }
 }
 
-// Prefill item: one q head, rows it.start .. it.start + 127 of the chunk, two
-// blocks of 16 rows per wave.
+// Prefill tiles share every 64-key chunk through LDS.  Wave w copies page w of the
+// chunk there with the DMA path (global_load_lds, 16 bytes per lane): its keys, its
+// values and, by an ordinary store, its two scales.  Keys keep the page's layout but
+// for the four 16-byte pieces of a 64-byte run, stored at piece i ^ key_swizzle(w): the
+// 16 lanes that the LDS serves at a time ({0-3, 12-15, 20-23, 24-27} and so on) then
+// hit distinct bank groups, in both pairs of pages that such a set reads.  Values are
+// unswizzled: the sets' 16 rows are distinct modulo 16 already.
+__device__ __forceinline__ int key_swizzle(int page) { return (4 - page) & 3; }
+template <int HD>
+struct SharedChunk8 {
+  static constexpr int PAGE = 16 * HD;        // bytes of a page's keys (values) of one head
+  static constexpr int BYTES = 8 * PAGE;      // a chunk: four pages' keys, then their values
+  static constexpr int SLOTS = 4;             // chunks kt .. kt + 3: copies run three ahead
+  static constexpr int NLD = 2 * PAGE / 1024; // 1 KB copies per wave per chunk
+  static constexpr int SCALES = SLOTS * BYTES;  // [slot][page] (key scale, value scale)
+};
+template <int HD>
+constexpr int smem_bytes() {
+  constexpr int ring = SharedChunk8<HD>::SCALES + SharedChunk8<HD>::SLOTS * 4 * 8;
+  constexpr int combine = (4 * 16 * (HD + 4) + 2 * 4 * 16) * 4;
+  return ring > combine ? ring : combine;
+}
+
+// The 4 bytes at LDS address addr + OFF; a pair of words there.
+template <int OFF>
+__device__ __forceinline__ uint32_t lds_read4_at(unsigned addr) {
+  uint32_t v;
+  asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF));
+  return v;
+}
+__device__ __forceinline__ void lds_write8(unsigned addr, u32x2 v) {
+  asm volatile("ds_write_b64 %0, %1" ::"v"(addr), "v"(v) : "memory");
+}
+__device__ __forceinline__ void pin1(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
+// Prefill item: one q head, rows it.start .. it.start + 127 of the chunk; wave w owns
+// two blocks of 16 consecutive rows, it.start + 32 w + (0 | 16) + col.
+//
+// Iteration kt of the chunk loop reads the keys of chunk kt + 1 for the score products
+// while the exponentials of chunk kt (whose scores the previous iteration left) run on
+// the vector units, then takes the value products of chunk kt, and raises the rows'
+// running max for chunk kt + 1 where needed.  The copies of chunk kt + 3 go out at the
+// top of iteration kt into the slot chunk kt - 1 used, after the barrier that ends
+// every wave's reads of it, and the scales of that chunk's page are read (scalar
+// loads) with them and stored to LDS one iteration later.  Every iteration issues the
+// same copies (chunks past the tile's last one copy the tile's last page into the free
+// slot and are never read), and they are the only vector-memory operations of the
+// loop, so one vmcnt value fits every wait: at the top of iteration kt the copies of
+// iteration kt - 1 may still be in flight, every earlier one (chunk kt + 1) has landed.
+static_assert(kPrefillTileRows == 4 * 32, "four waves of two 16-row blocks");
 template <int HD, bool TRACK>
 __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnItem& it,
-                                             const ReqDev& rq) {
+                                             const ReqDev& rq, char* smem) {
+  using SC = SharedChunk8<HD>;
+  constexpr int CB = SC::BYTES, NLD = SC::NLD, NH = HD / 64, ND = HD / 32;
   const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
-  const int col = lane & 15;  // query row of this lane within the block
-  const int g4 = lane >> 4;
-  for (int blk = 0; blk < 2; blk++) {
-    const int row0 = it.start + 32 * wave + 16 * blk;
-    if (row0 >= rq.n_new) return;
-    const int row = min(row0 + col, rq.n_new - 1);
-    const int64_t qtok = rq.tok_start + row;
-    RowState r = row_start();
-    f32x4 o[HD / 16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15;  // query row of this lane within each block
+  const int g4 = lane >> 4;   // lane group
+  const int qhead = it.head;
+  const int kvh = qhead / p.a.group;
+  const int row0 = it.start + 32 * wave;
+  const int row = row0 + col, row2 = row0 + 16 + col;
+  const bool row_valid = row < rq.n_new, row_valid2 = row2 < rq.n_new;
+  const int rowc = row_valid ? row : rq.n_new - 1;
+  const int rowc2 = row_valid2 ? row2 : rq.n_new - 1;
+  const int64_t qtok = rq.tok_start + rowc, qtok2 = rq.tok_start + rowc2;
+  const int row_pos = rq.ctx_len + rowc, row_pos2 = rq.ctx_len + rowc2;
+  const int last_row = min(row0 + 31, rq.n_new - 1);
+  const int page_end = row0 < rq.n_new ? (rq.ctx_len + last_row) / 16 + 1 : 0;
+  const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
+
+  bf16x8 qf[ND], qf2[ND];
+  load_q<HD>(p, qtok, qhead, row_valid, g4, qf);
+  load_q<HD>(p, qtok2, qhead, row_valid2, g4, qf2);
+  RowState r1 = row_start(), r2 = row_start();
+  f32x4 o[HD / 16], o2[HD / 16];
 #pragma unroll
-    for (int db = 0; db < HD / 16; db++) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    bf16x8 qf[HD / 32];
-    load_q<HD>(p, qtok, it.head, true, g4, qf);
-    Scan sc;
-    sc.first = 0;
-    sc.step = 4;
-    sc.row_pos = rq.ctx_len + row;
-    sc.first_row_pos = rq.ctx_len + row0;
-    sc.page_end = (rq.ctx_len + min(row0 + 15, rq.n_new - 1)) / 16 + 1;
-    sc.kv_len = rq.kv_len;
-    scan_rows<HD, false, TRACK>(p, p.a.pages + rq.page_start, it.head / p.a.group, sc, qf, o, r,
-                                col, g4, nullptr);
-    const float l = lane_groups_sum(r.l);
-    if (row0 + col >= rq.n_new) continue;
+  for (int db = 0; db < HD / 16; db++) o[db] = o2[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // the tile's last row bounds the pages every wave helps to copy
+  const int tile_last = min(it.start + kPrefillTileRows - 1, rq.n_new - 1);
+  const int item_pages = (rq.ctx_len + tile_last) / 16 + 1;
+  const int n_chunks = (item_pages + 3) / 4;
+  const int wave_chunks = (page_end + 3) / 4;  // 0 for a wave without valid rows
+  // page ids and scales through the constant address space: uniform reads of tables
+  // nothing writes during the launch, so they are scalar loads
+  typedef const __attribute__((address_space(4))) int32_t* ConstInts;
+  typedef const __attribute__((address_space(4))) float* ConstFloats;
+  const ConstInts ptab = (ConstInts)(p.a.pages + rq.page_start);
+  const ConstFloats k_scale = (ConstFloats)p.k_scale, v_scale = (ConstFloats)p.v_scale;
+
+  // byte offsets in the page of this lane's share of a key copy (of 64 dims) and of a
+  // value copy: the LDS is written in lane order
+  const unsigned k_off = (lane >> 2) * 64 + (((lane & 3) ^ key_swizzle(wave)) << 4);
+  const unsigned v_off = lane * 16;
+  const unsigned lds0 = (unsigned)(size_t)(MX_LDS char*)smem;
+  const unsigned dst0 = lds0 + (unsigned)(wave * SC::PAGE);
+  const unsigned scale0 = lds0 + SC::SCALES;
+  auto copy = [&](int c, int page) {  // the wave's copies of chunk c
+    const int64_t at = ((int64_t)page * p.a.nkv + kvh) * SC::PAGE;
+    const uint8_t *kp = p.k8 + at, *vp = p.v8 + at;
+    const unsigned dst = dst0 + (unsigned)((c & 3) * CB);
+#pragma unroll
+    for (int h = 0; h < NH; h++) dma16_at(kp, k_off + 1024 * h, dst + 1024 * h);
+#pragma unroll
+    for (int h = 0; h < NH; h++) dma16_at(vp, v_off + 1024 * h, dst + 4 * SC::PAGE + 1024 * h);
+  };
+  struct Scales {
+    float k, v;
+  };
+  auto scales_of = [&](int page) {
+    const int64_t at = (int64_t)page * p.a.nkv + kvh;
+    return Scales{k_scale[at], v_scale[at]};
+  };
+  auto put_scales = [&](int c, const Scales& s) {
+    if (lane == 0)
+      lds_write8(scale0 + (unsigned)((c & 3) * 32 + wave * 8),
+                 u32x2{__float_as_uint(s.k), __float_as_uint(s.v)});
+  };
+  // the page this wave copies of chunk c (past the tile's last page: that page, whose
+  // keys are masked there)
+  auto page_of = [&](int c) { return ptab[min(4 * c + wave, item_pages - 1)]; };
+
+  // fragment addresses within a slot: score block b of key rows kappa_b(col) is 256
+  // bytes after block b - 1, 64 dims are 1 KB; value dim rows 16 e + col of page g4
+  const int kpage = col >> 2;
+  const unsigned kaddr = lds0 + (unsigned)(kpage * SC::PAGE + (col & 3) * 64 +
+                                           ((g4 ^ key_swizzle(kpage)) << 4));
+  const unsigned vaddr = lds0 + (unsigned)((4 + g4) * SC::PAGE + col * 16);
+  const unsigned ks_addr = scale0 + kpage * 8, vs_addr = scale0 + g4 * 8;
+
+  // (slot: the chunk's ring slot as a constant, which then is part of the read
+  // instructions, or -1)
+  // raw scores of chunk c from its keys in LDS, their max, and whether some lane of
+  // the wave is above its row's threshold
+  f32x4 s1[4], s2[4];
+  float mx1 = kNegBig, mx2 = kNegBig;
+  auto scores = [&](auto mask, auto slot, int c) -> bool {
+    constexpr bool MASK = decltype(mask)::value;
+    constexpr int S = decltype(slot)::value, OFF = S >= 0 ? S * CB : 0, SOFF = S >= 0 ? S * 32 : 0;
+    const unsigned ka = S >= 0 ? kaddr : kaddr + (unsigned)((c & 3) * CB);
+    uint32_t ks = lds_read4_at<SOFF>(S >= 0 ? ks_addr : ks_addr + (unsigned)((c & 3) * 32));
+    u32x4 k[4][NH];
+    auto read = [&](auto b) {
+      constexpr int B = decltype(b)::value;
+      k[B][0] = lds_read16_at<OFF + B * 256>(ka);
+      if constexpr (NH == 2) k[B][1] = lds_read16_at<OFF + B * 256 + 1024>(ka);
+    };
+    auto block = [&](auto b) {
+      constexpr int B = decltype(b)::value;
+      lgkm_wait<(3 - B) * NH>();
+      if constexpr (B == 0) pin1(ks);
+      pin(k[B]);
+      const float kf = __uint_as_float(ks);
+      f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f}, a2 = a;
+#pragma unroll
+      for (int h = 0; h < NH; h++)
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+          const bf16x8 w = widen(k[B][h][2 * i], k[B][h][2 * i + 1], kf);
+          a = mfma16(w, qf[2 * h + i], a);
+          a2 = mfma16(w, qf2[2 * h + i], a2);
+        }
+      s1[B] = a;
+      s2[B] = a2;
+      __builtin_amdgcn_sched_barrier(0);  // these products go before the next wait
+    };
+    using std::integral_constant;
+    read(integral_constant<int, 0>{});
+    read(integral_constant<int, 1>{});
+    read(integral_constant<int, 2>{});
+    read(integral_constant<int, 3>{});
+    block(integral_constant<int, 0>{});
+    block(integral_constant<int, 1>{});
+    block(integral_constant<int, 2>{});
+    block(integral_constant<int, 3>{});
+    if constexpr (MASK) {
+      mask_scores(s1, 4 * c + g4, page_end, row_pos);
+      mask_scores(s2, 4 * c + g4, page_end, row_pos2);
+    }
+    mx1 = scores_max(s1);
+    mx2 = scores_max(s2);
+    return __any(mx1 > r1.thr || mx2 > r2.thr) != 0;
+  };
+  // value products of chunk c (values past the request's keys zeroed when MASK: only
+  // the chunk that holds the request's last key has such values)
+  auto values = [&](auto mask, auto slot, int c, const bf16x8 (&pb1)[2], const bf16x8 (&pb2)[2]) {
+    constexpr bool MASK = decltype(mask)::value;
+    constexpr int S = decltype(slot)::value, OFF = S >= 0 ? S * CB : 0, SOFF = S >= 0 ? S * 32 : 0;
+    constexpr int Q = HD / 64;  // value rows per part: four parts
+    const unsigned va = S >= 0 ? vaddr : vaddr + (unsigned)((c & 3) * CB);
+    uint32_t vs = lds_read4_at<SOFF + 4>(S >= 0 ? vs_addr : vs_addr + (unsigned)((c & 3) * 32));
+    u32x4 v[4][Q];
+    lds_read_run<0, Q, OFF, 256>(va, v[0]);
+    lds_read_run<0, Q, OFF + Q * 256, 256>(va, v[1]);
+    lds_read_run<0, Q, OFF + 2 * Q * 256, 256>(va, v[2]);
+    lds_read_run<0, Q, OFF + 3 * Q * 256, 256>(va, v[3]);
+    uint32_t keep[4];
+    if constexpr (MASK) value_keep(4 * c + g4, page_end, rq.kv_len, keep);
+    auto part = [&](auto b) {
+      constexpr int B = decltype(b)::value;
+      lgkm_wait<(3 - B) * Q>();
+      if constexpr (B == 0) pin1(vs);
+      pin(v[B]);
+#pragma unroll
+      for (int e = 0; e < Q; e++) {
+        u32x4 w = v[B][e];
+        if constexpr (MASK) {
+#pragma unroll
+          for (int i = 0; i < 4; i++) w[i] &= keep[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+          const bf16x8 f = widen(w[2 * i], w[2 * i + 1], __uint_as_float(vs));
+          o[B * Q + e] = mfma16(f, pb1[i], o[B * Q + e]);
+          o2[B * Q + e] = mfma16(f, pb2[i], o2[B * Q + e]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);  // these products go before the next wait
+    };
+    part(std::integral_constant<int, 0>{});
+    part(std::integral_constant<int, 1>{});
+    part(std::integral_constant<int, 2>{});
+    part(std::integral_constant<int, 3>{});
+  };
+  auto raise_rows = [&]() {
+    raise_max(r1, mx1, scale, inv_scale, o);
+    raise_max(r2, mx2, scale, inv_scale, o2);
+  };
+  using Masked = std::integral_constant<bool, true>;
+  using Unmasked = std::integral_constant<bool, false>;
+
+  // prologue: the copies of chunks 0 .. 2, the scales of chunks 0 and 1 in LDS
+  int ua, fa = 0;  // page of the chunk the next copy is for, and of the one after
+  Scales sc;       // scales of the chunk copied last
+  {
+    const int a0 = page_of(0), a1 = page_of(1), a2 = page_of(2);
+    copy(0, a0);
+    copy(1, a1);
+    ua = page_of(3);
+    copy(2, a2);
+    put_scales(0, scales_of(a0));
+    put_scales(1, scales_of(a1));
+    sc = scales_of(a2);
+  }
+  // top of iteration kt: this wave's copies of chunk kt + 1 have landed and its scale
+  // stores are done, then everyone's, and every read of chunk kt - 1 is done; chunk
+  // kt + 3 goes out, the scales of chunk kt + 2 go to LDS
+  auto top = [&](int kt, int& use, int& fill) {
+    vm_wait<NLD>();
+    lgkm_wait<0>();
+    wg_barrier();
+    put_scales(kt + 2, sc);
+    fill = page_of(kt + 4);
+    sc = scales_of(use);
+    copy(kt + 3, use);
+  };
+  auto run = [&](int kt0, int kt1, auto body) {  // iterations kt0 .. kt1 - 1
+    for (int kt = kt0; kt < kt1; kt += 2) {
+      top(kt, ua, fa);
+      body(kt);
+      if (kt + 1 >= kt1) {  // an odd count: the next iteration uses fa
+        const int t = ua;
+        ua = fa;
+        fa = t;
+        break;
+      }
+      top(kt + 1, fa, ua);
+      body(kt + 1);
+    }
+  };
+
+  // chunk 0 and the first scales have landed; chunks 1 and 2 may be in flight
+  vm_wait<2 * NLD>();
+  lgkm_wait<0>();
+  wg_barrier();
+  if (row0 >= rq.n_new) {
+    // no rows here: this wave only copies its page of every chunk
+    run(0, n_chunks, [](int) {});
+    vm_wait<0>();  // no copy may land in LDS after the workgroup has ended
+    return;
+  }
+  if (scores(Masked{}, std::integral_constant<int, 0>{}, 0)) raise_rows();  // the first step raises every row's max
+
+  // Chunks 0 .. n_int - 1 are inside every wave's range and at or before every row of
+  // the tile: no masks.  The last chunk of the tile is the only one that can hold keys
+  // past the request's end, so n_main <= n_chunks - 1.
+  const int first_pos = rq.ctx_len + it.start;
+  const int page_end0 = (rq.ctx_len + min(it.start + 31, rq.n_new - 1)) / 16 + 1;  // wave 0's
+  const int n_int = first_pos >= 63 ? min((first_pos - 63) / 64 + 1, page_end0 / 4) : 0;
+  const int n_main = max(0, n_int - 1);
+  auto step = [&](auto slot, int kt) {  // slot: kt % 4 or -1
+    constexpr int S = decltype(slot)::value, S1 = S < 0 ? -1 : (S + 1) % 4;
+    bf16x8 pb1[2], pb2[2];
+    probs<TRACK>(s1, r1, scale, pb1);
+    probs<TRACK>(s2, r2, scale, pb2);
+    const bool raise = scores(Unmasked{}, std::integral_constant<int, S1>{}, kt + 1);
+    values(Unmasked{}, slot, kt, pb1, pb2);
+    if (raise) raise_rows();
+  };
+  // four chunks at a time, whose ring slots are constants in the fragment reads
+  const int n4 = n_main & ~3;
+  for (int kt = 0; kt < n4; kt += 4) {
+    top(kt, ua, fa);
+    step(std::integral_constant<int, 0>{}, kt);
+    top(kt + 1, fa, ua);
+    step(std::integral_constant<int, 1>{}, kt + 1);
+    top(kt + 2, ua, fa);
+    step(std::integral_constant<int, 2>{}, kt + 2);
+    top(kt + 3, fa, ua);
+    step(std::integral_constant<int, 3>{}, kt + 3);
+  }
+  using AnySlot = std::integral_constant<int, -1>;
+  run(n4, n_main, [&](int kt) { step(AnySlot{}, kt); });
+  // the chunks around the diagonal and the tile's end, with masks and bounds
+  run(n_main, n_chunks, [&](int kt) {
+    const bool more = kt + 1 < wave_chunks;  // scores of chunk kt + 1
+    if (kt < wave_chunks) {
+      bf16x8 pb1[2], pb2[2];
+      probs<TRACK>(s1, r1, scale, pb1);
+      probs<TRACK>(s2, r2, scale, pb2);
+      values(Masked{}, AnySlot{}, kt, pb1, pb2);
+    }
+    if (more && scores(Masked{}, AnySlot{}, kt + 1)) raise_rows();
+  });
+  vm_wait<0>();  // no copy may land in LDS after the workgroup has ended
+
+  // the rows' sums over their four lane groups (every lane takes part)
+  const float l1 = lane_groups_sum(r1.l), l2 = lane_groups_sum(r2.l);
+  // dims 16 db + 4 g4 .. + 3 of the row: (db / 2) 32-column steps plus 16 (db % 2)
+  const int64_t step32 = p.a.out_tiled ? 512 : 32;
+  auto store = [&](int64_t tok, float l, const RowState& r, const f32x4 (&acc)[HD / 16]) {
     const float inv = 1.f / l;
-    const int64_t step32 = p.a.out_tiled ? 512 : 32;
-    uint16_t* op = out_ptr(p.a, qtok, it.head * HD + 4 * g4);
+    uint16_t* op = out_ptr(p.a, tok, qhead * HD + 4 * g4);
 #pragma unroll
     for (int db = 0; db < HD / 16; db++) {
       u32x2 w;
-      w[0] = pack_bf16x2(o[db][0] * inv, o[db][1] * inv);
-      w[1] = pack_bf16x2(o[db][2] * inv, o[db][3] * inv);
+      w[0] = pack_bf16x2(acc[db][0] * inv, acc[db][1] * inv);
+      w[1] = pack_bf16x2(acc[db][2] * inv, acc[db][3] * inv);
       *reinterpret_cast<u32x2*>(op + (db >> 1) * step32 + (db & 1) * 16) = w;
     }
-    if (TRACK && g4 == 0) p.a.lse[qtok * p.a.nq + it.head] = r.m + log2f(l);
-  }
+    if (TRACK && g4 == 0) p.a.lse[tok * p.a.nq + qhead] = r.m + log2f(l);
+  };
+  if (row_valid) store(qtok, l1, r1, o);
+  if (row_valid2) store(qtok2, l2, r2, o2);
+}
+
+// Launches of decode splits alone run a kernel of their own: without the prefill
+// tiles' registers and LDS, three waves fit a SIMD.
+template <int HD, bool TRACK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void decode_attn_f8_kernel(
+    AttnF8Params p) {
+  __shared__ __attribute__((aligned(16))) char smem[(4 * 16 * (HD + 4) + 2 * 4 * 16) * 4];
+  const AttnItem it = p.a.items[blockIdx.x];
+  decode_item<HD, true, TRACK>(p, it, p.a.reqs[it.req], smem);
 }
 
 template <int HD, bool TRACK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void paged_attn_f8_kernel(
     AttnF8Params p) {
-  __shared__ __attribute__((aligned(16))) char smem[(4 * 16 * (HD + 4) + 2 * 4 * 16) * 4];
+  __shared__ __attribute__((aligned(16))) char smem[smem_bytes<HD>()];
   const AttnItem it = p.a.items[blockIdx.x];
   const ReqDev rq = p.a.reqs[it.req];
   if (it.kind == 1)
-    prefill_item<HD, TRACK>(p, it, rq);
-  else if (p.a.decode_only)
-    decode_item<HD, true, TRACK>(p, it, rq, smem);
+    prefill_item<HD, TRACK>(p, it, rq, smem);
   else
     decode_item<HD, false, TRACK>(p, it, rq, smem);
 }
@@ -508,7 +790,11 @@ hipError_t launch(const AttnF8Params& p, int n_items, const MergeItem* merges, i
                   const WeightItem* dec, int n_dec, const WeightItem* pre, int n_pre,
                   hipStream_t stream) {
   if (n_items > 0) {
-    if (p.weight)
+    if (p.a.decode_only && p.weight)
+      decode_attn_f8_kernel<HD, true><<<n_items, 256, 0, stream>>>(p);
+    else if (p.a.decode_only)
+      decode_attn_f8_kernel<HD, false><<<n_items, 256, 0, stream>>>(p);
+    else if (p.weight)
       paged_attn_f8_kernel<HD, true><<<n_items, 256, 0, stream>>>(p);
     else
       paged_attn_f8_kernel<HD, false><<<n_items, 256, 0, stream>>>(p);
