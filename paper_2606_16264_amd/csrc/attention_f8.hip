@@ -90,32 +90,35 @@ __device__ __forceinline__ float scores_max(const f32x4 (&s)[4]) {
 // which the accumulated weights need: theirs is an fp32 result, and the rounded
 // sum of a row is off by up to 2^-9.
 template <bool EXACT>
-__device__ __forceinline__ void probs(const f32x4 (&sv)[4], RowState& r, float scale_log2,
-                                      bf16x8 (&pb)[2]) {
+__device__ __forceinline__ bf16x8 half_probs(const f32x4& s0, const f32x4& s1, RowState& r,
+                                             float scale_log2) {
   const mx_bf16x2 ones = __builtin_bit_cast(mx_bf16x2, 0x3F803F80u);
+  float pv[2][4];
 #pragma unroll
-  for (int h = 0; h < 2; h++) {
-    float pv[2][4];
-#pragma unroll
-    for (int b = 0; b < 2; b++)
-#pragma unroll
-      for (int i = 0; i < 4; i++)
-        pv[b][i] = fast_exp2(fmaf(sv[2 * h + b][i], scale_log2, -r.m));
-    const uint32_t w0 = pack_bf16x2(pv[0][0], pv[0][1]);
-    const uint32_t w1 = pack_bf16x2(pv[0][2], pv[0][3]);
-    const uint32_t w2 = pack_bf16x2(pv[1][0], pv[1][1]);
-    const uint32_t w3 = pack_bf16x2(pv[1][2], pv[1][3]);
-    if constexpr (EXACT) {
-      r.l += ((pv[0][0] + pv[0][1]) + (pv[0][2] + pv[0][3])) +
-             ((pv[1][0] + pv[1][1]) + (pv[1][2] + pv[1][3]));
-    } else {
-      r.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, w0), ones, r.l, false);
-      r.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, w1), ones, r.l, false);
-      r.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, w2), ones, r.l, false);
-      r.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, w3), ones, r.l, false);
-    }
-    pb[h] = as_bf16x8(u32x4{w0, w1, w2, w3});
+  for (int i = 0; i < 4; i++) {
+    pv[0][i] = fast_exp2(fmaf(s0[i], scale_log2, -r.m));
+    pv[1][i] = fast_exp2(fmaf(s1[i], scale_log2, -r.m));
   }
+  const uint32_t w0 = pack_bf16x2(pv[0][0], pv[0][1]);
+  const uint32_t w1 = pack_bf16x2(pv[0][2], pv[0][3]);
+  const uint32_t w2 = pack_bf16x2(pv[1][0], pv[1][1]);
+  const uint32_t w3 = pack_bf16x2(pv[1][2], pv[1][3]);
+  if constexpr (EXACT) {
+    r.l += ((pv[0][0] + pv[0][1]) + (pv[0][2] + pv[0][3])) +
+           ((pv[1][0] + pv[1][1]) + (pv[1][2] + pv[1][3]));
+  } else {
+    r.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, w0), ones, r.l, false);
+    r.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, w1), ones, r.l, false);
+    r.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, w2), ones, r.l, false);
+    r.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx_bf16x2, w3), ones, r.l, false);
+  }
+  return as_bf16x8(u32x4{w0, w1, w2, w3});
+}
+template <bool EXACT>
+__device__ __forceinline__ void probs(const f32x4 (&s)[4], RowState& r, float scale_log2,
+                                      bf16x8 (&pb)[2]) {
+  pb[0] = half_probs<EXACT>(s[0], s[1], r, scale_log2);
+  pb[1] = half_probs<EXACT>(s[2], s[3], r, scale_log2);
 }
 
 // Which of the 16 tokens of this lane's value page hold values (bytes of a value
@@ -316,6 +319,98 @@ __device__ __forceinline__ void decode_item(const AttnF8Params& p, const AttnIte
   }
 }
 
+// A prefill tile's query rows as the B operand of the score products.
+//
+// Where no weights are accumulated the products take the key codes as they are, with the
+// 16x16x128 fp8 instruction, which multiplies each operand by a power of two per row
+// (the page's scale, the row's scale) on the way; the query goes in as two codes per
+// element, q = (hi + lo / 16) * scale: hi carries the upper four of a bf16 value's eight
+// significant bits, lo the rest, so that the sum is q itself (to 2^-22 of the row's
+// largest element, where lo ends).  That takes as long on the matrix cores as bf16
+// products do and saves the conversion of the keys, half the conversions of a tile: 489
+// -> 445 us for 2048 tokens over 14336 of the 8B heads.
+// The instruction aligns its products before it adds them: scores come out within
+// 2^-15 of sum |q k| (2e-5 of the largest score measured on normal data), a hundredth
+// of what the probabilities' rounding to bf16 does to them.  The accumulated weights
+// are fp32 results, so there (TRACK) keys are widened to bf16 and the products exact.
+typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8;
+__device__ __forceinline__ i32x8 join(u32x4 a, u32x4 b) {
+  return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// 16x16x128: A's rows times B's columns, each times 2^(byte 0 of its lane's scale - 127).
+// k index 16 g + j is byte j of lane group g, 64 + 16 g + j its byte 16 + j; the scale
+// of lane group g belongs to k indices 32 g .. 32 g + 31.
+__device__ __forceinline__ f32x4 mfma_f8(i32x8 a, int as, i32x8 b, int bs, f32x4 c) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, as, 0, bs);
+}
+template <int HD>
+struct CodedQuery {
+  // HD = 128: hi and lo one product each; HD = 64: k indices 0 .. 63 are hi, 64 .. 127 lo
+  i32x8 op[HD / 64];
+  int exp[HD / 64];
+
+  __device__ __forceinline__ void load(const AttnF8Params& p, int64_t tok, int qhead, bool valid,
+                                       int g4) {
+    bf16x8 q[HD / 32];
+    load_q<HD>(p, tok, qhead, valid, g4, q);
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < HD / 32; e++)
+#pragma unroll
+      for (int i = 0; i < 8; i++) amax = fmaxf(amax, __builtin_fabsf((float)q[e][i]));
+    amax = lane_groups_max(amax);
+    // the least 2^e with amax <= 448 * 2^e (an infinite row's codes are NaN anyway)
+    const uint32_t bits = __float_as_uint(amax);
+    const int e8 = min(max((int)(bits >> 23) - 8 + ((bits & 0x7FFFFF) > 0x600000), 27), 247);
+    const float inv = __uint_as_float((uint32_t)(254 - e8) << 23);
+    u32x4 hi[HD / 64], lo[HD / 64];
+#pragma unroll
+    for (int h = 0; h < HD / 64; h++)
+#pragma unroll
+      for (int w = 0; w < 4; w++) {
+        int ch = 0, cl = 0;
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) x[i] = (float)q[2 * h + (w >> 1)][4 * (w & 1) + i] * inv;
+        ch = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], ch, false);
+        ch = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], ch, true);
+        const mx_f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(ch, false);
+        const mx_f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(ch, true);
+        cl = __builtin_amdgcn_cvt_pk_fp8_f32((x[0] - a[0]) * 16.f, (x[1] - a[1]) * 16.f, cl, false);
+        cl = __builtin_amdgcn_cvt_pk_fp8_f32((x[2] - b[0]) * 16.f, (x[3] - b[1]) * 16.f, cl, true);
+#pragma unroll
+        for (int i = 0; i < 4; i++)  // not finite: NaN, whatever the conversion makes of it
+          if (!(__builtin_fabsf(x[i]) <= 448.f)) ch |= 0x7F << (8 * i);
+        hi[h][w] = (uint32_t)ch;
+        lo[h][w] = (uint32_t)cl;
+      }
+    if constexpr (HD == 128) {
+      op[0] = join(hi[0], hi[1]);
+      op[1] = join(lo[0], lo[1]);
+      exp[0] = e8;
+      exp[1] = e8 - 4;
+    } else {
+      op[0] = join(hi[0], lo[0]);
+      exp[0] = g4 < 2 ? e8 : e8 - 4;
+    }
+  }
+  // a score block: the codes of 16 keys, their scales' exponents
+  __device__ __forceinline__ f32x4 score(const u32x4 (&k)[HD / 64], int ke) const {
+    const i32x8 a = join(k[0], k[HD / 64 - 1]);
+    f32x4 s = mfma_f8(a, ke, op[0], exp[0], f32x4{0.f, 0.f, 0.f, 0.f});
+    if constexpr (HD == 128) s = mfma_f8(a, ke, op[1], exp[1], s);
+    return s;
+  }
+};
+template <int HD>
+struct WideQuery {
+  bf16x8 q[HD / 32];
+  __device__ __forceinline__ void load(const AttnF8Params& p, int64_t tok, int qhead, bool valid,
+                                       int g4) {
+    load_q<HD>(p, tok, qhead, valid, g4, q);
+  }
+};
+
 // Prefill tiles share every 64-key chunk through LDS.  Wave w copies page w of the
 // chunk there with the DMA path (global_load_lds, 16 bytes per lane): its keys, its
 // values and, by an ordinary store, its two scales.  Keys keep the page's layout but
@@ -370,7 +465,7 @@ template <int HD, bool TRACK>
 __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnItem& it,
                                              const ReqDev& rq, char* smem) {
   using SC = SharedChunk8<HD>;
-  constexpr int CB = SC::BYTES, NLD = SC::NLD, NH = HD / 64, ND = HD / 32;
+  constexpr int CB = SC::BYTES, NLD = SC::NLD, NH = HD / 64;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15;  // query row of this lane within each block
@@ -388,9 +483,9 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   const int page_end = row0 < rq.n_new ? (rq.ctx_len + last_row) / 16 + 1 : 0;
   const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
 
-  bf16x8 qf[ND], qf2[ND];
-  load_q<HD>(p, qtok, qhead, row_valid, g4, qf);
-  load_q<HD>(p, qtok2, qhead, row_valid2, g4, qf2);
+  std::conditional_t<TRACK, WideQuery<HD>, CodedQuery<HD>> qf, qf2;
+  qf.load(p, qtok, qhead, row_valid, g4);
+  qf2.load(p, qtok2, qhead, row_valid2, g4);
   RowState r1 = row_start(), r2 = row_start();
   f32x4 o[HD / 16], o2[HD / 16];
 #pragma unroll
@@ -451,15 +546,16 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   // (slot: the chunk's ring slot as a constant, which then is part of the read
   // instructions, or -1)
   // raw scores of chunk c from its keys in LDS, their max, and whether some lane of
-  // the wave is above its row's threshold
+  // the wave is above its row's threshold; beside(b) goes with the products of block b
   f32x4 s1[4], s2[4];
   float mx1 = kNegBig, mx2 = kNegBig;
-  auto scores = [&](auto mask, auto slot, int c) -> bool {
+  auto scores = [&](auto mask, auto slot, int c, auto beside) -> bool {
     constexpr bool MASK = decltype(mask)::value;
     constexpr int S = decltype(slot)::value, OFF = S >= 0 ? S * CB : 0, SOFF = S >= 0 ? S * 32 : 0;
     const unsigned ka = S >= 0 ? kaddr : kaddr + (unsigned)((c & 3) * CB);
     uint32_t ks = lds_read4_at<SOFF>(S >= 0 ? ks_addr : ks_addr + (unsigned)((c & 3) * 32));
     u32x4 k[4][NH];
+    f32x4 n1[4], n2[4];
     auto read = [&](auto b) {
       constexpr int B = decltype(b)::value;
       k[B][0] = lds_read16_at<OFF + B * 256>(ka);
@@ -470,18 +566,22 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
       lgkm_wait<(3 - B) * NH>();
       if constexpr (B == 0) pin1(ks);
       pin(k[B]);
-      const float kf = __uint_as_float(ks);
-      f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f}, a2 = a;
+      if constexpr (TRACK) {
+        n1[B] = n2[B] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int h = 0; h < NH; h++)
+        for (int h = 0; h < NH; h++)
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-          const bf16x8 w = widen(k[B][h][2 * i], k[B][h][2 * i + 1], kf);
-          a = mfma16(w, qf[2 * h + i], a);
-          a2 = mfma16(w, qf2[2 * h + i], a2);
-        }
-      s1[B] = a;
-      s2[B] = a2;
+          for (int i = 0; i < 2; i++) {
+            const bf16x8 w = widen(k[B][h][2 * i], k[B][h][2 * i + 1], __uint_as_float(ks));
+            n1[B] = mfma16(w, qf.q[2 * h + i], n1[B]);
+            n2[B] = mfma16(w, qf2.q[2 * h + i], n2[B]);
+          }
+      } else {
+        const int ke = (int)(ks >> 23);
+        n1[B] = qf.score(k[B], ke);
+        n2[B] = qf2.score(k[B], ke);
+      }
+      beside(b);
       __builtin_amdgcn_sched_barrier(0);  // these products go before the next wait
     };
     using std::integral_constant;
@@ -493,6 +593,11 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
     block(integral_constant<int, 1>{});
     block(integral_constant<int, 2>{});
     block(integral_constant<int, 3>{});
+#pragma unroll
+    for (int b = 0; b < 4; b++) {
+      s1[b] = n1[b];
+      s2[b] = n2[b];
+    }
     if constexpr (MASK) {
       mask_scores(s1, 4 * c + g4, page_end, row_pos);
       mask_scores(s2, 4 * c + g4, page_end, row_pos2);
@@ -501,6 +606,7 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
     mx2 = scores_max(s2);
     return __any(mx1 > r1.thr || mx2 > r2.thr) != 0;
   };
+  auto nothing = [](auto) {};
   // value products of chunk c (values past the request's keys zeroed when MASK: only
   // the chunk that holds the request's last key has such values)
   auto values = [&](auto mask, auto slot, int c, const bf16x8 (&pb1)[2], const bf16x8 (&pb2)[2]) {
@@ -564,14 +670,18 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   }
   // top of iteration kt: this wave's copies of chunk kt + 1 have landed and its scale
   // stores are done, then everyone's, and every read of chunk kt - 1 is done; chunk
-  // kt + 3 goes out, the scales of chunk kt + 2 go to LDS
+  // kt + 3 goes out, the scales of chunk kt + 2 go to LDS.  Scalar loads return in any
+  // order, so a use of the last iteration's behind the issue of this one's would wait
+  // for those too: the empty statement takes the old ones first.
   auto top = [&](int kt, int& use, int& fill) {
     vm_wait<NLD>();
     lgkm_wait<0>();
-    wg_barrier();
-    put_scales(kt + 2, sc);
+    asm volatile("" : "+s"(use), "+s"(sc.k), "+s"(sc.v));
+    const Scales old = sc;
     fill = page_of(kt + 4);
     sc = scales_of(use);
+    wg_barrier();
+    put_scales(kt + 2, old);
     copy(kt + 3, use);
   };
   auto run = [&](int kt0, int kt1, auto body) {  // iterations kt0 .. kt1 - 1
@@ -599,7 +709,7 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
     vm_wait<0>();  // no copy may land in LDS after the workgroup has ended
     return;
   }
-  if (scores(Masked{}, std::integral_constant<int, 0>{}, 0)) raise_rows();  // the first step raises every row's max
+  if (scores(Masked{}, std::integral_constant<int, 0>{}, 0, nothing)) raise_rows();  // the first step raises every row's max
 
   // Chunks 0 .. n_int - 1 are inside every wave's range and at or before every row of
   // the tile: no masks.  The last chunk of the tile is the only one that can hold keys
@@ -611,9 +721,11 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   auto step = [&](auto slot, int kt) {  // slot: kt % 4 or -1
     constexpr int S = decltype(slot)::value, S1 = S < 0 ? -1 : (S + 1) % 4;
     bf16x8 pb1[2], pb2[2];
-    probs<TRACK>(s1, r1, scale, pb1);
-    probs<TRACK>(s2, r2, scale, pb2);
-    const bool raise = scores(Unmasked{}, std::integral_constant<int, S1>{}, kt + 1);
+    const bool raise = scores(Unmasked{}, std::integral_constant<int, S1>{}, kt + 1, [&](auto b) {
+      constexpr int B = decltype(b)::value, H = B & 1;
+      if constexpr (B < 2) pb1[H] = half_probs<TRACK>(s1[2 * H], s1[2 * H + 1], r1, scale);
+      else pb2[H] = half_probs<TRACK>(s2[2 * H], s2[2 * H + 1], r2, scale);
+    });
     values(Unmasked{}, slot, kt, pb1, pb2);
     if (raise) raise_rows();
   };
@@ -640,7 +752,7 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
       probs<TRACK>(s2, r2, scale, pb2);
       values(Masked{}, AnySlot{}, kt, pb1, pb2);
     }
-    if (more && scores(Masked{}, AnySlot{}, kt + 1)) raise_rows();
+    if (more && scores(Masked{}, AnySlot{}, kt + 1, nothing)) raise_rows();
   });
   vm_wait<0>();  // no copy may land in LDS after the workgroup has ended
 
