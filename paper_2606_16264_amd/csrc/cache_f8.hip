@@ -38,16 +38,28 @@ __device__ __forceinline__ uint32_t encode2(float a, float b, float inv) {
   const uint32_t c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false) & 0xFFFFu;
   return (finite(a) ? c & 0xFFu : 0x7Fu) | (finite(b) ? c & 0xFF00u : 0x7F00u);
 }
-// Four codes times a power of two at most 1, as codes; NaN codes stay as they are (the
-// conversions would change their bits).
-__device__ __forceinline__ uint32_t shift_codes(uint32_t c, float ratio) {
+// Four codes times powers of two at most 1, as codes; NaN codes stay as they are (the
+// conversions would change their bits).  down: eight times the exponents' decrease, a
+// byte per code (at most 120 each, which any larger one is given as).  Where every code
+// stays normal its exponent field is lowered in place; else the codes go through fp32,
+// times ratio[i] = 2^-decrease, and round to nearest even.
+__device__ __forceinline__ uint32_t shift_codes(uint32_t c, uint32_t down, const float (&ratio)[4]) {
+  const uint32_t mag = c & 0x7F7F7F7Fu;
+  // a byte's top bit: magnitude at least 8 * (decrease + 1); NaN, 0x7F plus one
+  const uint32_t normal = (mag + (0x80808080u - 0x08080808u - down)) & 0x80808080u;
+  const uint32_t nan = (mag + 0x01010101u) & 0x80808080u;
+  if (normal == 0x80808080u && nan == 0) return c - down;
   const mx_f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(c, false);
   const mx_f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(lo[0] * ratio, lo[1] * ratio, 0, false);
-  r = __builtin_amdgcn_cvt_pk_fp8_f32(hi[0] * ratio, hi[1] * ratio, r, true);
-  // (a byte's low seven bits plus one reach its top bit for NaN alone)
-  const uint32_t nan = ((((c & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u) * 0xFFu;
-  return ((uint32_t)r & ~nan) | (c & nan);
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(lo[0] * ratio[0], lo[1] * ratio[1], 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(hi[0] * ratio[2], hi[1] * ratio[3], r, true);
+  const uint32_t keep = (nan >> 7) * 0xFFu;
+  return ((uint32_t)r & ~keep) | (c & keep);
+}
+// How far the exponent of a power of two lies below another's, capped as shift_codes
+// takes it.
+__device__ __forceinline__ int exponent_drop(float from, float to) {
+  return min(max((int)(__float_as_uint(to) >> 23) - (int)(__float_as_uint(from) >> 23), 0), 15);
 }
 
 __device__ __forceinline__ float wave_max(float x) {
@@ -62,11 +74,18 @@ __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w &
 // that stay, which move to the new one (ratio = old / new, 1 where it did not change).
 struct PageScale {
   float now, ratio;
+  uint32_t down;  // ratio as shift_codes takes it, all four bytes alike
+
+  __device__ __forceinline__ uint32_t shift(uint32_t c) const {
+    const float r[4] = {ratio, ratio, ratio, ratio};
+    return shift_codes(c, down, r);
+  }
 };
 __device__ __forceinline__ PageScale page_scale(float amax, const float* scale, int s0) {
   const float need = fit_scale(amax);
   const float old = s0 > 0 ? *scale : 0.f;
-  return old >= need ? PageScale{old, 1.f} : PageScale{need, old * inverse(need)};
+  if (old >= need) return PageScale{old, 1.f, 0};
+  return PageScale{need, old * inverse(need), exponent_drop(old, need) * 0x08080808u};
 }
 
 // ---------------------------------------------------------------- append
@@ -106,8 +125,8 @@ __device__ __forceinline__ void append_keys(const uint16_t* __restrict__ src, in
     }
     if (ps.ratio != 1.f && t < s0) {
       u32x2 w = *reinterpret_cast<u32x2*>(d + t * 64);
-      w[0] = shift_codes(w[0], ps.ratio);
-      w[1] = shift_codes(w[1], ps.ratio);
+      w[0] = ps.shift(w[0]);
+      w[1] = ps.shift(w[1]);
       *reinterpret_cast<u32x2*>(d + t * 64) = w;
     }
   }
@@ -154,7 +173,7 @@ __device__ __forceinline__ void append_values(const uint16_t* __restrict__ src, 
         const unsigned __int128 before = s0 > 0 ? all >> (8 * (16 - s0)) : 0;
         u32x4 sh;
 #pragma unroll
-        for (int q = 0; q < 4; q++) sh[q] = shift_codes(old[q], ps.ratio);
+        for (int q = 0; q < 4; q++) sh[q] = ps.shift(old[q]);
         old = __builtin_bit_cast(u32x4, (__builtin_bit_cast(unsigned __int128, sh) & before) |
                                             (__builtin_bit_cast(unsigned __int128, old) & ~before));
       }
@@ -192,94 +211,138 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-constexpr int kSelectThreads = 1024;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 
-// One workgroup per (request, KV head): the threshold of the (keep - recent) largest
-// weights among the first len - recent tokens by radix selection, 8 bits a pass from
-// the top, then the kept tokens' indices in order.  Of the tokens at the threshold
-// the first ones are kept.
+// One workgroup per (request, KV head).  Among the first n = len - recent tokens the
+// want = keep - recent with the largest keys stay, of equal ones the first.
+//
+// The want-th largest key is found two bits at a time from the top, by counting the
+// keys at or above three candidates: K compares and ballots each, whatever the weights'
+// distribution is (a histogram of eight bits took longer, since most weights share
+// their exponent and the LDS adds to one counter in turn: 76 us for 16 requests of up
+// to 16384 tokens, 8 heads, against 34).  The counting ends early when a candidate
+// has exactly want keys at or above it.  Each wave holds 64 K consecutive tokens, K a
+// lane in registers (K = 0: any number, read again for every candidate), so the kept
+// indices need one scan over the waves.  Bound by latency: loads, then up to 16 rounds
+// of count, LDS add and barrier.
+template <int K>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
     const EvictReq* reqs, const int32_t* pages, const float* __restrict__ weight, int nkv,
     int32_t* __restrict__ kept) {
-  __shared__ uint32_t s_hist[256];
-  __shared__ uint32_t s_pick[2];  // digit, rank left within it
-  __shared__ uint32_t s_cnt[2][kSelectThreads / 64];
+  __shared__ uint32_t s_count[16][4];
+  __shared__ uint32_t s_total[2][kSelectWaves];
   const EvictReq rq = reqs[blockIdx.x];
-  const int g = blockIdx.y, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int g = blockIdx.y, t = threadIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int32_t* ptab = pages + rq.src;
-  auto key = [&](int j) {
-    return weight_key(weight[((int64_t)ptab[j >> 4] * nkv + g) * 16 + (j & 15)]);
-  };
   const int n = rq.len - rq.recent;
   const uint32_t want = rq.keep - rq.recent;
-  uint32_t thr = 0, left = want;  // left: how many of the tokens at the threshold stay
-  if (want > 0 && want < (uint32_t)n) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = t; i < 256; i += kSelectThreads) s_hist[i] = 0;
-      __syncthreads();
-      for (int j = t; j < n; j += kSelectThreads) {
-        const uint32_t k = key(j);
-        if (shift == 24 || (k >> (shift + 8)) == (thr >> (shift + 8)))
-          atomicAdd(&s_hist[(k >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (t == 0) {
-        uint32_t above = 0;
-        int dig = 255;
-        while (above + s_hist[dig] < left) above += s_hist[dig--];
-        s_pick[0] = dig;
-        s_pick[1] = left - above;
-      }
-      __syncthreads();
-      thr |= s_pick[0] << shift;
-      left = s_pick[1];
-    }
+  const int per = K > 0 ? K : (n + kSelectThreads - 1) / kSelectThreads;  // 64-token groups per wave
+  const int first = wave * per * 64 + lane;
+  auto load = [&](int i) -> uint32_t {
+    const int j = first + 64 * i;
+    // (past the end: 0, below every candidate)
+    return j < n ? weight_key(weight[((int64_t)ptab[j >> 4] * nkv + g) * 16 + (j & 15)]) : 0u;
+  };
+  uint32_t held[K > 0 ? K : 1];
+  if constexpr (K > 0) {
+#pragma unroll
+    for (int i = 0; i < K; i++) held[i] = load(i);
   }
+  auto each = [&](auto f) {  // f(64-token group, its keys)
+    if constexpr (K > 0) {
+#pragma unroll
+      for (int i = 0; i < K; i++) f(i, held[i]);
+    } else {
+      for (int i = 0; i < per; i++) f(i, load(i));
+    }
+  };
   int32_t* out = kept + rq.kept + (int64_t)g * rq.keep;
-  uint32_t done = 0, ties = 0;
-  const uint64_t below = (1ull << lane) - 1;
-  if (want > 0) {
-    for (int j0 = 0; j0 < n; j0 += kSelectThreads) {
-      const int j = j0 + t;
-      const uint32_t k = j < n ? key(j) : 0u;
-      // (want == n: thr is 0 and left is n, so that every token stays)
-      const bool gt = j < n && want < (uint32_t)n && k > thr;
-      const bool eq = j < n && (want == (uint32_t)n || k == thr);
-      const uint64_t bg = __ballot(gt), be = __ballot(eq);
-      if (lane == 0) {
-        s_cnt[0][wave] = __popcll(bg);
-        s_cnt[1][wave] = __popcll(be);
-      }
+  for (int i = t; i < rq.recent; i += kSelectThreads) out[want + i] = n + i;
+  if (want == 0) return;
+
+  // keys above thr stay, and the first `left` of those equal to it
+  uint32_t thr = 0;
+  const bool all = want >= (uint32_t)n;
+  if (!all) {
+    if (t < 64) s_count[t >> 2][t & 3] = 0;
+    __syncthreads();
+    for (int round = 0; round < 16; round++) {
+      const int shift = 30 - 2 * round;
+      const uint32_t c1 = thr | 1u << shift, c2 = thr | 2u << shift, c3 = thr | 3u << shift;
+      uint32_t n1 = 0, n2 = 0, n3 = 0;
+      each([&](int, uint32_t k) {
+        n1 += __popcll(__ballot(k >= c1));
+        n2 += __popcll(__ballot(k >= c2));
+        n3 += __popcll(__ballot(k >= c3));
+      });
+      if (lane < 3) atomicAdd(&s_count[round][lane], lane == 0 ? n1 : lane == 1 ? n2 : n3);
       __syncthreads();
-      uint32_t g0 = 0, e0 = 0, gall = 0, eall = 0;
-      for (int w = 0; w < kSelectThreads / 64; w++) {
-        if (w < wave) g0 += s_cnt[0][w], e0 += s_cnt[1][w];
-        gall += s_cnt[0][w];
-        eall += s_cnt[1][w];
+      n1 = s_count[round][0];
+      n2 = s_count[round][1];
+      n3 = s_count[round][2];
+      uint32_t at = 0;  // keys at or above the new thr, where a candidate was taken
+      if (n3 >= want) thr = c3, at = n3;
+      else if (n2 >= want) thr = c2, at = n2;
+      else if (n1 >= want) thr = c1, at = n1;
+      if (at == want) {
+        thr--;
+        break;
       }
-      g0 += __popcll(bg & below);
-      e0 += ties + __popcll(be & below);
-      // kept ties ahead of this token: those of the first `left` ties with a lower index
-      const uint32_t at = done + g0 + (min(e0, left) - min(ties, left));
-      if (gt || (eq && e0 < left)) out[at] = j;
-      done += gall + (min(ties + eall, left) - min(ties, left));
-      ties += eall;
-      __syncthreads();
     }
   }
-  for (int i = t; i < rq.recent; i += kSelectThreads) out[want + i] = n + i;
+  uint32_t above = 0, equal = 0;
+  each([&](int i, uint32_t k) {
+    const bool in = first + 64 * i < n;
+    above += __popcll(__ballot(in && (all || k > thr)));
+    equal += __popcll(__ballot(in && !all && k == thr));
+  });
+  if (lane == 0) {
+    s_total[0][wave] = above;
+    s_total[1][wave] = equal;
+  }
+  __syncthreads();
+  uint32_t done = 0, ties = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kSelectWaves; w++) {
+    total += s_total[0][w];
+    if (w < wave) {
+      done += s_total[0][w];
+      ties += s_total[1][w];
+    }
+  }
+  const uint32_t left = want - total;
+  done += min(ties, left);
+  const uint64_t below = (1ull << lane) - 1;
+  each([&](int i, uint32_t k) {
+    const int j = first + 64 * i;
+    const bool gt = j < n && (all || k > thr), eq = j < n && !all && k == thr;
+    const uint64_t bg = __ballot(gt), be = __ballot(eq);
+    const uint32_t tie = ties + __popcll(be & below);
+    if (gt || (eq && tie < left))
+      out[done + __popcll(bg & below) + min(tie, left) - min(ties, left)] = j;
+    const uint32_t next = ties + __popcll(be);
+    done += __popcll(bg) + min(next, left) - min(ties, left);
+    ties = next;
+  });
 }
 
 // Copies the kept tokens of one destination page and KV head, a wave each.  The page's
-// scale is the largest of those its tokens come from.
+// scale is the largest of those its tokens come from.  Bound by memory (keys 64-byte
+// runs; of a value page that holds one kept token all lines are read, since a token's
+// values lie 16 bytes apart).  Values: the tokens of a destination page come from source
+// pages in ascending order; of each such page a lane reads its rows as 16-byte words
+// and takes the bytes it needs with byte permutes whose selectors are the same in all
+// lanes (as loads of single bytes: 177 us for 8192 tokens of 16 requests, 8 heads).
 template <int HD>
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictReq* reqs,
                                                          const int32_t* pages,
                                                          const EvictPage* items, CacheF8 c, int nkv,
                                                          const int32_t* __restrict__ kept) {
+  constexpr int NR = HD / 64;  // value rows per lane: lane, lane + 64
   const EvictPage it = items[blockIdx.x];
   const EvictReq rq = reqs[it.req];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = blockIdx.y * 4 + wave;
   if (g >= nkv) return;
   const int n = min(16, rq.keep - it.start);  // tokens of this page
@@ -287,54 +350,115 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictReq* reqs,
   // token i of the page lives at lanes i, i + 16 ..: its source page and slot, and scales
   const int ti = min(lane & 15, n - 1);
   const int j = kept[rq.kept + (int64_t)g * rq.keep + it.start + ti];
-  const int64_t src = (int64_t)pages[rq.src + (j >> 4)] * nkv + g;
-  const int slot = j & 15;
-  float ks = c.k_scale[src], vs = c.v_scale[src];
+  const int page = pages[rq.src + (j >> 4)], slot = j & 15;
+  const int64_t src = (int64_t)page * nkv + g;
+  const float ks = c.k_scale[src], vs = c.v_scale[src];
   float kn = ks, vn = vs;
 #pragma unroll
   for (int m = 1; m < 16; m <<= 1) {
     kn = fmaxf(kn, __shfl_xor(kn, m));
     vn = fmaxf(vn, __shfl_xor(vn, m));
   }
-  const float kr = ks * inverse(kn), vr = vs * inverse(vn);
   if (lane == 0) {
     c.k_scale[dst] = kn;
     c.v_scale[dst] = vn;
   }
   if (lane < n) c.weight[dst * 16 + lane] = c.weight[src * 16 + slot];
-  // keys: 16 bytes per lane in the destination's order
+
+  // the first source page's values, on their way while the keys are copied
+  const int before = __shfl_up(page, 1);
+  uint32_t starts = (uint32_t)__ballot(lane < n && (lane == 0 || page != before));
+  auto rows = [&](int i, u32x4 (&r)[NR]) {  // value rows of token i's page
+    const int64_t at = (int64_t)__builtin_amdgcn_readlane(page, i) * nkv + g;
 #pragma unroll
-  for (int q = 0; q < HD / 64; q++) {
-    const int i = lane >> 2, from = min(i, n - 1);
-    const int64_t sp = __shfl(src, from);
-    const int ss = __shfl(slot, from);
-    const float ratio = __shfl(kr, from);
-    if (i < n) {
-      u32x4 w = *reinterpret_cast<const u32x4*>(c.k + sp * (16 * HD) + q * 1024 + ss * 64 + (lane & 3) * 16);
-      if (ratio != 1.f)
+    for (int q = 0; q < NR; q++)
+      r[q] = *reinterpret_cast<const u32x4*>(c.v + at * (16 * HD) + q * 1024 + lane * 16);
+  };
+  u32x4 r[NR], next[NR];
+  rows(0, r);
+
+  // keys: 16 bytes per lane in the destination's order, token lane / 4
+  {
+    const int i = min(lane >> 2, n - 1);
+    const int64_t sp = (int64_t)__shfl(page, i) * nkv + g;
+    const int ss = __shfl(slot, i);
+    const float from = __shfl(ks, i), ratio = from * inverse(kn);
+    const uint32_t down = exponent_drop(from, kn) * 0x08080808u;
+    const float all[4] = {ratio, ratio, ratio, ratio};
+    const uint8_t* s = c.k + sp * (16 * HD) + ss * 64 + (lane & 3) * 16;
+    uint8_t* d = c.k + dst * (16 * HD) + lane * 16;
+    u32x4 w[NR];
 #pragma unroll
-        for (int e = 0; e < 4; e++) w[e] = shift_codes(w[e], ratio);
-      *reinterpret_cast<u32x4*>(c.k + dst * (16 * HD) + q * 1024 + i * 64 + (lane & 3) * 16) = w;
+    for (int q = 0; q < NR; q++) w[q] = *reinterpret_cast<const u32x4*>(s + q * 1024);
+    if (down) {
+#pragma unroll
+      for (int q = 0; q < NR; q++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) w[q][e] = shift_codes(w[q][e], down, all);
+    }
+    if ((lane >> 2) < n) {
+#pragma unroll
+      for (int q = 0; q < NR; q++) *reinterpret_cast<u32x4*>(d + q * 1024) = w[q];
     }
   }
-  // values: a lane's rows of the transposed page, gathered byte by byte
+
+  // values: the words of the destination rows, bytes of one source page at a time
+  u32x4 w[NR];
 #pragma unroll
-  for (int q = 0; q < HD / 64; q++) {
-    const int e = q * 64 + lane;
-    u32x4* d = reinterpret_cast<u32x4*>(c.v + dst * (16 * HD) + e * 16);
-    u32x4 w = n < 16 ? *d : u32x4{0, 0, 0, 0};
+  for (int q = 0; q < NR; q++) w[q] = u32x4{0, 0, 0, 0};
+  auto quad = [&](uint32_t byte) {  // lanes 4 q .. 4 q + 3's bytes as one word
+    uint32_t x = byte << (8 * (lane & 3));
+    x |= __builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true);   // lanes 1 0 3 2
+    x |= __builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true);   // lanes 2 3 0 1
+    return x;
+  };
+  while (starts) {
+    const int i0 = __builtin_ctz(starts);
+    starts &= starts - 1;
+    const int i1 = starts ? __builtin_ctz(starts) : n;
+    if (starts) rows(i1, next);
+    // selector 12 is a zero byte
+    const bool mine = lane >= i0 && lane < i1;
+    const uint32_t lo = quad(mine && slot < 8 ? slot : 12), hi = quad(mine && slot >= 8 ? slot - 8 : 12);
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-      const int64_t sp = __shfl(src, i);
-      const int ss = __shfl(slot, i);
-      const float ratio = __shfl(vr, i);
-      if (i < n) {
-        uint32_t b = c.v[sp * (16 * HD) + e * 16 + ss];
-        if (ratio != 1.f) b = shift_codes(b, ratio) & 0xFFu;
-        w[i >> 2] = (w[i >> 2] & ~(0xFFu << (8 * (i & 3)))) | b << (8 * (i & 3));
+    for (int d = 0; d < 4; d++) {
+      const uint32_t sl = __builtin_amdgcn_readlane(lo, 4 * d), sh = __builtin_amdgcn_readlane(hi, 4 * d);
+#pragma unroll
+      for (int q = 0; q < NR; q++)
+        w[q][d] |= __builtin_amdgcn_perm(r[q][1], r[q][0], sl) | __builtin_amdgcn_perm(r[q][3], r[q][2], sh);
+    }
+#pragma unroll
+    for (int q = 0; q < NR; q++) r[q] = next[q];
+  }
+  const float ratio = vs * inverse(vn);
+  const int drop = 8 * exponent_drop(vs, vn);
+  if (__any(drop)) {
+    const uint32_t down = quad(drop);
+#pragma unroll
+    for (int d = 0; d < 4; d++) {
+      const uint32_t dd = __builtin_amdgcn_readlane(down, 4 * d);
+      float by[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        by[e] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ratio), 4 * d + e));
+      if (dd)
+#pragma unroll
+        for (int q = 0; q < NR; q++) w[q][d] = shift_codes(w[q][d], dd, by);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < NR; q++) {
+    u32x4* d = reinterpret_cast<u32x4*>(c.v + dst * (16 * HD) + q * 1024 + lane * 16);
+    if (n < 16) {  // the bytes behind the page's tokens stay
+      const u32x4 old = *d;
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const int b = min(max(n - 4 * e, 0), 4);
+        const uint32_t mask = b == 4 ? ~0u : (1u << (8 * b)) - 1;
+        w[q][e] = (w[q][e] & mask) | (old[e] & ~mask);
       }
     }
-    *d = w;
+    *d = w[q];
   }
 }
 
@@ -352,12 +476,19 @@ hipError_t launch_kv_append_f8(const uint16_t* k_new, const uint16_t* v_new, con
   return hipGetLastError();
 }
 
-hipError_t launch_kv_evict_f8(const EvictReq* reqs, int n_reqs, const int32_t* pages,
+hipError_t launch_kv_evict_f8(const EvictReq* reqs, int n_reqs, int longest, const int32_t* pages,
                               const EvictPage* items, int64_t n_items, const CacheF8& cache,
                               int32_t* kept, int nkv, int d, hipStream_t stream) {
   if (n_items == 0) return hipSuccess;
-  evict_select_kernel<<<dim3(n_reqs, nkv), kSelectThreads, 0, stream>>>(reqs, pages, cache.weight,
-                                                                       nkv, kept);
+  const dim3 heads(n_reqs, nkv);
+  auto select = [&](auto kernel) {
+    kernel<<<heads, kSelectThreads, 0, stream>>>(reqs, pages, cache.weight, nkv, kept);
+  };
+  // keys a thread holds: as few as the longest request needs
+  if (longest <= 4 * kSelectThreads) select(evict_select_kernel<4>);
+  else if (longest <= 16 * kSelectThreads) select(evict_select_kernel<16>);
+  else if (longest <= 32 * kSelectThreads) select(evict_select_kernel<32>);
+  else select(evict_select_kernel<0>);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)n_items, (nkv + 3) / 4);

@@ -1211,18 +1211,46 @@ mx_status check_not_capturing(hipStream_t stream) {
   return MX_OK;
 }
 
+// Marks on page ids, a bit each.  The bits are kept per thread and cleared by their
+// marks, so a call costs what it marks and not the pool's size.
+class PageMarks {
+ public:
+  ~PageMarks() {
+    for (const int32_t pg : marked_) bits()[pg >> 6] = 0;
+  }
+  // false: marked already
+  bool mark(int32_t pg) {
+    std::vector<uint64_t>& b = bits();
+    if ((size_t)(pg >> 6) >= b.size()) b.resize(std::max<size_t>(2 * b.size(), (pg >> 6) + 1));
+    const uint64_t bit = 1ull << (pg & 63);
+    if (b[pg >> 6] & bit) return false;
+    marked_.push_back(pg);
+    b[pg >> 6] |= bit;
+    return true;
+  }
+  bool has(int32_t pg) const {
+    const std::vector<uint64_t>& b = bits();
+    return (size_t)(pg >> 6) < b.size() && (b[pg >> 6] >> (pg & 63) & 1);
+  }
+
+ private:
+  static std::vector<uint64_t>& bits() {
+    thread_local std::vector<uint64_t> b;
+    return b;
+  }
+  std::vector<int32_t> marked_;
+};
+
 // The first page that two runs of the batch's new tokens touch, -1 if none: a page's
 // scale is written once per call.
 int64_t page_touched_twice(const mx_batch* b) {
-  std::vector<int32_t> touched;
+  PageMarks marks;
   for (int r = 0; r < b->num_reqs; r++) {
     const mx_request& q = b->reqs[r];
     for (int64_t pg = q.ctx_len / 16; pg <= ((int64_t)q.ctx_len + q.n_new - 1) / 16; pg++)
-      touched.push_back(q.pages[pg]);
+      if (!marks.mark(q.pages[pg])) return q.pages[pg];
   }
-  std::sort(touched.begin(), touched.end());
-  const auto it = std::adjacent_find(touched.begin(), touched.end());
-  return it == touched.end() ? -1 : *it;
+  return -1;
 }
 
 // Workspace of mx_paged_attn_f8: the metadata as for mx_paged_attn, then, where
@@ -1410,6 +1438,7 @@ namespace {
 
 struct EvictPlan {
   int64_t src_pages = 0, dst_pages = 0;
+  int32_t longest = 0;                     // largest len - recent
   size_t pages = 0, items = 0, total = 0;  // offsets after the requests
 };
 
@@ -1419,13 +1448,13 @@ mx_status validate_evict(int32_t R, const mx_evict_request* reqs, const mx_attn_
   if (st != MX_OK) return st;
   if (R < 0) return fail(MX_ERR_INVALID, "num_reqs %d < 0", R);
   if (R > 0 && !reqs) return fail(MX_ERR_NULL, "reqs is NULL");
-  std::vector<int32_t> dst;
+  PageMarks dst;
   for (int r = 0; r < R; r++) {
     const mx_evict_request& q = reqs[r];
     if (q.len < 0 || q.keep < 0 || q.keep > q.len || q.recent < 0 || q.recent > q.keep)
       return fail(MX_ERR_INVALID, "request %d: need 0 <= recent %d <= keep %d <= len %d", r,
                   q.recent, q.keep, q.len);
-    if (q.len > INT32_MAX - 16) return fail(MX_ERR_TOO_LARGE, "request %d: context too long", r);
+    if (q.len > INT32_MAX - 4096) return fail(MX_ERR_TOO_LARGE, "request %d: context too long", r);
     const int64_t ns = ceil_div(q.len, 16), nd = ceil_div(q.keep, 16);
     if (q.n_pages < ns || q.n_dst_pages < nd)
       return fail(MX_ERR_NO_SPACE, "request %d: %d pages and %d destination pages (need %lld, %lld)",
@@ -1438,21 +1467,19 @@ mx_status validate_evict(int32_t R, const mx_evict_request* reqs, const mx_attn_
         return fail(MX_ERR_INVALID, "request %d: page id %d outside [0, %lld)", r, pg,
                     (long long)s->pool_pages);
     }
-    dst.insert(dst.end(), q.dst_pages, q.dst_pages + nd);
+    // destination pages are nobody else's: neither another destination nor a source
+    for (int64_t i = 0; i < nd; i++)
+      if (!dst.mark(q.dst_pages[i]))
+        return fail(MX_ERR_INVALID, "page %d is the destination of two", q.dst_pages[i]);
     p.src_pages += ns;
     p.dst_pages += nd;
+    p.longest = std::max(p.longest, q.len - q.recent);
     if (p.src_pages + p.dst_pages > INT32_MAX / 2) return fail(MX_ERR_TOO_LARGE, "too many pages");
   }
-  // destination pages are nobody else's: neither another destination nor a source
-  std::sort(dst.begin(), dst.end());
-  const auto twice = std::adjacent_find(dst.begin(), dst.end());
-  if (twice != dst.end())
-    return fail(MX_ERR_INVALID, "page %d is the destination of two", *twice);
-  if (!dst.empty())
-    for (int r = 0; r < R; r++)
-      for (int64_t i = 0, ns = ceil_div(reqs[r].len, 16); i < ns; i++)
-        if (std::binary_search(dst.begin(), dst.end(), reqs[r].pages[i]))
-          return fail(MX_ERR_INVALID, "page %d is a source and a destination", reqs[r].pages[i]);
+  for (int r = 0; r < R; r++)
+    for (int64_t i = 0, ns = ceil_div(reqs[r].len, 16); i < ns; i++)
+      if (dst.has(reqs[r].pages[i]))
+        return fail(MX_ERR_INVALID, "page %d is a source and a destination", reqs[r].pages[i]);
   size_t o = align_up(R * sizeof(EvictReq));
   p.pages = o; o = align_up(o + (p.src_pages + p.dst_pages) * sizeof(int32_t));
   p.items = o; o = align_up(o + p.dst_pages * sizeof(EvictPage));
@@ -1511,7 +1538,7 @@ MX_EXPORT mx_status mx_kv_evict_f8(int32_t num_reqs, const mx_evict_request* req
         [&](const void* dev) { return launch_upload(dev, ws, p.total, stream); });
     if (st != MX_OK) return st;
     const hipError_t e = timed("kv_evict_f8", stream, [&] {
-      return launch_kv_evict_f8(at<EvictReq>(ws, 0), num_reqs, at<int32_t>(ws, p.pages),
+      return launch_kv_evict_f8(at<EvictReq>(ws, 0), num_reqs, p.longest, at<int32_t>(ws, p.pages),
                                 at<EvictPage>(ws, p.items), p.dst_pages, cache_args(cache), kept,
                                 shape->n_kv_heads, shape->head_dim, stream);
     });

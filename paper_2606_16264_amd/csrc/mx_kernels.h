@@ -78,7 +78,8 @@ struct EvictReq {
 struct EvictPage {
   int32_t req, start;
 };
-hipError_t launch_kv_evict_f8(const EvictReq* reqs, int n_reqs, const int32_t* pages,
+// (longest: the largest len - recent of the requests)
+hipError_t launch_kv_evict_f8(const EvictReq* reqs, int n_reqs, int longest, const int32_t* pages,
                               const EvictPage* items, int64_t n_items, const CacheF8& cache,
                               int32_t* kept, int nkv, int d, hipStream_t stream);
 
