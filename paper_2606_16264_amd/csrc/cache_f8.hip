@@ -213,24 +213,39 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 
+// Sum of x over this lane and the ones above it in the wave.
+__device__ __forceinline__ uint32_t suffix_sum(uint32_t x, int lane) {
+  // within rows of 16 lanes: lane i adds lane i + 1, + 2, + 4, + 8 (0 past the row)
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x101, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x102, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x104, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x108, 0xF, 0xF, true);
+  const uint32_t r1 = __builtin_amdgcn_readlane(x, 16), r2 = __builtin_amdgcn_readlane(x, 32),
+                 r3 = __builtin_amdgcn_readlane(x, 48);
+  const int row = lane >> 4;
+  return x + (row == 0 ? r1 + r2 + r3 : row == 1 ? r2 + r3 : row == 2 ? r3 : 0u);
+}
+
 // One workgroup per (request, KV head).  Among the first n = len - recent tokens the
 // want = keep - recent with the largest keys stay, of equal ones the first.
 //
-// The want-th largest key is found two bits at a time from the top, by counting the
-// keys at or above three candidates: K compares and ballots each, whatever the weights'
-// distribution is (a histogram of eight bits took longer, since most weights share
-// their exponent and the LDS adds to one counter in turn: 76 us for 16 requests of up
-// to 16384 tokens, 8 heads, against 34).  The counting ends early when a candidate
-// has exactly want keys at or above it.  Each wave holds 64 K consecutive tokens, K a
-// lane in registers (K = 0: any number, read again for every candidate), so the kept
-// indices need one scan over the waves.  Bound by latency: loads, then up to 16 rounds
-// of count, LDS add and barrier.
+// The want-th largest key is found eight bits at a time from the top, by a histogram in
+// LDS of the keys that agree with it so far.  Most weights share their exponent and many
+// are zero, and adds of one wave to one counter go in turn, so a digit has four counters,
+// of which a lane takes the one of its own index (16 requests of up to 16384 tokens, 8
+// heads: 16 us; counting up to 16 times the keys at or above three candidates by
+// ballots, 38).  The search ends early when a digit's keys are just what is missing.
+// Each wave holds 64 K consecutive tokens, K a lane in registers (K = 0: any number,
+// read again in every pass), so the kept indices need one scan over the waves.  Bound
+// by latency: loads, then up to four times adds, a barrier, the scan of the counters by
+// one wave, a barrier.
 template <int K>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
     const EvictReq* reqs, const int32_t* pages, const float* __restrict__ weight, int nkv,
     int32_t* __restrict__ kept) {
-  __shared__ uint32_t s_count[16][4];
-  __shared__ uint32_t s_total[2][kSelectWaves];
+  __shared__ __attribute__((aligned(16))) uint32_t s_hist[4][256][4];
+  __shared__ uint32_t s_pick[4][3];  // digit, keys missing within it, keys of it
+  __shared__ __attribute__((aligned(16))) uint32_t s_total[kSelectWaves][2];
   const EvictReq rq = reqs[blockIdx.x];
   const int g = blockIdx.y, t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -240,10 +255,15 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
   const int per = K > 0 ? K : (n + kSelectThreads - 1) / kSelectThreads;  // 64-token groups per wave
   const int first = wave * per * 64 + lane;
   auto load = [&](int i) -> uint32_t {
-    const int j = first + 64 * i;
-    // (past the end: 0, below every candidate)
-    return j < n ? weight_key(weight[((int64_t)ptab[j >> 4] * nkv + g) * 16 + (j & 15)]) : 0u;
+    // (past the end: 0, below every candidate; the load itself is unconditional, so that
+    // a thread's loads are in flight together)
+    const int j = first + 64 * i, jc = min(j, n - 1);
+    const uint32_t k = weight_key(weight[((int64_t)ptab[jc >> 4] * nkv + g) * 16 + (jc & 15)]);
+    return j < n ? k : 0u;
   };
+  int32_t* out = kept + rq.kept + (int64_t)g * rq.keep;
+  for (int i = t; i < rq.recent; i += kSelectThreads) out[want + i] = n + i;
+  if (want == 0) return;
   uint32_t held[K > 0 ? K : 1];
   if constexpr (K > 0) {
 #pragma unroll
@@ -257,59 +277,73 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
       for (int i = 0; i < per; i++) f(i, load(i));
     }
   };
-  int32_t* out = kept + rq.kept + (int64_t)g * rq.keep;
-  for (int i = t; i < rq.recent; i += kSelectThreads) out[want + i] = n + i;
-  if (want == 0) return;
 
   // keys above thr stay, and the first `left` of those equal to it
   uint32_t thr = 0;
   const bool all = want >= (uint32_t)n;
   if (!all) {
-    if (t < 64) s_count[t >> 2][t & 3] = 0;
+    reinterpret_cast<u32x4*>(s_hist)[t] = u32x4{0, 0, 0, 0};
     __syncthreads();
-    for (int round = 0; round < 16; round++) {
-      const int shift = 30 - 2 * round;
-      const uint32_t c1 = thr | 1u << shift, c2 = thr | 2u << shift, c3 = thr | 3u << shift;
-      uint32_t n1 = 0, n2 = 0, n3 = 0;
-      each([&](int, uint32_t k) {
-        n1 += __popcll(__ballot(k >= c1));
-        n2 += __popcll(__ballot(k >= c2));
-        n3 += __popcll(__ballot(k >= c3));
+    uint32_t missing = want;  // keys to take among those that agree with thr so far
+#pragma unroll 1
+    for (int pass = 0; pass < 4; pass++) {
+      const int shift = 24 - 8 * pass;
+      // (pass 0: every key agrees with none of its bits)
+      const uint32_t fixed = pass == 0 ? 0u : ~0u << (shift + 8);
+      each([&](int i, uint32_t k) {
+        if (first + 64 * i < n && ((k ^ thr) & fixed) == 0)
+          atomicAdd(&s_hist[pass][k >> shift & 255][lane & 3], 1u);
       });
-      if (lane < 3) atomicAdd(&s_count[round][lane], lane == 0 ? n1 : lane == 1 ? n2 : n3);
       __syncthreads();
-      n1 = s_count[round][0];
-      n2 = s_count[round][1];
-      n3 = s_count[round][2];
-      uint32_t at = 0;  // keys at or above the new thr, where a candidate was taken
-      if (n3 >= want) thr = c3, at = n3;
-      else if (n2 >= want) thr = c2, at = n2;
-      else if (n1 >= want) thr = c1, at = n1;
-      if (at == want) {
-        thr--;
+      if (wave == 0) {
+        uint32_t h[4], mine = 0;  // digits 4 lane .. 4 lane + 3
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const u32x4 c = *reinterpret_cast<const u32x4*>(s_hist[pass][4 * lane + e]);
+          h[e] = (c[0] + c[1]) + (c[2] + c[3]);
+          mine += h[e];
+        }
+        uint32_t above = suffix_sum(mine, lane) - mine;  // keys of larger digits
+#pragma unroll
+        for (int e = 3; e >= 0; e--) {
+          if (above < missing && missing <= above + h[e]) {  // one digit of one lane
+            s_pick[pass][0] = 4 * lane + e;
+            s_pick[pass][1] = missing - above;
+            s_pick[pass][2] = h[e];
+          }
+          above += h[e];
+        }
+      }
+      __syncthreads();
+      thr |= (uint32_t)__builtin_amdgcn_readfirstlane(s_pick[pass][0]) << shift;
+      missing = __builtin_amdgcn_readfirstlane(s_pick[pass][1]);
+      if (missing == (uint32_t)__builtin_amdgcn_readfirstlane(s_pick[pass][2])) {
+        thr--;  // every key from here on stays; want < n, so some key is below thr, which is not 0
         break;
       }
     }
   }
   uint32_t above = 0, equal = 0;
-  each([&](int i, uint32_t k) {
+  each([&](int i, uint32_t k) {  // per lane; a ballot each took four times as long
     const bool in = first + 64 * i < n;
-    above += __popcll(__ballot(in && (all || k > thr)));
-    equal += __popcll(__ballot(in && !all && k == thr));
+    above += in && (all || k > thr);
+    equal += in && !all && k == thr;
   });
+  above = suffix_sum(above, lane);
+  equal = suffix_sum(equal, lane);
   if (lane == 0) {
-    s_total[0][wave] = above;
-    s_total[1][wave] = equal;
+    s_total[wave][0] = above;
+    s_total[wave][1] = equal;
   }
   __syncthreads();
   uint32_t done = 0, ties = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kSelectWaves; w++) {
-    total += s_total[0][w];
-    if (w < wave) {
-      done += s_total[0][w];
-      ties += s_total[1][w];
-    }
+    const uint32_t a = __builtin_amdgcn_readfirstlane(s_total[w][0]);
+    const uint32_t e = __builtin_amdgcn_readfirstlane(s_total[w][1]);
+    total += a;
+    done += w < wave ? a : 0;
+    ties += w < wave ? e : 0;
   }
   const uint32_t left = want - total;
   done += min(ties, left);
@@ -317,7 +351,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
   each([&](int i, uint32_t k) {
     const int j = first + 64 * i;
     const bool gt = j < n && (all || k > thr), eq = j < n && !all && k == thr;
-    const uint64_t bg = __ballot(gt), be = __ballot(eq);
+    const uint64_t bg = __ballot(gt), be = left ? __ballot(eq) : 0;
     const uint32_t tie = ties + __popcll(be & below);
     if (gt || (eq && tie < left))
       out[done + __popcll(bg & below) + min(tie, left) - min(ties, left)] = j;
@@ -328,12 +362,13 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
 }
 
 // Copies the kept tokens of one destination page and KV head, a wave each.  The page's
-// scale is the largest of those its tokens come from.  Bound by memory (keys 64-byte
-// runs; of a value page that holds one kept token all lines are read, since a token's
-// values lie 16 bytes apart).  Values: the tokens of a destination page come from source
+// scale is the largest of those its tokens come from.  Bound by memory: 108 us for 8192
+// tokens of 16 requests, 8 heads, 550 MB (200 written; keys are 64-byte runs, and of a
+// value page that holds one kept token all lines are read, since a token's values lie
+// 16 bytes apart).  Values: the tokens of a destination page come from source
 // pages in ascending order; of each such page a lane reads its rows as 16-byte words
 // and takes the bytes it needs with byte permutes whose selectors are the same in all
-// lanes (as loads of single bytes: 177 us for 8192 tokens of 16 requests, 8 heads).
+// lanes (as loads of single bytes: 177 us).
 template <int HD>
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictReq* reqs,
                                                          const int32_t* pages,
