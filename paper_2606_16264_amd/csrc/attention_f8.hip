@@ -161,7 +161,8 @@ struct DecodeScan {
   const int32_t* ptab;
   int kvh, page_end, row_pos, kv_len, col, g4;
   float scale, inv_scale;
-  float* scores;  // where to leave the lane's scores in log2 units, or null
+  float* scores;  // TRACK: where the lane leaves scores in log2 units (store_scores), or null
+  int rows;       // TRACK: 4, 8 or 16, at least the item's rows
   u32x4 k[4][HD / 64], v[HD / 16];
   float ks, vs;
 
@@ -191,18 +192,50 @@ struct DecodeScan {
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  // The scores of the item's rows, 64 bytes a row and page.  With up to 4 (8) rows the
+  // lanes of the other columns take blocks 1 .. 3 (the odd blocks) of those rows, so
+  // that one store (two) holds whole runs and not a quarter of each with a quarter of
+  // the lanes: 64 decodes of the 8B heads 108 -> SCORES_US us.
+  __device__ __forceinline__ void store_scores(const f32x4 (&s)[4], int pi, bool valid) {
+    auto moved = [&](float to, float from, auto ctrl, auto banks) {  // banks: columns / 4
+      return __uint_as_float(__builtin_amdgcn_update_dpp(
+          (int)__float_as_uint(to), (int)__float_as_uint(from), decltype(ctrl)::value, 0xF,
+          decltype(banks)::value, false));
+    };
+    using std::integral_constant;
+    f32x4* out = reinterpret_cast<f32x4*>(scores + pi * 16);
+    const bool store = scores && valid;
+    if (rows == 4) {
+      f32x4 x;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        x[i] = moved(s[0][i], s[1][i], integral_constant<int, 0x114>{}, integral_constant<int, 2>{});
+        x[i] = moved(x[i], s[2][i], integral_constant<int, 0x118>{}, integral_constant<int, 4>{});
+        x[i] = moved(x[i], s[3][i], integral_constant<int, 0x11C>{}, integral_constant<int, 8>{});
+      }
+      if (store) *out = x * scale;
+    } else if (rows == 8) {
+      f32x4 x, y;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        x[i] = moved(s[0][i], s[1][i], integral_constant<int, 0x118>{}, integral_constant<int, 12>{});
+        y[i] = moved(s[2][i], s[3][i], integral_constant<int, 0x118>{}, integral_constant<int, 12>{});
+      }
+      if (store) {
+        out[0] = x * scale;
+        out[2] = y * scale;
+      }
+    } else if (store) {
+#pragma unroll
+      for (int b = 0; b < 4; b++) out[b] = s[b] * scale;
+    }
+  }
   template <bool LAST>
   __device__ __forceinline__ void softmax(f32x4 (&s)[4], int pi, RowState& r, f32x4 (&o)[HD / 16],
                                           bf16x8 (&pb)[2]) {
     const int page = pi + g4;
     if constexpr (LAST) mask_scores(s, page, page_end, row_pos);
-    if constexpr (TRACK) {
-      if (scores && (!LAST || page < page_end)) {
-#pragma unroll
-        for (int b = 0; b < 4; b++)
-          *reinterpret_cast<f32x4*>(scores + page * 16 + 4 * b) = s[b] * scale;
-      }
-    }
+    if constexpr (TRACK) store_scores(s, pi, !LAST || page < page_end);
     const float mx = scores_max(s);
     if (__any(mx > r.thr)) raise_max(r, mx, scale, inv_scale, o);
     probs<TRACK>(s, r, scale, pb);
@@ -212,16 +245,26 @@ struct DecodeScan {
     if (pi >= page_end) return;
     f32x4 s[4];
     bf16x8 pb[2];
-    load_keys(key_page(pi));
-    load_values(value_page(pi));
+    // The order of the loads is that of their uses, page ids of the next step first, on
+    // every way into the loop: a wait counts what was issued behind the load it is for,
+    // and takes the least count of all ways.
+    const int k0 = key_page(pi), v0 = value_page(pi);
     int kn = key_page(pi + 16), vn = value_page(pi + 16);
+    __builtin_amdgcn_sched_barrier(0);
+    load_keys(k0);
+    __builtin_amdgcn_sched_barrier(0);
+    load_values(v0);
+    __builtin_amdgcn_sched_barrier(0);
     for (; pi + 16 < page_end; pi += 16) {
       score(qf, s);
       const int kn2 = key_page(pi + 32), vn2 = value_page(pi + 32);
+      __builtin_amdgcn_sched_barrier(0);
       load_keys(kn);
+      __builtin_amdgcn_sched_barrier(0);
       softmax<false>(s, pi, r, o, pb);
       values_part<HD, 0, HD / 16>(v, vs, o, pb);
       load_values(vn);
+      __builtin_amdgcn_sched_barrier(0);
       kn = kn2;
       vn = vn2;
     }
@@ -257,13 +300,17 @@ __device__ __forceinline__ void decode_item(const AttnF8Params& p, const AttnIte
   bf16x8 qf[HD / 32];
   load_q<HD>(p, qtok, qhead, row_valid, g4, qf);
   float* scores = nullptr;
+  const int rows = it.nrows <= 4 ? 4 : it.nrows <= 8 ? 8 : 16;
   if constexpr (TRACK) {
-    if (row_valid) scores = p.scores + p.score_base[it.req] + (int64_t)qhead * 16 * rq.n_pages;
+    const int r = col & (rows - 1), b = col / rows;  // row and first block of the lane's stores
+    if (r < it.nrows)
+      scores = p.scores + p.score_base[it.req] + (it.head + r) * score_row(rq.n_pages) + 16 * g4 +
+               4 * b;
   }
   DecodeScan<HD, NT, TRACK> scan{p, p.a.pages + rq.page_start, it.head / p.a.group,
                                  min(it.start + p.a.split_pages, rq.n_pages), rq.kv_len - 1,
                                  rq.kv_len, col, g4, p.a.scale_log2, 1.f / p.a.scale_log2, scores,
-                                 {}, {}, 0.f, 0.f};
+                                 rows, {}, {}, 0.f, 0.f};
   scan.run(it.start + 4 * wave, qf, o, r);
 
   float(*s_o)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(smem);
@@ -804,47 +851,72 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 __device__ __forceinline__ void add_weight(float* w, float x) { unsafeAtomicAdd(w, x); }
 
 // weight[slot][g] += sum over the q heads h of group g of exp2(score - lse[h]), the
-// scores as the attention left them: one thread per four keys.
+// scores as the attention left them: four keys per thread, 256 apart, so that the adds
+// of a wave are one run (four neighbouring keys per thread: 30 us for 64 requests of
+// 300 to 8192 tokens of the 8B heads, DECODE_US this way).
 template <int HD>
 __global__ __launch_bounds__(256) void weight_decode_kernel(AttnF8Params p,
                                                             const WeightItem* items) {
-  const WeightItem it = items[blockIdx.x];
+  const WeightItem it = items[blockIdx.x / p.a.nkv];
   const ReqDev rq = p.a.reqs[it.req];
-  const int g = blockIdx.y, group = p.a.group;
-  const int key = it.start * 16 + 4 * threadIdx.x;
-  if (key >= rq.kv_len) return;
-  const int64_t len = 16 * (int64_t)rq.n_pages;
-  const float* s = p.scores + p.score_base[it.req] + (int64_t)g * group * len + key;
+  const int g = blockIdx.x % p.a.nkv, group = p.a.group;
+  const int64_t len = score_row(rq.n_pages);
+  const float* s = p.scores + p.score_base[it.req] + (int64_t)g * group * len;
   const float* lse = p.a.lse + (int64_t)rq.tok_start * p.a.nq + g * group;
-  f32x4 w = f32x4{0.f, 0.f, 0.f, 0.f};
+  static_assert(kWeightDecodePages == 64, "four rounds of 256 keys");
+  const int key0 = it.start * 16 + (int)threadIdx.x;
+  float w[4] = {0.f, 0.f, 0.f, 0.f};
+  int64_t page[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++)  // (keys past the request: its last one's, not used)
+    page[i] = p.a.pages[rq.page_start + (min(key0 + 256 * i, rq.kv_len - 1) >> 4)];
+#pragma unroll 4
   for (int h = 0; h < group; h++) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(s + h * len);
     const float l = lse[h];
 #pragma unroll
-    for (int i = 0; i < 4; i++) w[i] += fast_exp2(x[i] - l);
+    for (int i = 0; i < 4; i++)
+      w[i] += fast_exp2(s[h * len + min(key0 + 256 * i, rq.kv_len - 1)] - l);
   }
-  const int64_t page = p.a.pages[rq.page_start + (key >> 4)];
-  float* out = p.weight + (page * p.a.nkv + g) * 16 + (key & 15);
+#pragma unroll
   for (int i = 0; i < 4; i++)
-    if (key + i < rq.kv_len) add_weight(out + i, w[i]);
+    if (key0 + 256 * i < rq.kv_len)
+      add_weight(p.weight + (page[i] * p.a.nkv + g) * 16 + (key0 & 15), w[i]);
 }
 
-// The same for a prefill chunk, whose scores are computed again: a workgroup holds
-// 64 keys of one KV head, its four waves take the 16-row blocks of the group's query
-// rows in turn, and their sums meet in LDS.
+// The same for a prefill chunk, whose scores are computed again: a wave holds 64 keys
+// of one KV head in registers, and the four waves of a workgroup, 256 keys, go through
+// the group's query rows together, 32 rows of a head at a time through LDS, the next 32
+// in flight meanwhile.  (Read from global memory by the lanes that need them the rows
+// took longer than all the rest: they lie a power of two apart, in one L1 set and on
+// few L2 channels.  1024 tokens over 4001, 8B heads: 112 us against PREFILL_US.)  Where
+// there are few keys the rows are split into parts (p.parts); each leaves its sums in
+// the workspace, and a second launch adds them up in order.
+//
+// In LDS the 16-byte piece j of row r lies at j ^ row_swizzle(r), so that the 16 lanes
+// it serves at a time hit distinct bank groups.
+constexpr int kWeightRows = 32;
 template <int HD>
-__global__ __launch_bounds__(256) void weight_prefill_kernel(AttnF8Params p,
-                                                             const WeightItem* items) {
-  __shared__ float s_w[4][64];
-  const WeightItem it = items[blockIdx.x];
+__device__ __forceinline__ int row_swizzle(int r) {
+  if constexpr (HD == 128) return r & 15;
+  else return ((r >> 1) & 5) | ((r >> 2) & 2);
+}
+template <int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void weight_prefill_kernel(
+    AttnF8Params p, const WeightItem* items) {
+  __shared__ u32x4 s_q[2][kWeightRows * HD / 8];
+  __shared__ float s_lse[2][kWeightRows];
+  const int g = blockIdx.x % p.a.nkv, tile = blockIdx.x / p.a.nkv / p.parts;
+  const int part = blockIdx.x / p.a.nkv % p.parts;
+  const WeightItem it = items[tile];
   const ReqDev rq = p.a.reqs[it.req];
-  const int g = blockIdx.y, group = p.a.group;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = p.a.group;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g4 = lane >> 4;
-  const int page = it.start + g4;  // this lane's page
+  const int page0 = it.start + 4 * wave, page = page0 + g4;  // the wave's pages, this lane's
   bf16x8 kf[4][HD / 32];
   {
-    const int id = p.a.pages[rq.page_start + min(it.start + (col >> 2), rq.n_pages - 1)];
+    const int id = p.a.pages[rq.page_start + min(page0 + (col >> 2), rq.n_pages - 1)];
     const int64_t kp = (int64_t)id * p.a.nkv + g;
     const uint8_t* k = p.k8 + kp * (16 * HD) + (col & 3) * 64 + 16 * g4;
     const float ks = p.k_scale[kp];
@@ -858,43 +930,118 @@ __global__ __launch_bounds__(256) void weight_prefill_kernel(AttnF8Params p,
       }
   }
   float acc[4][4] = {};
-  // rows before the first key see none of these keys
-  const int blk0 = max(0, it.start * 16 - rq.ctx_len) / 16, blks = (rq.n_new + 15) / 16 - blk0;
-  for (int t = wave; t < blks * group; t += 4) {
-    const int row0 = 16 * (blk0 + t / group), head = g * group + t % group;
-    const int row = row0 + col;
-    const bool valid = row < rq.n_new;
-    const int64_t tok = rq.tok_start + (valid ? row : rq.n_new - 1);
-    bf16x8 qf[HD / 32];
-    load_q<HD>(p, tok, head, true, g4, qf);
-    const float lse = p.a.lse[tok * p.a.nq + head];
-    const int row_pos = valid ? rq.ctx_len + row : -1;
+  // Row blocks from the first that sees one of the 256 keys on, this part's share of
+  // them; from `whole` on the rows see them all.
+  const int first_key = it.start * 16, blocks = (rq.n_new + kWeightRows - 1) / kWeightRows;
+  const int blk0 = max(0, first_key - rq.ctx_len) / kWeightRows;
+  const int share = (blocks - blk0 + p.parts - 1) / p.parts;
+  const int begin = blk0 + part * share, end = min(begin + share, blocks);
+  const int whole = (max(0, first_key + 255 - rq.ctx_len) + kWeightRows - 1) / kWeightRows;
+
+  // this thread's pieces of a block of rows, and a row's log-sum (infinite past the last
+  // row, which then adds 0)
+  constexpr int PIECES = HD / 8, NP = kWeightRows * PIECES / 256;
+  u32x4 piece[NP];
+  float row_lse = 0.f;
+  auto fetch = [&](int blk, int head) {
+    const int h = g * group + head;
 #pragma unroll
-    for (int b = 0; b < 4; b++) {
-      f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NP; i++) {
+      const int u = threadIdx.x + 256 * i;
+      const int64_t tok = rq.tok_start + min(kWeightRows * blk + u / PIECES, rq.n_new - 1);
+      piece[i] = *reinterpret_cast<const u32x4*>(p.a.q + tok * p.a.q_tok_stride + (int64_t)h * HD +
+                                                 8 * (u % PIECES));
+    }
+    if (threadIdx.x < kWeightRows) {
+      const int row = kWeightRows * blk + threadIdx.x;
+      row_lse = row < rq.n_new ? p.a.lse[(int64_t)(rq.tok_start + row) * p.a.nq + h] : __builtin_inff();
+    }
+  };
+  auto put = [&](int buf) {
 #pragma unroll
-      for (int e = 0; e < HD / 32; e++) s = mfma16(kf[b][e], qf[e], s);
+    for (int i = 0; i < NP; i++) {
+      const int u = threadIdx.x + 256 * i, r = u / PIECES;
+      s_q[buf][r * PIECES + ((u % PIECES) ^ row_swizzle<HD>(r))] = piece[i];
+    }
+    if (threadIdx.x < kWeightRows) s_lse[buf][threadIdx.x] = row_lse;
+  };
+  auto add = [&](auto mask, int buf, int row0, int sub) {  // 16 rows of the block
+    const int r = 16 * sub + col;
+    bf16x8 q[HD / 32];
+#pragma unroll
+    for (int e = 0; e < HD / 32; e++)  // dims 64 (e / 2) + 16 g4 + 8 (e % 2) .. + 7
+      q[e] = as_bf16x8(s_q[buf][r * PIECES + ((8 * (e >> 1) + 2 * g4 + (e & 1)) ^ row_swizzle<HD>(r))]);
+    const float lse = s_lse[buf][r];
+    f32x4 s[4];
+#pragma unroll
+    for (int b = 0; b < 4; b++) s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < HD / 32; e++)
+#pragma unroll
+      for (int b = 0; b < 4; b++) s[b] = mfma16(kf[b][e], q[e], s[b]);
+    const int last = rq.ctx_len + row0 + r - page * 16;  // the page's last token that counts
+#pragma unroll
+    for (int b = 0; b < 4; b++)
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        const float w = fast_exp2(fmaf(s[i], p.a.scale_log2, -lse));
-        acc[b][i] += page * 16 + 4 * b + i <= row_pos ? w : 0.f;
+        const float w = fast_exp2(fmaf(s[b][i], p.a.scale_log2, -lse));
+        acc[b][i] += !decltype(mask)::value || 4 * b + i <= last ? w : 0.f;
       }
+  };
+  if (begin < end) {
+    fetch(begin, 0);
+    put(0);
+    __syncthreads();
+    int blk = begin, head = 0;
+    for (int buf = 0; blk < end; buf ^= 1) {
+      int nblk = blk, nhead = head + 1;
+      if (nhead == group) {
+        nhead = 0;
+        nblk++;
+      }
+      if (nblk < end) fetch(nblk, nhead);
+      const int row0 = kWeightRows * blk;
+#pragma unroll
+      for (int sub = 0; sub < kWeightRows / 16; sub++) {
+        if (blk < whole) add(std::integral_constant<bool, true>{}, buf, row0, sub);
+        else add(std::integral_constant<bool, false>{}, buf, row0, sub);
+      }
+      if (nblk < end) put(buf ^ 1);
+      __syncthreads();
+      blk = nblk;
+      head = nhead;
     }
   }
+  // the sums over the 16 rows of a block: lane 16 g4 + col keeps token col of page g4
+  float w = 0.f;
 #pragma unroll
   for (int b = 0; b < 4; b++)
 #pragma unroll
     for (int i = 0; i < 4; i++) {
 #pragma unroll
       for (int m = 1; m < 16; m <<= 1) acc[b][i] += __shfl_xor(acc[b][i], m);
-      if (col == 4 * b + i) s_w[wave][lane] = acc[b][i];
+      if (col == 4 * b + i) w = acc[b][i];
     }
-  __syncthreads();
+  const int key = page * 16 + col;
+  if (p.parts > 1)
+    p.part_w[(int64_t)blockIdx.x * 256 + threadIdx.x] = w;
+  else if (key < rq.kv_len)
+    add_weight(p.weight + ((int64_t)p.a.pages[rq.page_start + page] * p.a.nkv + g) * 16 + col, w);
+}
+
+// Adds the parts' sums of 256 keys of one KV head.
+__global__ __launch_bounds__(256) void weight_parts_kernel(AttnF8Params p, const WeightItem* items) {
+  const int g = blockIdx.x % p.a.nkv, tile = blockIdx.x / p.a.nkv;
+  const WeightItem it = items[tile];
+  const ReqDev rq = p.a.reqs[it.req];
   const int key = it.start * 16 + (int)threadIdx.x;
-  if (threadIdx.x >= 64 || key >= rq.kv_len) return;
-  const float w = (s_w[0][threadIdx.x] + s_w[1][threadIdx.x]) + (s_w[2][threadIdx.x] + s_w[3][threadIdx.x]);
+  if (key >= rq.kv_len) return;
+  const float* w = p.part_w + ((int64_t)tile * p.parts * p.a.nkv + g) * 256 + threadIdx.x;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < p.parts; i++) sum += w[(int64_t)i * p.a.nkv * 256];
   const int64_t id = p.a.pages[rq.page_start + (key >> 4)];
-  add_weight(p.weight + (id * p.a.nkv + g) * 16 + (key & 15), w);
+  add_weight(p.weight + (id * p.a.nkv + g) * 16 + (key & 15), sum);
 }
 
 template <int HD>
@@ -916,11 +1063,13 @@ hipError_t launch(const AttnF8Params& p, int n_items, const MergeItem* merges, i
   hipError_t e = launch_attn_merge(p.a, merges, n_merges, HD, stream);
   if (e != hipSuccess || !p.weight) return e;
   if (n_dec > 0) {
-    weight_decode_kernel<HD><<<dim3(n_dec, p.a.nkv), 256, 0, stream>>>(p, dec);
+    weight_decode_kernel<HD><<<n_dec * p.a.nkv, 256, 0, stream>>>(p, dec);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (n_pre > 0) {
-    weight_prefill_kernel<HD><<<dim3(n_pre, p.a.nkv), 256, 0, stream>>>(p, pre);
+    weight_prefill_kernel<HD><<<n_pre * p.parts * p.a.nkv, 256, 0, stream>>>(p, pre);
+    if ((e = hipGetLastError()) != hipSuccess || p.parts == 1) return e;
+    weight_parts_kernel<<<n_pre * p.a.nkv, 256, 0, stream>>>(p, pre);
     e = hipGetLastError();
   }
   return e;

@@ -1259,12 +1259,12 @@ int64_t page_touched_twice(const mx_batch* b) {
 // and the decodes' scores.
 struct LayoutF8 {
   Layout base;  // reqs, pages, items, merges, part_o, part_ml
-  size_t score_base = 0, dec = 0, pre = 0, meta_end = 0, lse = 0, scores = 0, total = 0;
+  size_t score_base = 0, dec = 0, pre = 0, meta_end = 0, lse = 0, scores = 0, part_w = 0, total = 0;
 };
 
 LayoutF8 make_layout_f8(int64_t R, int64_t T, int64_t n_pages, int64_t n_items, int64_t n_merges,
                         int64_t n_parts, int64_t n_dec, int64_t n_pre, int64_t n_scores,
-                        const mx_attn_shape* s, bool track) {
+                        int64_t n_part_w, const mx_attn_shape* s, bool track) {
   LayoutF8 F;
   Layout& L = F.base;
   size_t o = 0;
@@ -1284,14 +1284,20 @@ LayoutF8 make_layout_f8(int64_t R, int64_t T, int64_t n_pages, int64_t n_items, 
   if (track) {
     F.lse = o; o = align_up(o + T * s->n_q_heads * 4);
     F.scores = o; o = align_up(o + n_scores * 4);
+    F.part_w = o; o = align_up(o + n_part_w * 4);
   }
   F.total = o;
   return F;
 }
 
+// Workgroups of 256 keys, one KV head and a part of the rows that the weights of prompt
+// chunks are computed by: as many parts as it takes for two per CU.
+constexpr int64_t kWeightUnits = 512;
+
 struct PlanF8 {
   Plan p;
   int64_t n_dec = 0, n_pre = 0, n_scores = 0;
+  int parts = 1;  // of a chunk's rows in the accumulation of its weights
   LayoutF8 L;
 };
 
@@ -1301,13 +1307,16 @@ void build_plan_f8(const mx_batch* b, const mx_attn_shape* s, bool track, PlanF8
     for (const ReqDev& d : f.p.reqs) {
       if (d.phase == MX_DECODE) {
         f.n_dec += ceil_div(d.n_pages, kWeightDecodePages);
-        f.n_scores += (int64_t)s->n_q_heads * 16 * d.n_pages;
+        f.n_scores += s->n_q_heads * score_row(d.n_pages);
       } else {
         f.n_pre += ceil_div(d.n_pages, kWeightPrefillPages);
       }
     }
+  const int64_t units = f.n_pre * s->n_kv_heads;
+  f.parts = units > 0 ? (int)ceil_div(kWeightUnits, std::min(units, kWeightUnits)) : 1;
   f.L = make_layout_f8(f.p.R, f.p.T, f.p.n_pages, f.p.n_items, (int64_t)f.p.merges.size(),
-                       f.p.n_parts, f.n_dec, f.n_pre, f.n_scores, s, track);
+                       f.p.n_parts, f.n_dec, f.n_pre, f.n_scores,
+                       f.parts > 1 ? 256 * f.parts * units : 0, s, track);
 }
 
 void pack_meta_f8(const PlanF8& f, const mx_attn_shape* s, bool track, char* h) {
@@ -1321,7 +1330,7 @@ void pack_meta_f8(const PlanF8& f, const mx_attn_shape* s, bool track, char* h) 
     const ReqDev& d = f.p.reqs[r];
     base[r] = at;
     if (d.phase == MX_DECODE) {
-      at += (int64_t)s->n_q_heads * 16 * d.n_pages;
+      at += s->n_q_heads * score_row(d.n_pages);
       for (int pg = 0; pg < d.n_pages; pg += kWeightDecodePages) *dec++ = WeightItem{r, pg};
     } else {
       for (int pg = 0; pg < d.n_pages; pg += kWeightPrefillPages) *pre++ = WeightItem{r, pg};
@@ -1356,7 +1365,10 @@ MX_EXPORT size_t mx_workspace_bytes_f8(const mx_attn_shape* shape, int32_t track
       splits * nkv * ceil_div(group, 16) + (max_tokens / kPrefillTileRows + max_reqs) * nq;
   return std::max(make_layout_f8(max_reqs, max_tokens, max_pages, items, max_reqs, splits * nq,
                                  max_pages / kWeightDecodePages + max_reqs,
-                                 max_pages / kWeightPrefillPages + max_reqs, nq * 16 * max_pages,
+                                 max_pages / kWeightPrefillPages + max_reqs,
+                                 nq * (16 * max_pages + 64 * (int64_t)max_reqs),
+                                 // parts * units < kWeightUnits + units
+                                 256 * (kWeightUnits + nkv * (max_pages / kWeightPrefillPages + max_reqs)),
                                  shape, track != 0)
                       .total,
                   kAlign);
@@ -1424,6 +1436,8 @@ MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape*
     a.weight = cache->weight;
     a.scores = at<float>(ws, L.scores);
     a.score_base = at<int64_t>(ws, L.score_base);
+    a.part_w = at<float>(ws, L.part_w);
+    a.parts = f.parts;
     const hipError_t e = timed("paged_attn_f8", stream, [&] {
       return launch_paged_attn_f8(a, (int)f.p.n_items, at<MergeItem>(ws, L.base.merges),
                                   (int)f.p.merges.size(), at<WeightItem>(ws, L.dec), (int)f.n_dec,

@@ -42,18 +42,24 @@ struct CacheF8 {
 
 // Keys of one request whose attention weight a workgroup accumulates: pages start ..
 // of its table, kWeightDecodePages of a decode's, kWeightPrefillPages of a chunk's.
-constexpr int kWeightDecodePages = 64, kWeightPrefillPages = 4;
+constexpr int kWeightDecodePages = 64, kWeightPrefillPages = 16;
 struct WeightItem {
   int32_t req, start;
 };
+// Scores of one query row of a decode: 64 a step, so that every row starts a cache line.
+__host__ __device__ __forceinline__ int64_t score_row(int64_t n_pages) {
+  return (n_pages + 3) / 4 * 64;
+}
 
 struct AttnF8Params {
   AttnParams a;               // k_pool and v_pool unused; lse set where weight is
   const uint8_t *k8, *v8;
   const float *k_scale, *v_scale;
   float* weight;              // null: weights are not accumulated
-  float* scores;              // decodes' scores in log2 units, [nq][16 n_pages] per request
+  float* scores;              // decodes' scores in log2 units, [nq][score_row] per request
   const int64_t* score_base;  // [R] first score of the request
+  float* part_w;              // a chunk's weights by parts of its rows: [item][part][nkv][256]
+  int parts;                  // parts of a chunk's rows (1: part_w unused)
 };
 // The attention of the items, the merge of the key splits and, where p.weight is
 // set, the accumulation of the weights.

@@ -219,8 +219,8 @@ def test_launches(fake_hip):  # noqa: F811
         """)
     assert set(r["st"]) == {0} and r["bad"] == 0
     got = {k: [next(n for n in ("upload", "kv_append_f8", "paged_attn_f8", "weight_decode",
-                                "weight_prefill", "evict_select", "evict_move") if n in x)
+                                "weight_prefill", "weight_parts", "evict_select", "evict_move") if n in x)
                for x in v] for k, v in r["kernels"].items()}
     assert got == {"append": ["kv_append_f8"], "attn": ["upload", "paged_attn_f8"],
-                   "track": ["upload", "paged_attn_f8", "weight_decode", "weight_prefill"],
+                   "track": ["upload", "paged_attn_f8", "weight_decode", "weight_prefill", "weight_parts"],
                    "evict": ["upload", "evict_select", "evict_move"]}
