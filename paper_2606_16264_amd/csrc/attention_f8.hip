@@ -195,7 +195,7 @@ struct DecodeScan {
   // The scores of the item's rows, 64 bytes a row and page.  With up to 4 (8) rows the
   // lanes of the other columns take blocks 1 .. 3 (the odd blocks) of those rows, so
   // that one store (two) holds whole runs and not a quarter of each with a quarter of
-  // the lanes: 64 decodes of the 8B heads 108 -> SCORES_US us.
+  // the lanes: 64 decodes of the 8B heads 108 -> 101 us (82 without weights).
   __device__ __forceinline__ void store_scores(const f32x4 (&s)[4], int pi, bool valid) {
     auto moved = [&](float to, float from, auto ctrl, auto banks) {  // banks: columns / 4
       return __uint_as_float(__builtin_amdgcn_update_dpp(
@@ -352,7 +352,7 @@ __device__ __forceinline__ void decode_item(const AttnF8Params& p, const AttnIte
 #pragma unroll
     for (int e = 0; e < HD / 16; e += 2)
       *reinterpret_cast<uint32_t*>(op + e) = pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
-    if (TRACK && (threadIdx.x & 15) == 0) p.a.lse[qtok * p.a.nq + h] = M + log2f(L);
+    if (TRACK && (threadIdx.x & 15) == 0) p.lse[qtok * p.a.nq + h] = M + log2f(L);
   } else {
     const int64_t part = (int64_t)it.part + (int64_t)row * rq.n_split;
     float* po = p.a.part_o + part * HD + dseg;
@@ -817,7 +817,7 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
       w[1] = pack_bf16x2(acc[db][2] * inv, acc[db][3] * inv);
       *reinterpret_cast<u32x2*>(op + (db >> 1) * step32 + (db & 1) * 16) = w;
     }
-    if (TRACK && g4 == 0) p.a.lse[tok * p.a.nq + qhead] = r.m + log2f(l);
+    if (TRACK && g4 == 0) p.lse[tok * p.a.nq + qhead] = r.m + log2f(l);
   };
   if (row_valid) store(qtok, l1, r1, o);
   if (row_valid2) store(qtok2, l2, r2, o2);
@@ -850,32 +850,73 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 // and then several workgroups add to one token.
 __device__ __forceinline__ void add_weight(float* w, float x) { unsafeAtomicAdd(w, x); }
 
-// weight[slot][g] += sum over the q heads h of group g of exp2(score - lse[h]), the
-// scores as the attention left them: four keys per thread, 256 apart, so that the adds
-// of a wave are one run (four neighbouring keys per thread: 30 us for 64 requests of
-// 300 to 8192 tokens of the 8B heads, DECODE_US this way).
+// What follows the attention of decodes whose weights are accumulated, in one launch:
+// the merge of the key splits, and
+//   weight[slot][g] += sum over the q heads h of group g of exp2(score - lse[h]),
+// the scores as the attention left them, lse from the splits' own maxima and sums
+// (which the merge combines to the same) or, unsplit, as the attention left it.
+// weights: four keys per thread, 256 apart, so that the adds of a wave are one run
+// (four neighbouring keys per thread took 30 us for 64 requests of 300 to 8192 tokens
+// of the 8B heads, 10 this way).
 template <int HD>
-__global__ __launch_bounds__(256) void weight_decode_kernel(AttnF8Params p,
-                                                            const WeightItem* items) {
+__global__ __launch_bounds__(kMergeThreads) void weight_decode_kernel(AttnF8Params p,
+                                                                      const WeightItem* items,
+                                                                      int n_weights,
+                                                                      const MergeItem* merges) {
+  __shared__ __attribute__((aligned(16))) float smem[merge_floats<HD>()];
+  static_assert(kWeightDecodePages == 64 && kMergeThreads == 256, "four rounds of 256 keys");
+  if ((int)blockIdx.x >= n_weights) {
+    const int i = blockIdx.x - n_weights;
+    merge_splits<HD>(p.a, merges[i / p.a.nq], i % p.a.nq, smem);
+    return;
+  }
   const WeightItem it = items[blockIdx.x / p.a.nkv];
   const ReqDev rq = p.a.reqs[it.req];
   const int g = blockIdx.x % p.a.nkv, group = p.a.group;
   const int64_t len = score_row(rq.n_pages);
   const float* s = p.scores + p.score_base[it.req] + (int64_t)g * group * len;
-  const float* lse = p.a.lse + (int64_t)rq.tok_start * p.a.nq + g * group;
-  static_assert(kWeightDecodePages == 64, "four rounds of 256 keys");
-  const int key0 = it.start * 16 + (int)threadIdx.x;
-  float w[4] = {0.f, 0.f, 0.f, 0.f};
+  const int t = threadIdx.x, key0 = it.start * 16 + t;
+  int key[4];  // (past the request: its last key, whose sum is not used)
   int64_t page[4];
 #pragma unroll
-  for (int i = 0; i < 4; i++)  // (keys past the request: its last one's, not used)
-    page[i] = p.a.pages[rq.page_start + (min(key0 + 256 * i, rq.kv_len - 1) >> 4)];
-#pragma unroll 4
-  for (int h = 0; h < group; h++) {
-    const float l = lse[h];
+  for (int i = 0; i < 4; i++) {
+    key[i] = min(key0 + 256 * i, rq.kv_len - 1);
+    page[i] = p.a.pages[rq.page_start + (key[i] >> 4)];
+  }
+  float w[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int h0 = 0; h0 < group; h0 += 16) {  // 16 heads at a time, 16 threads each for lse
+    const int h = g * group + h0 + (t >> 4);
+    float m = kNegBig, l = 0.f;
+    if (h0 + (t >> 4) < group) {
+      if (rq.n_split == 1) {
+        m = p.lse[(int64_t)rq.tok_start * p.a.nq + h];
+        l = (t & 15) == 0 ? 1.f : 0.f;
+      } else {
+        const float2* ml = reinterpret_cast<const float2*>(p.a.part_ml) + it.part + (int64_t)h * rq.n_split;
+        for (int k = t & 15; k < rq.n_split; k += 16) {
+          const float2 x = ml[k];
+          const float mn = fmaxf(m, x.x);
+          l = l * exp2f(m - mn) + x.y * exp2f(x.x - mn);
+          m = mn;
+        }
+      }
+    }
+    float M = m;
 #pragma unroll
-    for (int i = 0; i < 4; i++)
-      w[i] += fast_exp2(s[h * len + min(key0 + 256 * i, rq.kv_len - 1)] - l);
+    for (int x = 1; x < 16; x <<= 1) M = fmaxf(M, __shfl_xor(M, x));
+    l *= exp2f(m - M);
+#pragma unroll
+    for (int x = 1; x < 16; x <<= 1) l += __shfl_xor(l, x);
+    if ((t & 15) == 0) smem[t >> 4] = M + log2f(l);
+    __syncthreads();
+    const int heads = min(16, group - h0);
+#pragma unroll 4
+    for (int k = 0; k < heads; k++) {
+      const float lse = smem[k];
+#pragma unroll
+      for (int i = 0; i < 4; i++) w[i] += fast_exp2(s[(h0 + k) * len + key[i]] - lse);
+    }
+    __syncthreads();
   }
 #pragma unroll
   for (int i = 0; i < 4; i++)
@@ -888,7 +929,7 @@ __global__ __launch_bounds__(256) void weight_decode_kernel(AttnF8Params p,
 // the group's query rows together, 32 rows of a head at a time through LDS, the next 32
 // in flight meanwhile.  (Read from global memory by the lanes that need them the rows
 // took longer than all the rest: they lie a power of two apart, in one L1 set and on
-// few L2 channels.  1024 tokens over 4001, 8B heads: 112 us against PREFILL_US.)  Where
+// few L2 channels.  1024 tokens over 4001, 8B heads: 112 us against 64.)  Where
 // there are few keys the rows are split into parts (p.parts); each leaves its sums in
 // the workspace, and a second launch adds them up in order.
 //
@@ -954,7 +995,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
     }
     if (threadIdx.x < kWeightRows) {
       const int row = kWeightRows * blk + threadIdx.x;
-      row_lse = row < rq.n_new ? p.a.lse[(int64_t)(rq.tok_start + row) * p.a.nq + h] : __builtin_inff();
+      row_lse = row < rq.n_new ? p.lse[(int64_t)(rq.tok_start + row) * p.a.nq + h] : __builtin_inff();
     }
   };
   auto put = [&](int buf) {
@@ -1060,10 +1101,12 @@ hipError_t launch(const AttnF8Params& p, int n_items, const MergeItem* merges, i
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipError_t e = launch_attn_merge(p.a, merges, n_merges, HD, stream);
-  if (e != hipSuccess || !p.weight) return e;
+  if (!p.weight) return launch_attn_merge(p.a, merges, n_merges, HD, stream);
+  hipError_t e = hipSuccess;
   if (n_dec > 0) {
-    weight_decode_kernel<HD><<<n_dec * p.a.nkv, 256, 0, stream>>>(p, dec);
+    const int weights = n_dec * p.a.nkv;
+    weight_decode_kernel<HD><<<weights + n_merges * p.a.nq, kMergeThreads, 0, stream>>>(
+        p, dec, weights, merges);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (n_pre > 0) {

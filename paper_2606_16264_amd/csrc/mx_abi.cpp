@@ -702,7 +702,6 @@ AttnParams attn_params(const Plan& p, const Layout& L, const mx_attn_shape* s, v
   a.split_pages = p.split_pages;
   a.scale_log2 = eff_scale(s) * 1.4426950408889634f;
   a.decode_only = p.has_prefill ? 0 : 1;
-  a.lse = nullptr;
   return a;
 }
 
@@ -1326,14 +1325,16 @@ void pack_meta_f8(const PlanF8& f, const mx_attn_shape* s, bool track, char* h) 
   WeightItem* dec = (WeightItem*)(h + f.L.dec);
   WeightItem* pre = (WeightItem*)(h + f.L.pre);
   int64_t at = 0;
+  int32_t part = 0;
   for (int r = 0; r < f.p.R; r++) {
     const ReqDev& d = f.p.reqs[r];
     base[r] = at;
     if (d.phase == MX_DECODE) {
       at += s->n_q_heads * score_row(d.n_pages);
-      for (int pg = 0; pg < d.n_pages; pg += kWeightDecodePages) *dec++ = WeightItem{r, pg};
+      for (int pg = 0; pg < d.n_pages; pg += kWeightDecodePages) *dec++ = WeightItem{r, pg, part};
+      if (d.n_split > 1) part += s->n_q_heads * d.n_split;
     } else {
-      for (int pg = 0; pg < d.n_pages; pg += kWeightPrefillPages) *pre++ = WeightItem{r, pg};
+      for (int pg = 0; pg < d.n_pages; pg += kWeightPrefillPages) *pre++ = WeightItem{r, pg, 0};
     }
   }
 }
@@ -1428,7 +1429,7 @@ MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape*
     AttnF8Params a;
     a.a = attn_params(f.p, L.base, shape, ws, q, (int64_t)shape->n_q_heads * shape->head_dim,
                       nullptr, nullptr, out);
-    a.a.lse = track ? at<float>(ws, L.lse) : nullptr;
+    a.lse = at<float>(ws, L.lse);
     a.k8 = cache->k_pool;
     a.v8 = cache->v_pool;
     a.k_scale = cache->k_scale;

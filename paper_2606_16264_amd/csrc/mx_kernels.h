@@ -24,7 +24,6 @@ struct AttnParams {
   int32_t nq, nkv, group, split_pages;
   float scale_log2;        // softmax scale * log2(e)
   int32_t decode_only;     // no prefill items: decode keys and values are read non-temporally
-  float* lse;              // [T][nq] log2 of the row's sum of exponentials, or null
 };
 
 hipError_t launch_paged_attn(const AttnParams& p, int n_items, const MergeItem* merges,
@@ -45,6 +44,7 @@ struct CacheF8 {
 constexpr int kWeightDecodePages = 64, kWeightPrefillPages = 16;
 struct WeightItem {
   int32_t req, start;
+  int32_t part;  // a decode's: its partial of q head 0, split 0 (as MergeItem's)
 };
 // Scores of one query row of a decode: 64 a step, so that every row starts a cache line.
 __host__ __device__ __forceinline__ int64_t score_row(int64_t n_pages) {
@@ -52,10 +52,11 @@ __host__ __device__ __forceinline__ int64_t score_row(int64_t n_pages) {
 }
 
 struct AttnF8Params {
-  AttnParams a;               // k_pool and v_pool unused; lse set where weight is
+  AttnParams a;               // k_pool and v_pool unused
   const uint8_t *k8, *v8;
   const float *k_scale, *v_scale;
   float* weight;              // null: weights are not accumulated
+  float* lse;                 // [T][nq] log2 of a row's sum of exponentials (not of split decodes)
   float* scores;              // decodes' scores in log2 units, [nq][score_row] per request
   const int64_t* score_base;  // [R] first score of the request
   float* part_w;              // a chunk's weights by parts of its rows: [item][part][nkv][256]
