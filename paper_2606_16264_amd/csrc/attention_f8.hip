@@ -845,6 +845,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
     decode_item<HD, false, TRACK>(p, it, rq, smem);
 }
 
+struct SmallAttn {
+  AttnF8Params p;
+  InlineMeta meta;
+};
+template <int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void small_attn_f8_kernel(
+    SmallAttn a) {
+  __shared__ __attribute__((aligned(16))) char smem[smem_bytes<HD>()];
+  AttnF8Params p = a.p;
+  p.a.reqs = inline_meta(offsetof(SmallAttn, meta), p.a.reqs);
+  p.a.pages = inline_meta(offsetof(SmallAttn, meta), p.a.pages);
+  p.a.items = inline_meta(offsetof(SmallAttn, meta), p.a.items);
+  const AttnItem it = p.a.items[blockIdx.x];
+  const ReqDev rq = p.a.reqs[it.req];
+  if (it.kind == 1)
+    prefill_item<HD, false>(p, it, rq, smem);
+  else
+    decode_item<HD, true, false>(p, it, rq, smem);
+}
+
 // ---------------------------------------------------------------- attention weights
 // Added with an atomic: requests of a batch may share the pages of a cached prefix,
 // and then several workgroups add to one token.
@@ -1119,6 +1139,17 @@ hipError_t launch(const AttnF8Params& p, int n_items, const MergeItem* merges, i
 }
 
 }  // namespace
+
+hipError_t launch_small_attn_f8(const AttnF8Params& p, const InlineMeta& meta, int n_items,
+                                int head_dim, hipStream_t stream) {
+  if (n_items == 0) return hipSuccess;
+  const SmallAttn a{p, meta};
+  if (head_dim == 128)
+    small_attn_f8_kernel<128><<<n_items, 256, 0, stream>>>(a);
+  else
+    small_attn_f8_kernel<64><<<n_items, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
 
 hipError_t launch_paged_attn_f8(const AttnF8Params& p, int n_items, const MergeItem* merges,
                                 int n_merges, const WeightItem* dec, int n_dec,

@@ -184,15 +184,12 @@ __device__ __forceinline__ void append_values(const uint16_t* __restrict__ src, 
   if (lane == 0) *scale = ps.now;
 }
 
+// This wave's unit of a run: 2 g is the keys of head g, 2 g + 1 its values.
 template <int HD>
-__global__ __launch_bounds__(256) void kv_append_f8_kernel(const uint16_t* __restrict__ k_new,
-                                                           const uint16_t* __restrict__ v_new,
-                                                           CacheF8 c, const AppendRun* runs,
-                                                           int nkv) {
-  const u32x4 rw = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(runs + blockIdx.x));
-  const AppendRun run = __builtin_bit_cast(AppendRun, rw);
+__device__ __forceinline__ void append_unit(const uint16_t* k_new, const uint16_t* v_new,
+                                            const CacheF8& c, const AppendRun& run, int nkv) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int unit = blockIdx.y * 4 + wave;  // 2 g: keys of head g, 2 g + 1: its values
+  const int unit = blockIdx.y * 4 + wave;
   if (unit >= 2 * nkv) return;
   const int g = unit >> 1, s0 = (int)(run.slot & 15);
   const int64_t at = (run.slot >> 4) * nkv + g, row = (int64_t)nkv * HD;
@@ -202,6 +199,26 @@ __global__ __launch_bounds__(256) void kv_append_f8_kernel(const uint16_t* __res
                     c.weight ? c.weight + at * 16 : nullptr, s0, run.n, lane);
   else
     append_values<HD>(v_new + src, row, c.v + at * (16 * HD), c.v_scale + at, s0, run.n, lane);
+}
+
+template <int HD>
+__global__ __launch_bounds__(256) void kv_append_f8_kernel(const uint16_t* k_new,
+                                                           const uint16_t* v_new, CacheF8 c,
+                                                           const AppendRun* runs, int nkv) {
+  const u32x4 rw = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(runs + blockIdx.x));
+  append_unit<HD>(k_new, v_new, c, __builtin_bit_cast(AppendRun, rw), nkv);
+}
+
+struct SmallAppend {
+  const uint16_t *k_new, *v_new;
+  CacheF8 c;
+  int64_t nkv;
+  InlineMeta runs;
+};
+template <int HD>
+__global__ __launch_bounds__(256) void small_append_f8_kernel(SmallAppend a) {
+  const AppendRun* runs = inline_meta<AppendRun>(offsetof(SmallAppend, runs), nullptr);
+  append_unit<HD>(a.k_new, a.v_new, a.c, runs[blockIdx.x], (int)a.nkv);
 }
 
 // ---------------------------------------------------------------- eviction
@@ -240,9 +257,9 @@ __device__ __forceinline__ uint32_t suffix_sum(uint32_t x, int lane) {
 // by latency: loads, then up to four times adds, a barrier, the scan of the counters by
 // one wave, a barrier.
 template <int K>
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
-    const EvictReq* reqs, const int32_t* pages, const float* __restrict__ weight, int nkv,
-    int32_t* __restrict__ kept) {
+__device__ __forceinline__ void evict_select(const EvictReq* reqs, const int32_t* pages,
+                                             const float* __restrict__ weight, int nkv,
+                                             int32_t* __restrict__ kept) {
   __shared__ __attribute__((aligned(16))) uint32_t s_hist[4][256][4];
   __shared__ uint32_t s_pick[4][3];  // digit, keys missing within it, keys of it
   __shared__ __attribute__((aligned(16))) uint32_t s_total[kSelectWaves][2];
@@ -361,6 +378,14 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
   });
 }
 
+template <int K>
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const EvictReq* reqs,
+                                                                      const int32_t* pages,
+                                                                      const float* weight, int nkv,
+                                                                      int32_t* kept) {
+  evict_select<K>(reqs, pages, weight, nkv, kept);
+}
+
 // Copies the kept tokens of one destination page and KV head, a wave each.  The page's
 // scale is the largest of those its tokens come from.  Bound by memory: 108 us for 8192
 // tokens of 16 requests, 8 heads, 550 MB (200 written; keys are 64-byte runs, and of a
@@ -370,10 +395,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(
 // and takes the bytes it needs with byte permutes whose selectors are the same in all
 // lanes (as loads of single bytes: 177 us).
 template <int HD>
-__global__ __launch_bounds__(256) void evict_move_kernel(const EvictReq* reqs,
-                                                         const int32_t* pages,
-                                                         const EvictPage* items, CacheF8 c, int nkv,
-                                                         const int32_t* __restrict__ kept) {
+__device__ __forceinline__ void evict_move(const EvictReq* reqs, const int32_t* pages,
+                                           const EvictPage* items, const CacheF8& c, int nkv,
+                                           const int32_t* __restrict__ kept) {
   constexpr int NR = HD / 64;  // value rows per lane: lane, lane + 64
   const EvictPage it = items[blockIdx.x];
   const EvictReq rq = reqs[it.req];
@@ -497,7 +521,66 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictReq* reqs,
   }
 }
 
+template <int HD>
+__global__ __launch_bounds__(256) void evict_move_kernel(const EvictReq* reqs,
+                                                         const int32_t* pages,
+                                                         const EvictPage* items, CacheF8 c, int nkv,
+                                                         const int32_t* kept) {
+  evict_move<HD>(reqs, pages, items, c, nkv, kept);
+}
+
+struct SmallEvict {
+  const EvictReq* reqs;
+  const int32_t* pages;
+  const EvictPage* items;
+  CacheF8 c;
+  int32_t* kept;
+  int64_t nkv;
+  InlineMeta meta;
+};
+static_assert(kSmallEvict == 4 * kSelectThreads, "four keys a thread");
+__global__ __launch_bounds__(kSelectThreads) void small_evict_select_kernel(SmallEvict a) {
+  constexpr size_t at = offsetof(SmallEvict, meta);
+  evict_select<4>(inline_meta(at, a.reqs), inline_meta(at, a.pages), a.c.weight, (int)a.nkv, a.kept);
+}
+template <int HD>
+__global__ __launch_bounds__(256) void small_evict_move_kernel(SmallEvict a) {
+  constexpr size_t at = offsetof(SmallEvict, meta);
+  evict_move<HD>(inline_meta(at, a.reqs), inline_meta(at, a.pages), inline_meta(at, a.items), a.c,
+                 (int)a.nkv, a.kept);
+}
+
 }  // namespace
+
+hipError_t launch_small_append_f8(const uint16_t* k_new, const uint16_t* v_new,
+                                  const CacheF8& cache, const InlineMeta& meta, int64_t n_runs,
+                                  int nkv, int d, hipStream_t stream) {
+  if (n_runs == 0) return hipSuccess;
+  const dim3 grid((unsigned)n_runs, (2 * nkv + 3) / 4);
+  const SmallAppend a{k_new, v_new, cache, nkv, meta};
+  if (d == 128)
+    small_append_f8_kernel<128><<<grid, 256, 0, stream>>>(a);
+  else
+    small_append_f8_kernel<64><<<grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_small_evict_f8(const EvictReq* reqs, int n_reqs, const int32_t* pages,
+                                 const EvictPage* items, int64_t n_items, const InlineMeta& meta,
+                                 const CacheF8& cache, int32_t* kept, int nkv, int d,
+                                 hipStream_t stream) {
+  if (n_items == 0) return hipSuccess;
+  const SmallEvict a{reqs, pages, items, cache, kept, nkv, meta};
+  small_evict_select_kernel<<<dim3(n_reqs, nkv), kSelectThreads, 0, stream>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)n_items, (nkv + 3) / 4);
+  if (d == 128)
+    small_evict_move_kernel<128><<<grid, 256, 0, stream>>>(a);
+  else
+    small_evict_move_kernel<64><<<grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
 
 hipError_t launch_kv_append_f8(const uint16_t* k_new, const uint16_t* v_new, const CacheF8& cache,
                                const AppendRun* runs, int64_t n_runs, int nkv, int d,

@@ -1293,6 +1293,16 @@ LayoutF8 make_layout_f8(int64_t R, int64_t T, int64_t n_pages, int64_t n_items, 
 // chunks are computed by: as many parts as it takes for two per CU.
 constexpr int64_t kWeightUnits = 512;
 
+// The metadata of a call without splits, closely packed.
+Layout small_layout(const Plan& p) {
+  Layout L;
+  auto next = [](size_t end) { return (end + 15) / 16 * 16; };
+  L.items = next(p.R * sizeof(ReqDev));
+  L.pages = next(L.items + p.n_items * sizeof(AttnItem));
+  L.meta_end = next(L.pages + p.n_pages * sizeof(int32_t));
+  return L;
+}
+
 struct PlanF8 {
   Plan p;
   int64_t n_dec = 0, n_pre = 0, n_scores = 0;
@@ -1391,6 +1401,13 @@ MX_EXPORT mx_status mx_kv_append_f8(const mx_batch* batch, const mx_attn_shape* 
       return fail(MX_ERR_INVALID, "two requests append to page %lld", (long long)pg);
     if ((st = check_not_capturing(stream)) != MX_OK) return st;
     const int64_t n_runs = count_runs(batch);
+    if (n_runs * sizeof(AppendRun) <= sizeof(InlineMeta)) {
+      alignas(16) InlineMeta meta;
+      pack_runs(batch, reinterpret_cast<AppendRun*>(meta.b));
+      const hipError_t e = launch_small_append_f8(k_new, v_new, cache_args(cache), meta, n_runs,
+                                                  shape->n_kv_heads, shape->head_dim, stream);
+      return e == hipSuccess ? MX_OK : hip_fail(e, "append launch");
+    }
     return staged(
         n_runs * sizeof(AppendRun), stream,
         [&](char* h) { pack_runs(batch, reinterpret_cast<AppendRun*>(h)); },
@@ -1422,10 +1439,6 @@ MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape*
     if (ws_bytes < L.total)
       return fail(MX_ERR_TOO_LARGE, "workspace %zu bytes < %zu needed", ws_bytes, L.total);
     if ((st = check_not_capturing(stream)) != MX_OK) return st;
-    st = staged(
-        L.meta_end, stream, [&](char* h) { pack_meta_f8(f, shape, track, h); },
-        [&](const void* dev) { return launch_upload(dev, ws, L.meta_end, stream); });
-    if (st != MX_OK) return st;
     AttnF8Params a;
     a.a = attn_params(f.p, L.base, shape, ws, q, (int64_t)shape->n_q_heads * shape->head_dim,
                       nullptr, nullptr, out);
@@ -1439,6 +1452,22 @@ MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape*
     a.score_base = at<int64_t>(ws, L.score_base);
     a.part_w = at<float>(ws, L.part_w);
     a.parts = f.parts;
+    if (const Layout small = small_layout(f.p); small.meta_end <= sizeof(InlineMeta) && !track &&
+                                                f.p.merges.empty()) {
+      alignas(16) InlineMeta meta;
+      pack_meta(f.p, small, shape, meta.b);
+      a.a.reqs = reinterpret_cast<const ReqDev*>(small.reqs);
+      a.a.pages = reinterpret_cast<const int32_t*>(small.pages);
+      a.a.items = reinterpret_cast<const AttnItem*>(small.items);
+      const hipError_t e = timed("paged_attn_f8", stream, [&] {
+        return launch_small_attn_f8(a, meta, (int)f.p.n_items, shape->head_dim, stream);
+      });
+      return e == hipSuccess ? MX_OK : hip_fail(e, "attention launch");
+    }
+    st = staged(
+        L.meta_end, stream, [&](char* h) { pack_meta_f8(f, shape, track, h); },
+        [&](const void* dev) { return launch_upload(dev, ws, L.meta_end, stream); });
+    if (st != MX_OK) return st;
     const hipError_t e = timed("paged_attn_f8", stream, [&] {
       return launch_paged_attn_f8(a, (int)f.p.n_items, at<MergeItem>(ws, L.base.merges),
                                   (int)f.p.merges.size(), at<WeightItem>(ws, L.dec), (int)f.n_dec,
@@ -1531,26 +1560,36 @@ MX_EXPORT mx_status mx_kv_evict_f8(int32_t num_reqs, const mx_evict_request* req
     if (ws_bytes < p.total)
       return fail(MX_ERR_TOO_LARGE, "workspace %zu bytes < %zu needed", ws_bytes, p.total);
     if ((st = check_not_capturing(stream)) != MX_OK) return st;
-    st = staged(
-        p.total, stream,
-        [&](char* h) {
-          EvictReq* er = (EvictReq*)h;
-          int32_t* pages = (int32_t*)(h + p.pages);
-          EvictPage* item = (EvictPage*)(h + p.items);
-          int64_t at_kept = 0;
-          int32_t pg = 0;
-          for (int r = 0; r < num_reqs; r++) {
-            const mx_evict_request& q = reqs[r];
-            const int32_t ns = (int32_t)ceil_div(q.len, 16), nd = (int32_t)ceil_div(q.keep, 16);
-            er[r] = EvictReq{q.len, q.keep, q.recent, pg, pg + ns, 0, at_kept};
-            if (ns) memcpy(pages + pg, q.pages, ns * sizeof(int32_t));
-            if (nd) memcpy(pages + pg + ns, q.dst_pages, nd * sizeof(int32_t));
-            for (int32_t i = 0; i < nd; i++) *item++ = EvictPage{r, 16 * i};
-            pg += ns + nd;
-            at_kept += (int64_t)shape->n_kv_heads * q.keep;
-          }
-        },
-        [&](const void* dev) { return launch_upload(dev, ws, p.total, stream); });
+    auto pack = [&](char* h) {
+      EvictReq* er = (EvictReq*)h;
+      int32_t* pages = (int32_t*)(h + p.pages);
+      EvictPage* item = (EvictPage*)(h + p.items);
+      int64_t at_kept = 0;
+      int32_t pg = 0;
+      for (int r = 0; r < num_reqs; r++) {
+        const mx_evict_request& q = reqs[r];
+        const int32_t ns = (int32_t)ceil_div(q.len, 16), nd = (int32_t)ceil_div(q.keep, 16);
+        er[r] = EvictReq{q.len, q.keep, q.recent, pg, pg + ns, 0, at_kept};
+        if (ns) memcpy(pages + pg, q.pages, ns * sizeof(int32_t));
+        if (nd) memcpy(pages + pg + ns, q.dst_pages, nd * sizeof(int32_t));
+        for (int32_t i = 0; i < nd; i++) *item++ = EvictPage{r, 16 * i};
+        pg += ns + nd;
+        at_kept += (int64_t)shape->n_kv_heads * q.keep;
+      }
+    };
+    if (p.total <= sizeof(InlineMeta) && p.longest <= kSmallEvict) {
+      alignas(16) InlineMeta meta;
+      pack(meta.b);
+      const hipError_t e = timed("kv_evict_f8", stream, [&] {
+        return launch_small_evict_f8(nullptr, num_reqs, reinterpret_cast<const int32_t*>(p.pages),
+                                     reinterpret_cast<const EvictPage*>(p.items), p.dst_pages, meta,
+                                     cache_args(cache), kept, shape->n_kv_heads, shape->head_dim,
+                                     stream);
+      });
+      return e == hipSuccess ? MX_OK : hip_fail(e, "eviction launch");
+    }
+    st = staged(p.total, stream, pack,
+                [&](const void* dev) { return launch_upload(dev, ws, p.total, stream); });
     if (st != MX_OK) return st;
     const hipError_t e = timed("kv_evict_f8", stream, [&] {
       return launch_kv_evict_f8(at<EvictReq>(ws, 0), num_reqs, p.longest, at<int32_t>(ws, p.pages),

@@ -127,6 +127,14 @@ __device__ __forceinline__ void dma16_at(const void* base, unsigned off, unsigne
                : "memory");
 }
 
+// A table inside the kernel's own argument block: `offset` bytes into the member that
+// starts `member` bytes into the kernel's only argument.
+template <typename T>
+__device__ __forceinline__ const T* inline_meta(size_t member, const T* offset) {
+  const char* args = (const char*)__builtin_amdgcn_kernarg_segment_ptr();
+  return reinterpret_cast<const T*>(args + member + reinterpret_cast<uintptr_t>(offset));
+}
+
 // Request record uploaded by the host planner.
 struct ReqDev {
   int32_t tok_start;  // first row of the request in the batch

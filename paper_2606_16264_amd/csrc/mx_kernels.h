@@ -32,6 +32,14 @@ hipError_t launch_paged_attn(const AttnParams& p, int n_items, const MergeItem* 
 hipError_t launch_attn_merge(const AttnParams& p, const MergeItem* merges, int n_merges,
                              int head_dim, hipStream_t stream);
 
+// Metadata of a small call, handed over with the kernel's arguments: no staging buffer
+// and no upload, which are most of such a call's time.  Offsets in it stand in the
+// argument's pointers (inline_meta, mx_device.h).
+constexpr int kInlineBytes = 3584;  // beside the other arguments within the 4 KB of a launch
+struct InlineMeta {
+  char b[kInlineBytes];
+};
+
 // The 8-bit cache of a layer, as the ABI's mx_cache_f8.
 struct CacheF8 {
   uint8_t *k, *v;           // [pages][nkv][d / 64][16][64] and [pages][nkv][d][16] e4m3 codes
@@ -69,11 +77,21 @@ hipError_t launch_paged_attn_f8(const AttnF8Params& p, int n_items, const MergeI
                                 const WeightItem* pre, int n_pre, int head_dim,
                                 hipStream_t stream);
 
+// The same for a call without splits and weights, its metadata (reqs, pages and items,
+// whose pointers are offsets) with the arguments.
+hipError_t launch_small_attn_f8(const AttnF8Params& p, const InlineMeta& meta, int n_items,
+                                int head_dim, hipStream_t stream);
+
 // Append to the 8-bit cache, one run per page that new tokens touch (runs as for
 // launch_kv_append; no two of one page).
 hipError_t launch_kv_append_f8(const uint16_t* k_new, const uint16_t* v_new, const CacheF8& cache,
                                const AppendRun* runs, int64_t n_runs, int nkv, int d,
                                hipStream_t stream);
+
+// The same with the runs at the start of meta.
+hipError_t launch_small_append_f8(const uint16_t* k_new, const uint16_t* v_new,
+                                  const CacheF8& cache, const InlineMeta& meta, int64_t n_runs,
+                                  int nkv, int d, hipStream_t stream);
 
 // Eviction: src and dst are offsets of a request's page tables in the flat page
 // array, kept that of its first index in the kept array ([nkv][keep] per request).
@@ -89,6 +107,13 @@ struct EvictPage {
 hipError_t launch_kv_evict_f8(const EvictReq* reqs, int n_reqs, int longest, const int32_t* pages,
                               const EvictPage* items, int64_t n_items, const CacheF8& cache,
                               int32_t* kept, int nkv, int d, hipStream_t stream);
+// The same with the metadata in meta (reqs, pages and items are offsets there) and
+// longest at most kSmallEvict.
+constexpr int kSmallEvict = 4096;
+hipError_t launch_small_evict_f8(const EvictReq* reqs, int n_reqs, const int32_t* pages,
+                                 const EvictPage* items, int64_t n_items, const InlineMeta& meta,
+                                 const CacheF8& cache, int32_t* kept, int nkv, int d,
+                                 hipStream_t stream);
 
 // Copies `bytes` (a multiple of 16, both ends 16-byte aligned) from pinned host
 // memory, given by its device mapping, into device memory.  A kernel on the

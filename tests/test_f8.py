@@ -196,31 +196,44 @@ def test_workspace_bound_covers_batches(track):
 
 
 def test_launches(fake_hip):  # noqa: F811
-    """The kernels of each call, and staging buffers that outlive their readers."""
+    """The kernels of each call, small ones (whose metadata goes with the kernel's arguments) and
+    others, and staging buffers that outlive their readers."""
     r = run(fake_hip, """
         import ctypes
         s = mx.attn_shape(8, 2, 128, 1 << 20)
         c = lambda w: ctypes.byref(mx._CacheF8(1 << 20, 2 << 20, 3 << 20, 4 << 20, w))
-        calls = {
-            "append": lambda st: mx.lib().mx_kv_append_f8(batch(3, 20).ptr, ctypes.byref(s), A(0), A(1), c(None), st),
-            "attn": lambda st: mx.lib().mx_paged_attn_f8(batch(3, 20).ptr, ctypes.byref(s), A(0), c(None), A(1), A(2), BIG, st),
-            "track": lambda st: mx.lib().mx_paged_attn_f8(batch(3, 20).ptr, ctypes.byref(s), A(0), c(5 << 20), A(1), A(2), BIG, st),
-        }
-        e = mx.EvictBatch([40, 3], [20, 0], [4, 0], [[1, 2, 3], [4]], [[5, 6], []])
-        calls["evict"] = lambda st: mx.lib().mx_kv_evict_f8(2, e.ptr, ctypes.byref(s), c(5 << 20), A(0), A(2), BIG, st)
+        L, S = mx.lib(), ctypes.byref(s)
+        append = lambda b: lambda st: L.mx_kv_append_f8(b.ptr, S, A(0), A(1), c(None), st)
+        attn = lambda b, w: lambda st: L.mx_paged_attn_f8(b.ptr, S, A(0), c(w), A(1), A(2), BIG, st)
+        def evict(n, keep):
+            e = mx.EvictBatch([n, 3], [keep, 0], [4, 0], [np.arange(-(-n // 16)), [1 << 15]],
+                              [np.arange(1 << 16, (1 << 16) + -(-keep // 16)), []])
+            return lambda st: L.mx_kv_evict_f8(2, e.ptr, S, c(5 << 20), A(0), A(2), BIG, st)
+        long = mx.Batch([1], [1], [5000], [np.arange(400)])  # split over keys
+        calls = dict(append=append(batch(3, 20)), append_many=append(batch(300, 20)),
+                     attn=attn(batch(3, 20), None), attn_many=attn(batch(60, 20), None),
+                     attn_split=attn(long, None), track=attn(batch(3, 20), 5 << 20),
+                     track_decodes=attn(long, 5 << 20),
+                     evict=evict(40, 20), evict_long=evict(16000, 5000))
         kernels, st = {}, []
         for name, f in calls.items():
             n = len(log())
             st.append(f(None))
             kernels[name] = [l[0] for l in log()[n:]]
-        for i in range(60):
+        for i in range(40):
             st += [f([None, None, A(30), None, A(31)][i % 5]) for f in calls.values()]
         print(json.dumps(dict(kernels=kernels, st=st, bad=fake.fake_violations())))
         """)
     assert set(r["st"]) == {0} and r["bad"] == 0
-    got = {k: [next(n for n in ("upload", "kv_append_f8", "paged_attn_f8", "weight_decode",
-                                "weight_prefill", "weight_parts", "evict_select", "evict_move") if n in x)
-               for x in v] for k, v in r["kernels"].items()}
-    assert got == {"append": ["kv_append_f8"], "attn": ["upload", "paged_attn_f8"],
-                   "track": ["upload", "paged_attn_f8", "weight_decode", "weight_prefill", "weight_parts"],
-                   "evict": ["upload", "evict_select", "evict_move"]}
+    names = ("upload", "small_append_f8", "kv_append_f8", "small_attn_f8", "paged_attn_f8", "attn_merge",
+             "decode_attn_f8", "weight_decode", "weight_prefill", "weight_parts", "small_evict_select",
+             "small_evict_move", "evict_select", "evict_move")
+    got = {k: [next(n for n in names if n in x) for x in v] for k, v in r["kernels"].items()}
+    assert got == {
+        "append": ["small_append_f8"], "append_many": ["kv_append_f8"],
+        "attn": ["small_attn_f8"], "attn_many": ["upload", "paged_attn_f8"],
+        "attn_split": ["upload", "decode_attn_f8", "attn_merge"],
+        "track": ["upload", "paged_attn_f8", "weight_decode", "weight_prefill", "weight_parts"],
+        "track_decodes": ["upload", "decode_attn_f8", "weight_decode"],
+        "evict": ["small_evict_select", "small_evict_move"],
+        "evict_long": ["upload", "evict_select", "evict_move"]}
