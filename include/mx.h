@@ -263,8 +263,9 @@ mx_status mx_layer_step(const mx_batch* batch, const mx_layer_cfg* cfg, const vo
  * is the attention weight that each cached token has received so far (below); with
  * weight == NULL nothing is accumulated and nothing can be evicted by it.
  *
- * The calls below read host staging buffers like all others of this library, and
- * refuse a stream that is being captured into a graph (MX_ERR_UNSUPPORTED).
+ * The calls below read host staging buffers like all others of this library (small
+ * ones excepted, whose metadata goes with the kernel's arguments), and all refuse a
+ * stream that is being captured into a graph (MX_ERR_UNSUPPORTED).
  */
 typedef struct {
   uint8_t *k_pool, *v_pool;
@@ -377,10 +378,11 @@ mx_status mx_debug_gather(const mx_batch* batch, const mx_attn_shape* shape, int
                           uint16_t* v_out, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Launch timing, for profiling.  When enabled, every kernel launch of
- * mx_layer_step and mx_paged_attn is bracketed by two hipEvents recorded on the
+ * mx_layer_step and mx_paged_attn (and those of mx_paged_attn_f8 together, of
+ * mx_kv_evict_f8 together) is bracketed by two hipEvents recorded on the
  * caller's stream (the launch's own stream), tagged with the step it performs
  * ("token_map+rmsnorm_1", "gemm_qkv", "paged_attn", "gemm_o", "rmsnorm_2",
- * "gemm_gate_up", "gemm_down"; a tag covers a split-K GEMM's reduce, the
+ * "gemm_gate_up", "gemm_down", "paged_attn_f8", "kv_evict_f8"; a tag covers a split-K GEMM's reduce, the
  * launches of a GEMM whose rows run as two parts, and the attention's split
  * merge, except that when rows of the output projection are split over K their
  * reduce runs fused with the second RMSNorm, timed as "o_reduce+rmsnorm_2"

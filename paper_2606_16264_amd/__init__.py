@@ -193,6 +193,9 @@ class CacheF8:
                 raise ValueError(f"{name} must be contiguous, {size} byte(s) per element")
         heads, d = tuple(k_scale.shape), v_pool.shape[2]  # (pages, KV heads), head_dim
         self._dims = heads + (d,)
+        self._device = k_pool.device.index  # None: not on a GPU
+        if any(t is not None and t.device != k_pool.device for t in (v_pool, k_scale, v_scale, weight)):
+            raise ValueError("the cache's tensors are on different devices")
         for name, t, shape in (("k_pool", k_pool, heads + (d // 64, 16, 64)),
                                ("v_pool", v_pool, heads + (d, 16)), ("v_scale", v_scale, heads),
                                ("weight", weight, heads + (16,))):
@@ -206,6 +209,10 @@ class CacheF8:
         """The C struct, for calls of `shape`."""
         if self._dims != (shape.pool_pages, shape.n_kv_heads, shape.head_dim):
             raise ValueError("the cache is not of this attention shape")
+        if self._device is not None:
+            import torch
+            if self._device != torch.cuda.current_device():
+                raise ValueError(f"the cache is on device {self._device}, not the current one")
         return ctypes.byref(self._cache)
 
 
@@ -246,6 +253,12 @@ def layer_cfg(hidden, ffn, n_q_heads, n_kv_heads, head_dim, pool_pages, rms_eps=
 
 def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+def _holds(n: int, **tensors) -> None:
+    for name, t in tensors.items():
+        if t.numel() < n:
+            raise ValueError(f"{name} has {t.numel()} elements, the call needs {n}")
 
 
 def _stream(stream) -> Optional[int]:
@@ -333,6 +346,7 @@ def mx_layer_step(batch: Batch, cfg: LayerCfg, packed, x, y, k_pool, v_pool, ws,
 def mx_kv_append_f8(batch: Batch, shape: AttnShape, k_new, v_new, cache: CacheF8,
                     stream=None) -> None:
     """The new tokens' keys and values into the 8-bit cache."""
+    _holds(batch.T * shape.n_kv_heads * shape.head_dim, k_new=k_new, v_new=v_new)
     _check(_lib.mx_kv_append_f8(batch.ptr, ctypes.byref(shape), _ptr(k_new), _ptr(v_new),
                                 cache.ptr(shape), _stream(stream)))
 
@@ -356,6 +370,7 @@ def mx_workspace_bytes_f8(shape: AttnShape, track: bool, max_tokens: int, max_re
 def mx_paged_attn_f8(batch: Batch, shape: AttnShape, q, cache: CacheF8, out, ws,
                      stream=None) -> None:
     """Attention over the 8-bit cache; adds to cache.weight where it has one."""
+    _holds(batch.T * shape.n_q_heads * shape.head_dim, q=q, out=out)
     _check(_lib.mx_paged_attn_f8(batch.ptr, ctypes.byref(shape), _ptr(q), cache.ptr(shape), _ptr(out),
                                  _ptr(ws), ws.numel(), _stream(stream)))
 
@@ -371,6 +386,7 @@ def mx_kv_evict_f8(batch: EvictBatch, shape: AttnShape, cache: CacheF8, kept, ws
                    stream=None) -> None:
     """Copies the tokens that stay to the destination pages; kept (int32, n_kv_heads *
     batch.total_keep elements) receives their indices."""
+    _holds(shape.n_kv_heads * batch.total_keep, kept=kept)
     _check(_lib.mx_kv_evict_f8(batch.R, batch.ptr, ctypes.byref(shape), cache.ptr(shape), _ptr(kept),
                                _ptr(ws), ws.numel(), _stream(stream)))
 

@@ -178,6 +178,17 @@ def test_binding_checks_the_cache():
         mx.CacheF8(c.k_pool, c.v_pool, c.k_scale, c.v_scale, c.weight[:, :1].contiguous())
 
 
+def test_binding_checks_sizes():
+    s = shape()
+    c, small, b = cache(s), Raw(n=4 * 2 * 64 - 1), one()
+    with pytest.raises(ValueError, match="v_new"):
+        mx.mx_kv_append_f8(b, s, Raw(), small, c, stream=0)
+    with pytest.raises(ValueError, match="out"):
+        mx.mx_paged_attn_f8(b, s, Raw(), c, Raw(n=4 * 4 * 64 - 1), Raw(), stream=0)
+    with pytest.raises(ValueError, match="kept"):
+        mx.mx_kv_evict_f8(mx.EvictBatch([4], [2], [1], [[1]], [[2]]), s, c, Raw(n=3), Raw(), stream=0)
+
+
 @pytest.mark.parametrize("track", [False, True])
 def test_workspace_bound_covers_batches(track):
     rng = np.random.default_rng(5)

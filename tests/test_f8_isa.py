@@ -20,8 +20,8 @@ def asm(tmp_path_factory):
 
 
 def test_no_lds_read_hazard(asm):
-    res = {k: v for k, v in check(asm).items() if "paged_attn_f8_kernel" in k}
-    assert len(res) == 4, sorted(res)  # two head dims, with and without weights
+    res = {k: v for k, v in check(asm).items() if re.search("(paged|small)_attn_f8_kernel", k)}
+    assert len(res) == 6, sorted(res)  # two head dims: with weights, without, small calls
     bad = {k: v[:3] for k, v in res.items() if v}
     assert not bad, bad
 
@@ -40,7 +40,7 @@ def test_copies_alone_use_m0(asm):
 def test_no_spills_in_the_prefill_tiles(asm):
     """A spilled register's reload is a vector-memory load: it would count among the copies, whose
     waits are placed by hand."""
-    meta = re.findall(r"\.name:\s+(\S*paged_attn_f8_kernel\S*)\n(.*?)\.wavefront_size", asm, re.S)
-    assert len(meta) == 4
+    meta = re.findall(r"\.name:\s+(\S*(?:paged|small)_attn_f8_kernel\S*)\n(.*?)\.wavefront_size", asm, re.S)
+    assert len(meta) == 6
     for name, body in meta:
         assert re.search(r"\.private_segment_fixed_size:\s+0\b", body), name

@@ -323,6 +323,52 @@ def test_attention_late_chunk():
     check_weights(c, c.hw, reqs, weights, worst)
 
 
+def test_chunk_weights_without_parts():
+    """Keys and KV heads enough that a chunk's rows are not split, causal edges inside."""
+    c, reqs, q = make_case(32, 32, 64, [(0, 300, 4001), (0, 33, 0)], 14, True)
+    out, mag, weights, worst = attend_ref(c, 32, reqs, q.double().numpy())
+    got, _ = run_attn(c, 32, reqs, q.cuda())
+    check_out(got, out, mag)
+    check_weights(c, c.hw, reqs, weights, worst)
+
+
+def test_small_calls_give_what_large_ones_give():
+    """The same requests in one call, whose metadata is staged, and one by one, where it goes with
+    the kernel's arguments: append, attention and eviction, bit for bit."""
+    rng = np.random.default_rng(30)
+    R, nq, nkv, d = 250, 8, 2, 128
+    ctx = rng.integers(1, 300, R)
+    pages = int((-(-(ctx + 1) // 16)).sum() + (-(-ctx // 2 // 16)).sum()) + 300
+    tabs = tables(rng, pages, list(ctx + 1) + list(np.maximum(ctx // 2, 1)))
+    kv = bf16(rng.normal(0, 1, (2, R, nkv, d))).cuda()
+    q = bf16(rng.normal(0, 1, (R, nq, d))).cuda()
+    reqs = [(1, 1, int(n), t) for n, t in zip(ctx, tabs)]
+    ev = [(int(n), max(int(n) // 2, 1), min(3, max(int(n) // 2, 1)), tabs[r], tabs[R + r])
+          for r, n in enumerate(ctx)]
+    got = []
+    for one_by_one in (False, True):
+        c = Cache(pages, nkv, d, poison=False)
+        r2 = np.random.default_rng(31)
+        for t, n in zip(tabs, ctx):
+            fill(c, r2, t, int(n))
+        c.upload()
+        s = c.shape(nq)
+        plain = mx.CacheF8(c.k, c.v, c.ks, c.vs)
+        out = torch.zeros(R, nq, d, dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+        kept = []
+        for part in ([[r] for r in range(R)] if one_by_one else [list(range(R))]):
+            lo, hi = part[0], part[-1] + 1
+            b = batch_of([reqs[r] for r in part])
+            k, v = kv[0, lo:hi].contiguous(), kv[1, lo:hi].contiguous()
+            mx.mx_kv_append_f8(b, s, k, v, c.mx)
+            mx.mx_paged_attn_f8(b, s, q[lo:hi], plain, out[lo:hi], ws)
+            kept.append(run_evict(c, [ev[r] for r in part])[0][:-8])
+        got.append((out, torch.cat(kept), c.k, c.v, c.ks, c.vs, c.w))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert got[0][0].float().abs().min(-1).values.max() > 0
+
+
 def test_attention_scales_far_apart():
     """Pages whose scales differ by up to 2^40, values that no common scale could hold."""
     c, reqs, q = make_case(8, 2, 128, [(1, 1, 700), (0, 90, 200)], 5, False, spread=20)
@@ -458,8 +504,10 @@ def test_evict_ties_and_odd_weights(name, weights):
     check_evict(*evict_case(2, 64, [300, 1500, 2048], [100, 700, 1030], [10, 0, 1], 9, weights))
 
 
-def test_evict_long():
-    check_evict(*evict_case(1, 64, [40001], [12345], [300], 10))
+@pytest.mark.parametrize("n,keep,recent", [(40001, 12345, 300), (20000, 19999, 1), (4097, 5, 0),
+                                           (32769, 1, 1)])
+def test_evict_long(n, keep, recent):
+    check_evict(*evict_case(1, 64, [n], [keep], [recent], 10))
 
 
 def test_evict_keeps_nothing_or_everything():
