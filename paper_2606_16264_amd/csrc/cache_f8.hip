@@ -222,9 +222,10 @@ __global__ __launch_bounds__(256) void small_append_f8_kernel(SmallAppend a) {
 }
 
 // ---------------------------------------------------------------- eviction
-// An order-preserving map of fp32 weights to unsigned integers (-0 as 0).
+// An order-preserving map of fp32 weights to unsigned integers: -0 as 0, every NaN, of
+// either sign, as the largest.
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  const uint32_t b = w == 0.f ? 0u : __float_as_uint(w);
+  const uint32_t b = w == 0.f ? 0u : w != w ? 0x7FFFFFFFu : __float_as_uint(w);
   return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
@@ -387,10 +388,10 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(const Evic
 }
 
 // Copies the kept tokens of one destination page and KV head, a wave each.  The page's
-// scale is the largest of those its tokens come from.  Bound by memory: 108 us for 8192
-// tokens of 16 requests, 8 heads, 550 MB (200 written; keys are 64-byte runs, and of a
-// value page that holds one kept token all lines are read, since a token's values lie
-// 16 bytes apart).  Values: the tokens of a destination page come from source
+// scale is the largest of those its tokens come from.  Bound by memory: 108 us for up to
+// 8192 tokens each of 16 requests, 8 heads, 623 MB (190 written; keys are 64-byte runs,
+// and of a value page that holds one kept token all lines are read, since a token's
+// values lie 16 bytes apart).  Values: the tokens of a destination page come from source
 // pages in ascending order; of each such page a lane reads its rows as 16-byte words
 // and takes the bytes it needs with byte permutes whose selectors are the same in all
 // lanes (as loads of single bytes: 177 us).

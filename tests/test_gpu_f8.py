@@ -504,6 +504,18 @@ def test_evict_ties_and_odd_weights(name, weights):
     check_evict(*evict_case(2, 64, [300, 1500, 2048], [100, 700, 1030], [10, 0, 1], 9, weights))
 
 
+def test_evict_any_nan_counts_as_the_largest():
+    """NaNs of either sign and any payload: above infinity, equal among themselves."""
+    c, reqs = evict_case(2, 64, [300, 1500, 5000], [100, 700, 1030], [10, 0, 1], 13,
+                         lambda rng, j: [math.inf, math.nan, 1.0, -math.inf][rng.integers(0, 4)])
+    bits = torch.tensor([0x7FC00000, 0x7F800001, 0x7FFFFFFF, -0x00400000, -0x007FFFFF, -1],
+                        dtype=torch.int32, device="cuda")
+    w = c.w.view(torch.int32).flatten()
+    w[:] = torch.where(c.w.flatten().isnan(), bits[torch.arange(w.numel(), device="cuda") % 6], w)
+    assert (c.w.cpu().isnan() == torch.from_numpy(c.hw).isnan()).all()
+    check_evict(c, reqs)
+
+
 @pytest.mark.parametrize("n,keep,recent", [(40001, 12345, 300), (20000, 19999, 1), (4097, 5, 0),
                                            (32769, 1, 1)])
 def test_evict_long(n, keep, recent):
