@@ -300,7 +300,8 @@ mx_status mx_kv_append_f8(const mx_batch* batch, const mx_attn_shape* shape,
  *                           p[t][h][j].
  * Sums are in fp32.  A page that several requests of the batch share receives the sum
  * over all of them (in no fixed order; every other weight, and every output, is the
- * same from run to run).  Sizes of the workspace: mx_workspace_bytes_f8_for, with
+ * same from run to run).  A NaN value reaches the rows that attend to its token, and no
+ * earlier row of its chunk.  Sizes of the workspace: mx_workspace_bytes_f8_for, with
  * track != 0 where cache->weight is given (it holds the decodes' scores then); its
  * upper bound for any batch of at most max_tokens new tokens, max_reqs requests and
  * max_pages page-table entries in total: mx_workspace_bytes_f8.

@@ -366,6 +366,37 @@ __device__ __forceinline__ void decode_item(const AttnF8Params& p, const AttnIte
   }
 }
 
+// The top bits of the bytes that hold a NaN (a code of magnitude 0x7F).
+__device__ __forceinline__ u32x4 nan_codes(const u32x4& w) {
+  u32x4 x;
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = ((w[i] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+  return x;
+}
+// Where rows see some of the keys only and a value is NaN, a probability of 0 would not
+// keep it out of their products.  So it is taken out there (by the caller), and what it
+// belongs in is found by a product of its own, of the NaNs' places with the keys that the
+// lane's row sees (its page's tokens 0 .. last).  The search costs a fresh prompt of 512
+// tokens of the 8B heads 0.8 us of 17, one of 2048 1 of 58 (a branch for two blocks at
+// a time: no less, and 15 registers spilled where weights are accumulated).
+__device__ __forceinline__ void nan_values(const u32x4& nan, int last, f32x4& o) {
+  f32x4 seen = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    uint32_t row[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      const int tok = 8 * i + 2 * e;
+      row[e] = (tok <= last ? 0x3F80u : 0u) | (tok < last ? 0x3F800000u : 0u);
+    }
+    // (0x38: the code of 1.0)
+    seen = mfma16(widen((nan[2 * i] >> 7) * 0x38u, (nan[2 * i + 1] >> 7) * 0x38u, 1.f),
+                  as_bf16x8(u32x4{row[0], row[1], row[2], row[3]}), seen);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; e++) o[e] = seen[e] > 0.f ? __builtin_nanf("") : o[e];
+}
+
 // A prefill tile's query rows as the B operand of the score products.
 //
 // Where no weights are accumulated the products take the key codes as they are, with the
@@ -680,6 +711,14 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
         if constexpr (MASK) {
 #pragma unroll
           for (int i = 0; i < 4; i++) w[i] &= keep[i];
+          const u32x4 nan = nan_codes(w);
+          if (__any(((nan[0] | nan[1]) | (nan[2] | nan[3])) != 0)) {
+            const int key = (4 * c + g4) * 16;
+            nan_values(nan, row_pos - key, o[B * Q + e]);
+            nan_values(nan, row_pos2 - key, o2[B * Q + e]);
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] &= ~((nan[i] >> 7) * 0xFFu);
+          }
         }
 #pragma unroll
         for (int i = 0; i < 2; i++) {

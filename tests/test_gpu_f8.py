@@ -406,6 +406,28 @@ def test_nan_stays_in_its_rows():
     assert (np.isnan(got) == bad).all()
 
 
+@pytest.mark.parametrize("weight", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_nan_values_of_later_tokens(d, weight):
+    """A NaN value of a chunk's token leaves the chunk's earlier rows as they are without it,
+    and makes that dim of the token's own row and of all later ones NaN."""
+    at = [(0, 0, 0, 3), (0, 37, 1, 0), (0, 130, 1, d - 1), (1, 63, 0, 17), (1, 64, 1, 40), (2, 2, 0, 1)]
+    c, reqs, q = make_case(8, 2, d, [(False, 150, 0), (False, 65, 50), (False, 3, 8)], 23, weight)
+    start = np.cumsum([0] + [r[1] for r in reqs])
+    exp, mag, weights, worst = attend_ref(c, 8, reqs, q.double().numpy())
+    bad = np.zeros(exp.shape, bool)
+    for r, row, g, e in at:
+        _, n, ctx, table = reqs[r]
+        c.hv[table[(ctx + row) // 16], g, (ctx + row) % 16, e] = NAN if row % 2 else 0xFF
+        bad[start[r] + row:start[r] + n, 4 * g:4 * g + 4, e] = True
+    c.upload()
+    got = run_attn(c, 8, reqs, q.cuda())[0].cpu()
+    assert (got.isnan().numpy() == bad).all()
+    check_out(got.masked_fill(torch.from_numpy(bad), 0), np.where(bad, 0, exp), mag)
+    if weight:
+        check_weights(c, c.hw, reqs, weights, worst)
+
+
 def test_shared_prefix_weights_add_up():
     """Requests that read the same cached pages: each key receives the sum over all of them."""
     c, reqs, q = make_case(8, 2, 64, [(1, 1, 90), (0, 33, 64)], 7, True)
