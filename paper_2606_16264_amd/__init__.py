@@ -194,6 +194,10 @@ class CacheF8:
         heads, d = tuple(k_scale.shape), v_pool.shape[2]  # (pages, KV heads), head_dim
         self._dims = heads + (d,)
         self._device = k_pool.device.index  # None: not on a GPU
+        if self._device is not None:
+            import torch
+            self._current_device = torch.cuda.current_device
+            self._current_stream = torch._C._cuda_getCurrentRawStream
         if any(t is not None and t.device != k_pool.device for t in (v_pool, k_scale, v_scale, weight)):
             raise ValueError("the cache's tensors are on different devices")
         for name, t, shape in (("k_pool", k_pool, heads + (d // 64, 16, 64)),
@@ -205,14 +209,17 @@ class CacheF8:
         self.weight = weight
         self._cache = _CacheF8(*(_ptr(t) for t in (k_pool, v_pool, k_scale, v_scale, weight)))
 
+    def stream(self, stream):
+        """The handle of a stream, by default the current one of the cache's device."""
+        return _stream(stream) if self._device is None or stream is not None \
+            else self._current_stream(self._device)
+
     def ptr(self, shape: AttnShape):
         """The C struct, for calls of `shape`."""
         if self._dims != (shape.pool_pages, shape.n_kv_heads, shape.head_dim):
             raise ValueError("the cache is not of this attention shape")
-        if self._device is not None:
-            import torch
-            if self._device != torch.cuda.current_device():
-                raise ValueError(f"the cache is on device {self._device}, not the current one")
+        if self._device is not None and self._device != self._current_device():
+            raise ValueError(f"the cache is on device {self._device}, not the current one")
         return ctypes.byref(self._cache)
 
 
@@ -255,10 +262,14 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _holds(n: int, **tensors) -> None:
-    for name, t in tensors.items():
-        if t.numel() < n:
-            raise ValueError(f"{name} has {t.numel()} elements, the call needs {n}")
+def _check_tensor(cache: CacheF8, name: str, t, n: int, size: int) -> None:
+    """t has n elements; where the cache is on a GPU, of `size` bytes each, on that GPU, in order."""
+    if t.numel() < n:
+        raise ValueError(f"{name} has {t.numel()} elements, the call needs {n}")
+    device = cache._device
+    if device is not None and (t.get_device() != device or t.element_size() != size
+                               or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous, {size} byte(s) per element, on device {device}")
 
 
 def _stream(stream) -> Optional[int]:
@@ -346,9 +357,11 @@ def mx_layer_step(batch: Batch, cfg: LayerCfg, packed, x, y, k_pool, v_pool, ws,
 def mx_kv_append_f8(batch: Batch, shape: AttnShape, k_new, v_new, cache: CacheF8,
                     stream=None) -> None:
     """The new tokens' keys and values into the 8-bit cache."""
-    _holds(batch.T * shape.n_kv_heads * shape.head_dim, k_new=k_new, v_new=v_new)
+    n = batch.T * shape.n_kv_heads * shape.head_dim
+    _check_tensor(cache, "k_new", k_new, n, 2)
+    _check_tensor(cache, "v_new", v_new, n, 2)
     _check(_lib.mx_kv_append_f8(batch.ptr, ctypes.byref(shape), _ptr(k_new), _ptr(v_new),
-                                cache.ptr(shape), _stream(stream)))
+                                cache.ptr(shape), cache.stream(stream)))
 
 
 def mx_workspace_bytes_f8_for(batch: Batch, shape: AttnShape, track: bool = False) -> int:
@@ -370,9 +383,12 @@ def mx_workspace_bytes_f8(shape: AttnShape, track: bool, max_tokens: int, max_re
 def mx_paged_attn_f8(batch: Batch, shape: AttnShape, q, cache: CacheF8, out, ws,
                      stream=None) -> None:
     """Attention over the 8-bit cache; adds to cache.weight where it has one."""
-    _holds(batch.T * shape.n_q_heads * shape.head_dim, q=q, out=out)
+    n = batch.T * shape.n_q_heads * shape.head_dim
+    _check_tensor(cache, "q", q, n, 2)
+    _check_tensor(cache, "out", out, n, 2)
+    _check_tensor(cache, "ws", ws, 0, 1)
     _check(_lib.mx_paged_attn_f8(batch.ptr, ctypes.byref(shape), _ptr(q), cache.ptr(shape), _ptr(out),
-                                 _ptr(ws), ws.numel(), _stream(stream)))
+                                 _ptr(ws), ws.numel(), cache.stream(stream)))
 
 
 def mx_kv_evict_f8_ws_bytes(batch: EvictBatch, shape: AttnShape) -> int:
@@ -386,9 +402,10 @@ def mx_kv_evict_f8(batch: EvictBatch, shape: AttnShape, cache: CacheF8, kept, ws
                    stream=None) -> None:
     """Copies the tokens that stay to the destination pages; kept (int32, n_kv_heads *
     batch.total_keep elements) receives their indices."""
-    _holds(shape.n_kv_heads * batch.total_keep, kept=kept)
+    _check_tensor(cache, "kept", kept, shape.n_kv_heads * batch.total_keep, 4)
+    _check_tensor(cache, "ws", ws, 0, 1)
     _check(_lib.mx_kv_evict_f8(batch.R, batch.ptr, ctypes.byref(shape), cache.ptr(shape), _ptr(kept),
-                               _ptr(ws), ws.numel(), _stream(stream)))
+                               _ptr(ws), ws.numel(), cache.stream(stream)))
 
 
 def mx_layer_workspace_offsets(batch: Batch, cfg: LayerCfg) -> dict:

@@ -656,6 +656,30 @@ def test_captured_streams_are_refused():
     assert torch.equal(run_attn(c, 4, reqs, q)[0], out)
 
 
+def test_binding_refuses_other_tensors():
+    """Strided, of another type, or not on the cache's device: refused before anything runs."""
+    c, reqs, q = make_case(4, 2, 64, [(0, 5, 3)], 30, True)
+    b, s, q = batch_of(reqs), c.shape(4), q.cuda()
+    kv = torch.zeros(5, 2, 64, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(mx.mx_workspace_bytes_f8_for(b, s, True), dtype=torch.uint8, device="cuda")
+    e = mx.EvictBatch([8], [4], [1], [reqs[0][3]], [[p for p in range(c.pages) if p not in reqs[0][3]][:1]])
+    kept = torch.zeros(2 * 4, dtype=torch.int32, device="cuda")
+    for bad in (lambda t: torch.zeros(t.shape + (2,), dtype=t.dtype, device="cuda")[..., 0],
+                lambda t: t.to(torch.float64), lambda t: t.cpu()):
+        for args in ((bad(kv), kv), (kv, bad(kv))):
+            with pytest.raises(ValueError):
+                mx.mx_kv_append_f8(b, s, *args, c.mx)
+        for i in range(3):
+            t = [q, q.clone(), ws]
+            t[i] = bad(t[i])
+            with pytest.raises(ValueError):
+                mx.mx_paged_attn_f8(b, s, t[0], c.mx, t[1], t[2])
+        for args in ((bad(kept), ws), (kept, bad(ws))):
+            with pytest.raises(ValueError):
+                mx.mx_kv_evict_f8(e, s, c.mx, *args)
+    c.check("refused")
+
+
 def test_pages_beyond_4_gib():
     """Pages whose byte offsets pass 2^32 in every pool, against the same requests in low pages."""
     nq, nkv, d = 16, 8, 128
