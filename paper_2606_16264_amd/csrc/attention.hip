@@ -715,18 +715,15 @@ hipError_t launch_paged_attn(const AttnParams& p, int n_items, const MergeItem* 
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  return launch_attn_merge(p, merges, n_merges, head_dim, stream);
-}
-
-hipError_t launch_attn_merge(const AttnParams& p, const MergeItem* merges, int n_merges,
-                             int head_dim, hipStream_t stream) {
-  if (n_merges == 0) return hipSuccess;
-  dim3 grid(n_merges, p.nq);
-  if (head_dim == 128)
-    attn_merge_kernel<128><<<grid, kMergeThreads, 0, stream>>>(p, merges);
-  else
-    attn_merge_kernel<64><<<grid, kMergeThreads, 0, stream>>>(p, merges);
-  return hipGetLastError();
+  if (n_merges > 0) {
+    dim3 grid(n_merges, p.nq);
+    if (head_dim == 128)
+      attn_merge_kernel<128><<<grid, kMergeThreads, 0, stream>>>(p, merges);
+    else
+      attn_merge_kernel<64><<<grid, kMergeThreads, 0, stream>>>(p, merges);
+    return hipGetLastError();
+  }
+  return hipSuccess;
 }
 
 }  // namespace mx

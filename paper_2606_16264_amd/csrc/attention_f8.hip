@@ -524,8 +524,13 @@ __device__ __forceinline__ void lds_write8(unsigned addr, u32x2 v) {
 }
 __device__ __forceinline__ void pin1(uint32_t& x) { asm volatile("" : "+v"(x)); }
 
-// Prefill item: one q head, rows it.start .. it.start + 127 of the chunk; wave w owns
-// two blocks of 16 consecutive rows, it.start + 32 w + (0 | 16) + col.
+// Prefill item: rows it.start .. it.start + 127 of `pack` q heads of one KV head (a power
+// of two), row r being q head it.head + r % pack and new token r / pack, so that heads
+// which share their keys share a tile; wave w owns two blocks of 16 consecutive rows,
+// it.start + 32 w + (0 | 16) + col.  With few tiles over long contexts each is split over
+// its keys (choose_tiles): a split takes its chunks as a tile of a shorter request, whose
+// positions count from its first key, and leaves unnormalised rows, their maxima and
+// sums for merge_tile.
 //
 // Iteration kt of the chunk loop reads the keys of chunk kt + 1 for the score products
 // while the exponentials of chunk kt (whose scores the previous iteration left) run on
@@ -548,37 +553,56 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15;  // query row of this lane within each block
   const int g4 = lane >> 4;   // lane group
-  const int qhead = it.head;
-  const int kvh = qhead / p.a.group;
-  const int row0 = it.start + 32 * wave;
-  const int row = row0 + col, row2 = row0 + 16 + col;
-  const bool row_valid = row < rq.n_new, row_valid2 = row2 < rq.n_new;
-  const int rowc = row_valid ? row : rq.n_new - 1;
-  const int rowc2 = row_valid2 ? row2 : rq.n_new - 1;
-  const int64_t qtok = rq.tok_start + rowc, qtok2 = rq.tok_start + rowc2;
-  const int row_pos = rq.ctx_len + rowc, row_pos2 = rq.ctx_len + rowc2;
-  const int last_row = min(row0 + 31, rq.n_new - 1);
-  const int page_end = row0 < rq.n_new ? (rq.ctx_len + last_row) / 16 + 1 : 0;
+  const int kvh = it.head / p.a.group, shift = p.pack_log2, rows = rq.n_new << shift;
+  const int n_split = it.nrows, split = it.start % kPrefillTileRows, start = it.start - split;
+  const int row0 = start + 32 * wave;
+  // the split's chunks: `per` each, as split_tile of the host has it
+  int ctx_len = rq.ctx_len, kv_len = rq.kv_len, first_page = 0, most_pages = rq.n_pages;
+  if (n_split > 1) {
+    const int chunks = (ctx_len + (start >> shift)) / 64 + 1;
+    const int per = (chunks + n_split - 1) / n_split;
+    ctx_len -= 64 * per * split;
+    kv_len -= 64 * per * split;
+    first_page = 4 * per * split;
+    if (split < n_split - 1) most_pages = 4 * per;
+  }
+  struct Row {
+    int token, head;  // of the chunk's new tokens; q head
+    bool valid;
+  };
+  auto row_at = [&](int r) {
+    const int rc = min(r, rows - 1), token = rc >> shift;
+    return Row{token, it.head + rc - (token << shift), r < rows};
+  };
+  auto pages_to = [&](int r) {  // that row r, or the last one, sees
+    return min((ctx_len + (min(r, rows - 1) >> shift)) / 16 + 1, most_pages);
+  };
+  const int page_end = row0 < rows ? pages_to(row0 + 31) : 0;
   const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
 
   std::conditional_t<TRACK, WideQuery<HD>, CodedQuery<HD>> qf, qf2;
-  qf.load(p, qtok, qhead, row_valid, g4);
-  qf2.load(p, qtok2, qhead, row_valid2, g4);
+  int row_pos, row_pos2;
+  {
+    const Row a = row_at(row0 + col), b = row_at(row0 + 16 + col);
+    qf.load(p, rq.tok_start + a.token, a.head, a.valid, g4);
+    qf2.load(p, rq.tok_start + b.token, b.head, b.valid, g4);
+    row_pos = ctx_len + a.token;
+    row_pos2 = ctx_len + b.token;
+  }
   RowState r1 = row_start(), r2 = row_start();
   f32x4 o[HD / 16], o2[HD / 16];
 #pragma unroll
   for (int db = 0; db < HD / 16; db++) o[db] = o2[db] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // the tile's last row bounds the pages every wave helps to copy
-  const int tile_last = min(it.start + kPrefillTileRows - 1, rq.n_new - 1);
-  const int item_pages = (rq.ctx_len + tile_last) / 16 + 1;
+  const int item_pages = pages_to(start + kPrefillTileRows - 1);
   const int n_chunks = (item_pages + 3) / 4;
   const int wave_chunks = (page_end + 3) / 4;  // 0 for a wave without valid rows
   // page ids and scales through the constant address space: uniform reads of tables
   // nothing writes during the launch, so they are scalar loads
   typedef const __attribute__((address_space(4))) int32_t* ConstInts;
   typedef const __attribute__((address_space(4))) float* ConstFloats;
-  const ConstInts ptab = (ConstInts)(p.a.pages + rq.page_start);
+  const ConstInts ptab = (ConstInts)(p.a.pages + rq.page_start + first_page);
   const ConstFloats k_scale = (ConstFloats)p.k_scale, v_scale = (ConstFloats)p.v_scale;
 
   // byte offsets in the page of this lane's share of a key copy (of 64 dims) and of a
@@ -699,7 +723,7 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
     lds_read_run<0, Q, OFF + 2 * Q * 256, 256>(va, v[2]);
     lds_read_run<0, Q, OFF + 3 * Q * 256, 256>(va, v[3]);
     uint32_t keep[4];
-    if constexpr (MASK) value_keep(4 * c + g4, page_end, rq.kv_len, keep);
+    if constexpr (MASK) value_keep(4 * c + g4, page_end, kv_len, keep);
     auto part = [&](auto b) {
       constexpr int B = decltype(b)::value;
       lgkm_wait<(3 - B) * Q>();
@@ -789,7 +813,7 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   vm_wait<2 * NLD>();
   lgkm_wait<0>();
   wg_barrier();
-  if (row0 >= rq.n_new) {
+  if (row0 >= rows) {
     // no rows here: this wave only copies its page of every chunk
     run(0, n_chunks, [](int) {});
     vm_wait<0>();  // no copy may land in LDS after the workgroup has ended
@@ -800,8 +824,8 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   // Chunks 0 .. n_int - 1 are inside every wave's range and at or before every row of
   // the tile: no masks.  The last chunk of the tile is the only one that can hold keys
   // past the request's end, so n_main <= n_chunks - 1.
-  const int first_pos = rq.ctx_len + it.start;
-  const int page_end0 = (rq.ctx_len + min(it.start + 31, rq.n_new - 1)) / 16 + 1;  // wave 0's
+  const int first_pos = ctx_len + (start >> shift);
+  const int page_end0 = pages_to(start + 31);  // wave 0's
   const int n_int = first_pos >= 63 ? min((first_pos - 63) / 64 + 1, page_end0 / 4) : 0;
   const int n_main = max(0, n_int - 1);
   auto step = [&](auto slot, int kt) {  // slot: kt % 4 or -1
@@ -846,9 +870,27 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   const float l1 = lane_groups_sum(r1.l), l2 = lane_groups_sum(r2.l);
   // dims 16 db + 4 g4 .. + 3 of the row: (db / 2) 32-column steps plus 16 (db % 2)
   const int64_t step32 = p.a.out_tiled ? 512 : 32;
-  auto store = [&](int64_t tok, float l, const RowState& r, const f32x4 (&acc)[HD / 16]) {
+  int end_col = threadIdx.x;  // (the rows once more: kept over the loop they cost registers)
+  asm volatile("" : "+v"(end_col));
+  end_col &= 15;
+  if (n_split > 1) {
+    auto leave = [&](int r, float l, const RowState& st, const f32x4 (&acc)[HD / 16]) {
+      if (row0 + r >= rows) return;
+      const int64_t part = (int64_t)it.part + 32 * wave + r;
+#pragma unroll
+      for (int db = 0; db < HD / 16; db++)
+        *reinterpret_cast<f32x4*>(p.a.part_o + part * HD + 16 * db + 4 * g4) = acc[db];
+      if (g4 == 0) *reinterpret_cast<float2*>(p.a.part_ml + 2 * part) = float2{st.m, l};
+    };
+    leave(end_col, l1, r1, o);
+    leave(16 + end_col, l2, r2, o2);
+    return;
+  }
+  auto store = [&](const Row& at, float l, const RowState& r, const f32x4 (&acc)[HD / 16]) {
+    if (!at.valid) return;
+    const int64_t tok = rq.tok_start + at.token;
     const float inv = 1.f / l;
-    uint16_t* op = out_ptr(p.a, tok, qhead * HD + 4 * g4);
+    uint16_t* op = out_ptr(p.a, tok, at.head * HD + 4 * g4);
 #pragma unroll
     for (int db = 0; db < HD / 16; db++) {
       u32x2 w;
@@ -856,10 +898,10 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
       w[1] = pack_bf16x2(acc[db][2] * inv, acc[db][3] * inv);
       *reinterpret_cast<u32x2*>(op + (db >> 1) * step32 + (db & 1) * 16) = w;
     }
-    if (TRACK && g4 == 0) p.lse[tok * p.a.nq + qhead] = r.m + log2f(l);
+    if (TRACK && g4 == 0) p.lse[tok * p.a.nq + at.head] = r.m + log2f(l);
   };
-  if (row_valid) store(qtok, l1, r1, o);
-  if (row_valid2) store(qtok2, l2, r2, o2);
+  store(row_at(row0 + end_col), l1, r1, o);
+  store(row_at(row0 + 16 + end_col), l2, r2, o2);
 }
 
 // Launches of decode splits alone run a kernel of their own: without the prefill
@@ -909,8 +951,46 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
 // and then several workgroups add to one token.
 __device__ __forceinline__ void add_weight(float* w, float x) { unsafeAtomicAdd(w, x); }
 
-// What follows the attention of decodes whose weights are accumulated, in one launch:
-// the merge of the key splits, and
+// Merges the splits of a prefill tile over its keys: HD / 4 threads a row, 8 (HD = 128) or
+// 16 rows of one unit a workgroup.  Bound by memory.
+template <int HD>
+constexpr int kMergeRows = 4 * kMergeThreads / HD;
+template <int HD>
+__device__ __forceinline__ void merge_tile(const AttnF8Params& p, const TileMerge* tiles, int index) {
+  constexpr int BLOCKS = kPrefillTileRows / kMergeRows<HD>;
+  const int shift = p.pack_log2, units = p.a.nq >> shift;
+  const TileMerge tm = tiles[index / BLOCKS / units];
+  const ReqDev rq = p.a.reqs[tm.req];
+  const int unit = index / BLOCKS % units;
+  const int r = index % BLOCKS * kMergeRows<HD> + threadIdx.x / (HD / 4), d = 4 * (threadIdx.x % (HD / 4));
+  const int row = tm.start + r;
+  if (row >= rq.n_new << shift) return;
+  const int64_t base = (int64_t)tm.part + unit * tm.n_split * kPrefillTileRows + r;
+  float m = kNegBig, l = 0.f;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < tm.n_split; s++) {
+    const int64_t at = base + s * kPrefillTileRows;
+    const float2 ml = *reinterpret_cast<const float2*>(p.a.part_ml + 2 * at);
+    const f32x4 o = *reinterpret_cast<const f32x4*>(p.a.part_o + at * HD + d);
+    const float mn = fmaxf(m, ml.x);
+    const float a = exp2f(m - mn), w = exp2f(ml.x - mn);
+    acc = acc * a + o * w;
+    l = l * a + ml.y * w;
+    m = mn;
+  }
+  const int64_t tok = rq.tok_start + (row >> shift);
+  const int head = (unit << shift) + (row & ((1 << shift) - 1));
+  const float inv = 1.f / l;
+  u32x2 w;
+  w[0] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  w[1] = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+  *reinterpret_cast<u32x2*>(out_ptr(p.a, tok, head * HD + d)) = w;
+  if (p.weight && d == 0) p.lse[tok * p.a.nq + head] = m + log2f(l);
+}
+
+// What follows the attention in one launch: the accumulation of decodes' weights, the
+// merge of decodes' key splits and that of prefill tiles'.  The first is
 //   weight[slot][g] += sum over the q heads h of group g of exp2(score - lse[h]),
 // the scores as the attention left them, lse from the splits' own maxima and sums
 // (which the merge combines to the same) or, unsplit, as the attention left it.
@@ -918,15 +998,16 @@ __device__ __forceinline__ void add_weight(float* w, float x) { unsafeAtomicAdd(
 // (four neighbouring keys per thread took 30 us for 64 requests of 300 to 8192 tokens
 // of the 8B heads, 10 this way).
 template <int HD>
-__global__ __launch_bounds__(kMergeThreads) void weight_decode_kernel(AttnF8Params p,
-                                                                      const WeightItem* items,
-                                                                      int n_weights,
-                                                                      const MergeItem* merges) {
+__global__ __launch_bounds__(kMergeThreads) void finish_kernel(AttnF8Params p,
+                                                               const WeightItem* items, int n_weights,
+                                                               const MergeItem* merges, int n_merges,
+                                                               const TileMerge* tiles) {
   __shared__ __attribute__((aligned(16))) float smem[merge_floats<HD>()];
   static_assert(kWeightDecodePages == 64 && kMergeThreads == 256, "four rounds of 256 keys");
   if ((int)blockIdx.x >= n_weights) {
     const int i = blockIdx.x - n_weights;
-    merge_splits<HD>(p.a, merges[i / p.a.nq], i % p.a.nq, smem);
+    if (i < n_merges) merge_splits<HD>(p.a, merges[i / p.a.nq], i % p.a.nq, smem);
+    else merge_tile<HD>(p, tiles, i - n_merges);
     return;
   }
   const WeightItem it = items[blockIdx.x / p.a.nkv];
@@ -1146,8 +1227,8 @@ __global__ __launch_bounds__(256) void weight_parts_kernel(AttnF8Params p, const
 
 template <int HD>
 hipError_t launch(const AttnF8Params& p, int n_items, const MergeItem* merges, int n_merges,
-                  const WeightItem* dec, int n_dec, const WeightItem* pre, int n_pre,
-                  hipStream_t stream) {
+                  const TileMerge* tiles, int n_tiles, const WeightItem* dec, int n_dec,
+                  const WeightItem* pre, int n_pre, hipStream_t stream) {
   if (n_items > 0) {
     if (p.a.decode_only && p.weight)
       decode_attn_f8_kernel<HD, true><<<n_items, 256, 0, stream>>>(p);
@@ -1160,15 +1241,14 @@ hipError_t launch(const AttnF8Params& p, int n_items, const MergeItem* merges, i
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (!p.weight) return launch_attn_merge(p.a, merges, n_merges, HD, stream);
   hipError_t e = hipSuccess;
-  if (n_dec > 0) {
-    const int weights = n_dec * p.a.nkv;
-    weight_decode_kernel<HD><<<weights + n_merges * p.a.nq, kMergeThreads, 0, stream>>>(
-        p, dec, weights, merges);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int weights = n_dec * p.a.nkv, rows = n_merges * p.a.nq;
+  const int blocks = kPrefillTileRows / kMergeRows<HD> * (p.a.nq >> p.pack_log2);
+  if (const int n = weights + rows + n_tiles * blocks; n > 0) {
+    finish_kernel<HD><<<n, kMergeThreads, 0, stream>>>(p, dec, weights, merges, rows, tiles);
+    e = hipGetLastError();
   }
-  if (n_pre > 0) {
+  if (e == hipSuccess && n_pre > 0) {
     weight_prefill_kernel<HD><<<n_pre * p.parts * p.a.nkv, 256, 0, stream>>>(p, pre);
     if ((e = hipGetLastError()) != hipSuccess || p.parts == 1) return e;
     weight_parts_kernel<<<n_pre * p.a.nkv, 256, 0, stream>>>(p, pre);
@@ -1191,12 +1271,11 @@ hipError_t launch_small_attn_f8(const AttnF8Params& p, const InlineMeta& meta, i
 }
 
 hipError_t launch_paged_attn_f8(const AttnF8Params& p, int n_items, const MergeItem* merges,
-                                int n_merges, const WeightItem* dec, int n_dec,
-                                const WeightItem* pre, int n_pre, int head_dim,
-                                hipStream_t stream) {
-  return head_dim == 128
-             ? launch<128>(p, n_items, merges, n_merges, dec, n_dec, pre, n_pre, stream)
-             : launch<64>(p, n_items, merges, n_merges, dec, n_dec, pre, n_pre, stream);
+                                int n_merges, const TileMerge* tiles, int n_tiles,
+                                const WeightItem* dec, int n_dec, const WeightItem* pre, int n_pre,
+                                int head_dim, hipStream_t stream) {
+  const auto call = head_dim == 128 ? launch<128> : launch<64>;
+  return call(p, n_items, merges, n_merges, tiles, n_tiles, dec, n_dec, pre, n_pre, stream);
 }
 
 }  // namespace mx

@@ -174,9 +174,13 @@ struct Plan {
   std::vector<ReqDev> reqs;
   std::vector<MergeItem> merges;
   int64_t n_pages = 0, n_items = 0, n_parts = 0;
-  int64_t n_tiles = 0;       // prefill tiles (work items: one per q head each)
+  int64_t n_tiles = 0;       // prefill tiles (work items: one per unit each)
   int split_pages = 16;
   int group = 1;
+  int pack = 1;              // rows of a token in a prefill tile: q heads unit * pack ..
+  int units = 1;             // of prefill tiles: n_q_heads / pack
+  int tile_chunks = 0;       // 64-key chunks of a prefill tile's split, 0: tiles are whole
+  std::vector<TileMerge> tile_merges;
   bool has_prefill = false;  // some work item is a prefill tile
 };
 
@@ -218,12 +222,58 @@ int choose_split_pages(const mx_batch* b, const mx_attn_shape* s, int step) {
 
 constexpr int kStepPages = 2, kStepPagesF8 = 4;
 
-void build_plan(const mx_batch* b, const mx_attn_shape* s, bool with_items, Plan& p,
-                int step = kStepPages) {
+// A prefill tile's splits over its keys, chunks of 64: `per` chunks each, the last one to
+// the tile's end.  They divide the chunks up to the one that holds the position of the
+// tile's first row, so that every row has a key in every split.
+constexpr int kMaxTileSplits = 64;
+struct TileSplit {
+  int n, per;
+};
+TileSplit split_tile(const Plan& p, int ctx_len, int start) {
+  if (p.tile_chunks == 0) return {1, 0};
+  const int chunks = (ctx_len + start / p.pack) / 64 + 1;
+  const int n = std::min<int>(ceil_div(chunks, p.tile_chunks), kMaxTileSplits);
+  const int per = (int)ceil_div(chunks, n);
+  return {(int)ceil_div(chunks, per), per};
+}
+
+// The 8-bit cache's prefill tiles: how many q heads of a KV head share a tile (a power of
+// two), and whether tiles are split over their keys.
+//
+// The chip holds 512 of their workgroups, and two on a CU take 1.7 us for a chunk of
+// keys each where one takes 1.1, so fewer tiles than that are split to about as many
+// items, of at least kMinTileChunks chunks (the merge and its launch cost what five
+// chunks do).  Heads that share a tile read their keys once and waste fewer rows of
+// short chunks, but make fewer tiles: as many of them as leave a workgroup per CU.
+constexpr int64_t kTileSlots = 512, kMinTileChunks = 16;
+void choose_tiles(const mx_batch* b, const mx_attn_shape* s, Plan& p) {
+  for (p.pack = std::min(p.group & -p.group, kPrefillTileRows);; p.pack /= 2) {
+    p.units = s->n_q_heads / p.pack;
+    int64_t tiles = 0, chunks = 0;
+    for (int r = 0; r < b->num_reqs; r++) {
+      const mx_request& q = b->reqs[r];
+      if (q.phase != MX_PREFILL) continue;
+      const int64_t rows = (int64_t)q.n_new * p.pack;
+      for (int64_t row = 0; row < rows; row += kPrefillTileRows) {
+        tiles += p.units;
+        if (tiles >= kTileSlots) return;
+        chunks += p.units * ((q.ctx_len + std::min(row + kPrefillTileRows, rows) / p.pack) / 64 + 1);
+      }
+    }
+    if (p.pack > 1 && std::max(tiles, chunks / kMinTileChunks) < kCUs) continue;
+    p.tile_chunks = (int)std::max(kMinTileChunks, ceil_div(chunks, kTileSlots));
+    return;
+  }
+}
+
+// (f8: for the 8-bit cache)
+void build_plan(const mx_batch* b, const mx_attn_shape* s, bool with_items, Plan& p, bool f8 = false) {
   p.batch = b;
   p.R = b->num_reqs;
   p.group = s->n_q_heads / s->n_kv_heads;
-  p.split_pages = choose_split_pages(b, s, step);
+  p.units = s->n_q_heads;
+  if (f8) choose_tiles(b, s, p);
+  p.split_pages = choose_split_pages(b, s, f8 ? kStepPagesF8 : kStepPages);
   p.reqs.resize(p.R);
   const int nq = s->n_q_heads;
   const int64_t sub = s->n_kv_heads * ceil_div(p.group, 16);  // decode items per split
@@ -243,7 +293,15 @@ void build_plan(const mx_batch* b, const mx_attn_shape* s, bool with_items, Plan
     pg += d.n_pages;
     if (!with_items) continue;
     if (d.phase == MX_PREFILL) {
-      p.n_tiles += ceil_div(d.n_new, kPrefillTileRows);
+      const int64_t n = ceil_div((int64_t)d.n_new * p.pack, kPrefillTileRows);
+      p.n_tiles += n;
+      for (int64_t t = n - 1; p.tile_chunks > 0 && t >= 0; t--) {  // in write_items' order
+        const int start = (int)t * kPrefillTileRows;
+        const TileSplit sp = split_tile(p, d.ctx_len, start);
+        if (sp.n == 1) continue;
+        p.n_tiles += sp.n - 1;
+        p.tile_merges.push_back(TileMerge{r, start, sp.n, 0});
+      }
     } else {
       d.n_split = (int)ceil_div(d.n_pages, p.split_pages);
       if (d.n_split > 1) {
@@ -253,7 +311,12 @@ void build_plan(const mx_batch* b, const mx_attn_shape* s, bool with_items, Plan
       p.n_items += d.n_split * sub;
     }
   }
-  p.n_items += p.n_tiles * nq;
+  // the tiles' partials after the decodes', 128 rows each
+  for (TileMerge& m : p.tile_merges) {
+    m.part = (int32_t)p.n_parts;
+    p.n_parts += (int64_t)p.units * m.n_split * kPrefillTileRows;
+  }
+  p.n_items += p.n_tiles * p.units;
   p.has_prefill = p.n_tiles > 0;
   p.T = tok;
   p.n_pages = pg;
@@ -266,29 +329,40 @@ void write_items(const Plan& p, const mx_attn_shape* s, AttnItem* out) {
   // items must not be left for the end: prefill tiles by the keys their last
   // rows scan, and the decode splits by page count, each longest first.
   struct Tile {
-    int req, start, keys;
+    int req, start, keys;  // (start: of split i of a tile, its first row + i)
+    int n_split, part;     // part: of unit 0, split 0
   };
   std::vector<Tile> tiles;
   tiles.reserve(p.n_tiles);
+  size_t n_split_tiles = 0;
   for (int r = 0; r < p.R; r++) {
     const ReqDev& d = p.reqs[r];
     if (d.phase != MX_PREFILL) continue;
-    for (int t = (d.n_new - 1) / kPrefillTileRows; t >= 0; t--) {
+    const int rows = d.n_new * p.pack;
+    for (int t = (rows - 1) / kPrefillTileRows; t >= 0; t--) {
       const int start = t * kPrefillTileRows;
-      tiles.push_back({r, start, d.ctx_len + std::min(start + kPrefillTileRows, d.n_new)});
+      const int last = std::min(start + kPrefillTileRows, rows) - 1;
+      const int keys = d.ctx_len + last / p.pack + 1;
+      const TileSplit sp = split_tile(p, d.ctx_len, start);
+      const int part = sp.n > 1 ? p.tile_merges[n_split_tiles++].part : 0;
+      for (int i = 0; i < sp.n; i++)
+        tiles.push_back(
+            {r, start + i, i < sp.n - 1 ? 64 * sp.per : keys - 64 * sp.per * i, sp.n, part});
     }
   }
   auto longer = [](const Tile& a, const Tile& b) { return a.keys > b.keys; };
   // (one prompt's tiles are generated in this order already)
   if (!std::is_sorted(tiles.begin(), tiles.end(), longer))
     std::stable_sort(tiles.begin(), tiles.end(), longer);
-  auto prefill = [&](const Tile& t, int head) {
-    return AttnItem{t.req, (int16_t)head, 1, 16, t.start, 0};
+  auto prefill = [&](const Tile& t, int unit) {
+    const int split = t.start % kPrefillTileRows;
+    const int part = t.part + (unit * t.n_split + split) * kPrefillTileRows;
+    return AttnItem{t.req, (int16_t)(unit * p.pack), 1, (int8_t)t.n_split, t.start, part};
   };
   // Decode splits: the whole ones of every request, then the requests' last
   // parts by a stable counting sort on their page count (1 .. split_pages; a
   // last part may be whole), so equal lengths keep request, split and head order.
-  const int64_t nD = p.n_items - p.n_tiles * nq;
+  const int64_t nD = p.n_items - p.n_tiles * p.units;
   std::vector<AttnItem> dec(p.n_tiles ? nD : 0);
   AttnItem* dp = p.n_tiles ? dec.data() : out;
   int64_t part_base = 0;
@@ -331,7 +405,7 @@ void write_items(const Plan& p, const mx_attn_shape* s, AttnItem* out) {
   if (!p.n_tiles) return;
   if (nD == 0) {
     for (const Tile& t : tiles)
-      for (int h = 0; h < nq; h++) *out++ = prefill(t, h);
+      for (int u = 0; u < p.units; u++) *out++ = prefill(t, u);
     return;
   }
   // Prefill tiles (matrix-core bound) and decode splits (bound by HBM) are
@@ -348,16 +422,16 @@ void write_items(const Plan& p, const mx_attn_shape* s, AttnItem* out) {
   // fabric to the decode stream beside them: the 70B launch at P = 8192 took
   // 2.10 ms against 2.24 ms with one list for all XCDs (same at P <= 4096).
   struct Lane {
-    std::vector<int> heads;        // q heads of this XCD's prefill tiles
+    std::vector<int> units;        // units of this XCD's prefill tiles
     int64_t n_pre, n_dec;          // items of either kind
     int64_t i = 0, j = 0;          // next of either
-    size_t tile = 0, head = 0;     // the next prefill item
+    size_t tile = 0, unit = 0;     // the next prefill item
   } lane[kXcds];
-  for (int h = 0; h < nq; h++) lane[(h / p.group) % kXcds].heads.push_back(h);
+  for (int u = 0; u < p.units; u++) lane[u * p.pack / p.group % kXcds].units.push_back(u);
   int64_t longest = 0;
   for (int x = 0; x < kXcds; x++) {
     Lane& l = lane[x];
-    l.n_pre = p.n_tiles * (int64_t)l.heads.size();
+    l.n_pre = p.n_tiles * (int64_t)l.units.size();
     l.n_dec = (nD - x + kXcds - 1) / kXcds;
     longest = std::max(longest, l.n_pre + l.n_dec);
   }
@@ -368,10 +442,10 @@ void write_items(const Plan& p, const mx_attn_shape* s, AttnItem* out) {
       // the list that is behind in its fraction done goes next
       if (l.j >= l.n_dec ||
           (l.i < l.n_pre && (double)l.i * (double)l.n_dec <= (double)l.j * (double)l.n_pre)) {
-        *out++ = prefill(tiles[l.tile], l.heads[l.head]);
+        *out++ = prefill(tiles[l.tile], l.units[l.unit]);
         l.i++;
-        if (++l.head == l.heads.size()) {
-          l.head = 0;
+        if (++l.unit == l.units.size()) {
+          l.unit = 0;
           l.tile++;
         }
       } else {
@@ -1197,6 +1271,14 @@ R no_throw(R failed, F&& f) {
   }
 }
 
+// Rows of a prefill tile are numbered in 32 bits.
+mx_status check_rows(const mx_batch* b, const mx_attn_shape* s) {
+  for (int r = 0; r < b->num_reqs; r++)
+    if ((int64_t)b->reqs[r].n_new * (s->n_q_heads / s->n_kv_heads) > INT32_MAX - 4096)
+      return fail(MX_ERR_TOO_LARGE, "request %d: %d new tokens", r, b->reqs[r].n_new);
+  return MX_OK;
+}
+
 // These calls read host staging buffers that later calls write again, so a captured
 // one would read whatever lies there at its replay.
 mx_status check_not_capturing(hipStream_t stream) {
@@ -1258,12 +1340,12 @@ int64_t page_touched_twice(const mx_batch* b) {
 // and the decodes' scores.
 struct LayoutF8 {
   Layout base;  // reqs, pages, items, merges, part_o, part_ml
-  size_t score_base = 0, dec = 0, pre = 0, meta_end = 0, lse = 0, scores = 0, part_w = 0, total = 0;
+  size_t tiles = 0, score_base = 0, dec = 0, pre = 0, meta_end = 0, lse = 0, scores = 0, part_w = 0, total = 0;
 };
 
 LayoutF8 make_layout_f8(int64_t R, int64_t T, int64_t n_pages, int64_t n_items, int64_t n_merges,
-                        int64_t n_parts, int64_t n_dec, int64_t n_pre, int64_t n_scores,
-                        int64_t n_part_w, const mx_attn_shape* s, bool track) {
+                        int64_t n_tiles, int64_t n_parts, int64_t n_dec, int64_t n_pre,
+                        int64_t n_scores, int64_t n_part_w, const mx_attn_shape* s, bool track) {
   LayoutF8 F;
   Layout& L = F.base;
   size_t o = 0;
@@ -1272,6 +1354,7 @@ LayoutF8 make_layout_f8(int64_t R, int64_t T, int64_t n_pages, int64_t n_items, 
   L.items = o; o = align_up(o + n_items * sizeof(AttnItem));
   L.merges = o; o = align_up(o + n_merges * sizeof(MergeItem));
   L.meta_end = o;
+  F.tiles = o; o = align_up(o + n_tiles * sizeof(TileMerge));
   if (track) {
     F.score_base = o; o = align_up(o + R * sizeof(int64_t));
     F.dec = o; o = align_up(o + n_dec * sizeof(WeightItem));
@@ -1311,7 +1394,7 @@ struct PlanF8 {
 };
 
 void build_plan_f8(const mx_batch* b, const mx_attn_shape* s, bool track, PlanF8& f) {
-  build_plan(b, s, true, f.p, kStepPagesF8);
+  build_plan(b, s, true, f.p, true);
   if (track)
     for (const ReqDev& d : f.p.reqs) {
       if (d.phase == MX_DECODE) {
@@ -1324,12 +1407,14 @@ void build_plan_f8(const mx_batch* b, const mx_attn_shape* s, bool track, PlanF8
   const int64_t units = f.n_pre * s->n_kv_heads;
   f.parts = units > 0 ? (int)ceil_div(kWeightUnits, std::min(units, kWeightUnits)) : 1;
   f.L = make_layout_f8(f.p.R, f.p.T, f.p.n_pages, f.p.n_items, (int64_t)f.p.merges.size(),
-                       f.p.n_parts, f.n_dec, f.n_pre, f.n_scores,
+                       (int64_t)f.p.tile_merges.size(), f.p.n_parts, f.n_dec, f.n_pre, f.n_scores,
                        f.parts > 1 ? 256 * f.parts * units : 0, s, track);
 }
 
 void pack_meta_f8(const PlanF8& f, const mx_attn_shape* s, bool track, char* h) {
   pack_meta(f.p, f.L.base, s, h);
+  if (!f.p.tile_merges.empty())
+    memcpy(h + f.L.tiles, f.p.tile_merges.data(), f.p.tile_merges.size() * sizeof(TileMerge));
   if (!track) return;
   int64_t* base = (int64_t*)(h + f.L.score_base);
   WeightItem* dec = (WeightItem*)(h + f.L.dec);
@@ -1355,7 +1440,7 @@ MX_EXPORT size_t mx_workspace_bytes_f8_for(const mx_batch* batch, const mx_attn_
                                            int32_t track) {
   g_err.clear();
   return no_throw((size_t)0, [&]() -> size_t {
-    if (validate_batch(batch, shape, nullptr) != MX_OK) return 0;
+    if (validate_batch(batch, shape, nullptr) != MX_OK || check_rows(batch, shape) != MX_OK) return 0;
     PlanF8 f;
     build_plan_f8(batch, shape, track != 0, f);
     return std::max(f.L.total, kAlign);
@@ -1372,9 +1457,17 @@ MX_EXPORT size_t mx_workspace_bytes_f8(const mx_attn_shape* shape, int32_t track
   }
   const int64_t nq = shape->n_q_heads, nkv = shape->n_kv_heads, group = nq / nkv;
   const int64_t splits = max_pages / 8 + max_reqs;  // as in mx_workspace_bytes
-  const int64_t items =
-      splits * nkv * ceil_div(group, 16) + (max_tokens / kPrefillTileRows + max_reqs) * nq;
-  return std::max(make_layout_f8(max_reqs, max_tokens, max_pages, items, max_reqs, splits * nq,
+  // (prefill tiles of fewer heads each than the group has: at most n_q_heads of a request
+  // beside the full ones)
+  const int64_t tiles = max_tokens * nq / kPrefillTileRows + max_reqs * nq;
+  // splits of prefill tiles: none unless there are fewer than kTileSlots, and then at most
+  // that many more than tiles
+  const int64_t split_tiles = std::min(tiles, kTileSlots),
+                per_tile = ceil_div(max_pages / 4 + 1, kMinTileChunks),
+                tile_parts = per_tile > 1 ? std::min(split_tiles + kTileSlots, split_tiles * per_tile) : 0;
+  const int64_t items = splits * nkv * ceil_div(group, 16) + tiles + tile_parts;
+  return std::max(make_layout_f8(max_reqs, max_tokens, max_pages, items, max_reqs, tile_parts,
+                                 splits * nq + tile_parts * kPrefillTileRows,
                                  max_pages / kWeightDecodePages + max_reqs,
                                  max_pages / kWeightPrefillPages + max_reqs,
                                  nq * (16 * max_pages + 64 * (int64_t)max_reqs),
@@ -1431,6 +1524,7 @@ MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape*
     if (T == 0) return MX_OK;
     if (!q || !out) return fail(MX_ERR_NULL, "tensor pointer is NULL");
     if ((st = check_aligned({q, out, ws})) != MX_OK) return st;
+    if ((st = check_rows(batch, shape)) != MX_OK) return st;
     const bool track = cache->weight != nullptr;
     PlanF8 f;
     build_plan_f8(batch, shape, track, f);
@@ -1452,8 +1546,9 @@ MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape*
     a.score_base = at<int64_t>(ws, L.score_base);
     a.part_w = at<float>(ws, L.part_w);
     a.parts = f.parts;
+    a.pack_log2 = __builtin_ctz(f.p.pack);
     if (const Layout small = small_layout(f.p); small.meta_end <= sizeof(InlineMeta) && !track &&
-                                                f.p.merges.empty()) {
+                                                f.p.merges.empty() && f.p.tile_merges.empty()) {
       alignas(16) InlineMeta meta;
       pack_meta(f.p, small, shape, meta.b);
       a.a.reqs = reinterpret_cast<const ReqDev*>(small.reqs);
@@ -1470,7 +1565,8 @@ MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape*
     if (st != MX_OK) return st;
     const hipError_t e = timed("paged_attn_f8", stream, [&] {
       return launch_paged_attn_f8(a, (int)f.p.n_items, at<MergeItem>(ws, L.base.merges),
-                                  (int)f.p.merges.size(), at<WeightItem>(ws, L.dec), (int)f.n_dec,
+                                  (int)f.p.merges.size(), at<TileMerge>(ws, L.tiles),
+                                  (int)f.p.tile_merges.size(), at<WeightItem>(ws, L.dec), (int)f.n_dec,
                                   at<WeightItem>(ws, L.pre), (int)f.n_pre, shape->head_dim, stream);
     });
     if (e != hipSuccess) return hip_fail(e, "attention launch");

@@ -154,6 +154,8 @@ struct ReqDev {
 //   kind 1 (prefill): q head `head`, query rows [start, start + kPrefillTileRows)
 //                     of the request.
 constexpr int kPrefillTileRows = 128;  // four waves x two blocks of 16 rows
+// (Of a prefill tile split over its keys, 8-bit cache: nrows is the number of splits,
+// start the tile's first row, a multiple of 128, + the split.)
 struct AttnItem {
   int32_t req;
   int16_t head;
@@ -173,6 +175,11 @@ struct AppendRun {
 struct MergeItem {
   int32_t req;
   int32_t part_base;  // partial index of (req, q head 0, split 0)
+};
+// A prefill tile whose keys are split: its first row and, of its first unit and split,
+// the partial of its first row.
+struct TileMerge {
+  int32_t req, start, n_split, part;
 };
 
 }  // namespace mx

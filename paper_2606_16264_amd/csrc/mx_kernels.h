@@ -28,9 +28,6 @@ struct AttnParams {
 
 hipError_t launch_paged_attn(const AttnParams& p, int n_items, const MergeItem* merges,
                              int n_merges, int head_dim, hipStream_t stream);
-// The merge of the key splits alone (part of launch_paged_attn).
-hipError_t launch_attn_merge(const AttnParams& p, const MergeItem* merges, int n_merges,
-                             int head_dim, hipStream_t stream);
 
 // Metadata of a small call, handed over with the kernel's arguments: no staging buffer
 // and no upload, which are most of such a call's time.  Offsets in it stand in the
@@ -69,13 +66,14 @@ struct AttnF8Params {
   const int64_t* score_base;  // [R] first score of the request
   float* part_w;              // a chunk's weights by parts of its rows: [item][part][nkv][256]
   int parts;                  // parts of a chunk's rows (1: part_w unused)
+  int pack_log2;              // q heads of a prefill tile
 };
 // The attention of the items, the merge of the key splits and, where p.weight is
 // set, the accumulation of the weights.
 hipError_t launch_paged_attn_f8(const AttnF8Params& p, int n_items, const MergeItem* merges,
-                                int n_merges, const WeightItem* dec, int n_dec,
-                                const WeightItem* pre, int n_pre, int head_dim,
-                                hipStream_t stream);
+                                int n_merges, const TileMerge* tiles, int n_tiles,
+                                const WeightItem* dec, int n_dec, const WeightItem* pre, int n_pre,
+                                int head_dim, hipStream_t stream);
 
 // The same for a call without splits and weights, its metadata (reqs, pages and items,
 // whose pointers are offsets) with the arguments.

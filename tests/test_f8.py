@@ -221,10 +221,12 @@ def test_launches(fake_hip):  # noqa: F811
                               [np.arange(1 << 16, (1 << 16) + -(-keep // 16)), []])
             return lambda st: L.mx_kv_evict_f8(2, e.ptr, S, c(5 << 20), A(0), A(2), BIG, st)
         long = mx.Batch([1], [1], [5000], [np.arange(400)])  # split over keys
+        late = mx.Batch([0], [9], [5000], [np.arange(400)])
         calls = dict(append=append(batch(3, 20)), append_many=append(batch(300, 20)),
                      attn=attn(batch(3, 20), None), attn_many=attn(batch(60, 20), None),
                      attn_split=attn(long, None), track=attn(batch(3, 20), 5 << 20),
-                     track_decodes=attn(long, 5 << 20),
+                     track_decodes=attn(long, 5 << 20), attn_late=attn(late, None),
+                     track_late=attn(late, 5 << 20),
                      evict=evict(40, 20), evict_long=evict(16000, 5000))
         kernels, st = {}, []
         for name, f in calls.items():
@@ -236,15 +238,17 @@ def test_launches(fake_hip):  # noqa: F811
         print(json.dumps(dict(kernels=kernels, st=st, bad=fake.fake_violations())))
         """)
     assert set(r["st"]) == {0} and r["bad"] == 0
-    names = ("upload", "small_append_f8", "kv_append_f8", "small_attn_f8", "paged_attn_f8", "attn_merge",
-             "decode_attn_f8", "weight_decode", "weight_prefill", "weight_parts", "small_evict_select",
+    names = ("upload", "small_append_f8", "kv_append_f8", "small_attn_f8", "paged_attn_f8", "finish",
+             "decode_attn_f8", "weight_prefill", "weight_parts", "small_evict_select",
              "small_evict_move", "evict_select", "evict_move")
     got = {k: [next(n for n in names if n in x) for x in v] for k, v in r["kernels"].items()}
     assert got == {
         "append": ["small_append_f8"], "append_many": ["kv_append_f8"],
         "attn": ["small_attn_f8"], "attn_many": ["upload", "paged_attn_f8"],
-        "attn_split": ["upload", "decode_attn_f8", "attn_merge"],
-        "track": ["upload", "paged_attn_f8", "weight_decode", "weight_prefill", "weight_parts"],
-        "track_decodes": ["upload", "decode_attn_f8", "weight_decode"],
+        "attn_split": ["upload", "decode_attn_f8", "finish"],
+        "track": ["upload", "paged_attn_f8", "finish", "weight_prefill", "weight_parts"],
+        "track_decodes": ["upload", "decode_attn_f8", "finish"],
+        "attn_late": ["upload", "paged_attn_f8", "finish"],
+        "track_late": ["upload", "paged_attn_f8", "finish", "weight_prefill", "weight_parts"],
         "evict": ["small_evict_select", "small_evict_move"],
         "evict_long": ["upload", "evict_select", "evict_move"]}

@@ -323,6 +323,25 @@ def test_attention_late_chunk():
     check_weights(c, c.hw, reqs, weights, worst)
 
 
+@pytest.mark.parametrize("weight", [False, True])
+@pytest.mark.parametrize("nq,nkv,d,reqs", [
+    (8, 2, 128, [(0, 5, 5000)]), (8, 2, 64, [(0, 1, 3000)]), (4, 1, 128, [(0, 33, 2047)]),
+    (6, 2, 64, [(0, 50, 4100), (0, 9, 1500), (0, 3, 0)]), (5, 1, 128, [(0, 260, 2500)]),
+    (3, 3, 64, [(0, 130, 1985)]), (16, 1, 128, [(0, 20, 6001), (1, 1, 2500), (1, 1, 33)]),
+    (40, 2, 64, [(0, 7, 1030), (1, 1, 9000)]), (32, 8, 128, [(0, 140, 1100), (0, 65, 4095)]),
+    (8, 8, 64, [(0, 300, 1900)]), (256, 2, 64, [(0, 4, 1500)])])
+def test_attention_split_tiles(nq, nkv, d, reqs, weight):
+    """Few prefill tiles over long contexts, which are split over their keys: groups that are a
+    power of two, that hold one, that are odd; a first split that ends at a tile's positions."""
+    c, reqs, q = make_case(nq, nkv, d, reqs, nq + d, weight)
+    out, mag, weights, worst = attend_ref(c, nq, reqs, q.double().numpy())
+    got, _ = run_attn(c, nq, reqs, q.cuda())
+    check_out(got, out, mag)
+    if weight:
+        check_weights(c, c.hw, reqs, weights, worst)
+    assert torch.equal(run_attn(c, nq, reqs, q.cuda())[0], got)
+
+
 def test_chunk_weights_without_parts():
     """Keys and KV heads enough that a chunk's rows are not split, causal edges inside."""
     c, reqs, q = make_case(32, 32, 64, [(0, 300, 4001), (0, 33, 0)], 14, True)
