@@ -952,7 +952,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void s
 __device__ __forceinline__ void add_weight(float* w, float x) { unsafeAtomicAdd(w, x); }
 
 // Merges the splits of a prefill tile over its keys: HD / 4 threads a row, 8 (HD = 128) or
-// 16 rows of one unit a workgroup.  Bound by memory.
+// 16 rows of one unit a workgroup.  Bound by memory (1024 rows of 32 heads in two splits,
+// 34 MB of partials just written, beside the weights of 16 decodes: 10 us, 5 those alone).
 template <int HD>
 constexpr int kMergeRows = 4 * kMergeThreads / HD;
 template <int HD>

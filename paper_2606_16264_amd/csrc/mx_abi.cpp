@@ -225,13 +225,14 @@ constexpr int kStepPages = 2, kStepPagesF8 = 4;
 // A prefill tile's splits over its keys, chunks of 64: `per` chunks each, the last one to
 // the tile's end.  They divide the chunks up to the one that holds the position of the
 // tile's first row, so that every row has a key in every split.
-constexpr int kMaxTileSplits = 64;
+constexpr int kMaxTileSplits = 64, kWholeTileChunks = 16;
 struct TileSplit {
   int n, per;
 };
 TileSplit split_tile(const Plan& p, int ctx_len, int start) {
   if (p.tile_chunks == 0) return {1, 0};
   const int chunks = (ctx_len + start / p.pack) / 64 + 1;
+  if (chunks <= kWholeTileChunks) return {1, 0};
   const int n = std::min<int>(ceil_div(chunks, p.tile_chunks), kMaxTileSplits);
   const int per = (int)ceil_div(chunks, n);
   return {(int)ceil_div(chunks, per), per};
@@ -242,10 +243,14 @@ TileSplit split_tile(const Plan& p, int ctx_len, int start) {
 //
 // The chip holds 512 of their workgroups, and two on a CU take 1.7 us for a chunk of
 // keys each where one takes 1.1, so fewer tiles than that are split to about as many
-// items, of at least kMinTileChunks chunks (the merge and its launch cost what five
-// chunks do).  Heads that share a tile read their keys once and waste fewer rows of
-// short chunks, but make fewer tiles: as many of them as leave a workgroup per CU.
-constexpr int64_t kTileSlots = 512, kMinTileChunks = 16;
+// items, of at least kMinTileChunks chunks; the merge and its launch cost what five
+// chunks do, so tiles of few chunks stay whole (8B heads: 16 new tokens over 100000
+// 1549 -> 67 us, 128 over 14336 250 -> 52, 1024 over 14336 297 -> 268; a least split of
+// 16 chunks instead of 8: 1 over 3000 21 -> 28, 128 over 4000 34 -> 37, 512 over 1500 43
+// -> 41; of 15 chunks 8 and 7 each instead of the whole: 22 -> 23).  Heads that share a
+// tile read their keys once and waste fewer rows of short chunks, but make fewer tiles:
+// as many of them as leave a workgroup per CU.
+constexpr int64_t kTileSlots = 512, kMinTileChunks = 8;
 void choose_tiles(const mx_batch* b, const mx_attn_shape* s, Plan& p) {
   for (p.pack = std::min(p.group & -p.group, kPrefillTileRows);; p.pack /= 2) {
     p.units = s->n_q_heads / p.pack;
