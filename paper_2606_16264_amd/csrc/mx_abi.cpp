@@ -242,15 +242,16 @@ TileSplit split_tile(const Plan& p, int ctx_len, int start) {
 // two), and whether tiles are split over their keys.
 //
 // The chip holds 512 of their workgroups, and two on a CU take 1.7 us for a chunk of
-// keys each where one takes 1.1, so fewer tiles than that are split to about as many
-// items, of at least kMinTileChunks chunks; the merge and its launch cost what five
+// keys each where one takes 1.1, so up to kSplitTiles tiles are split to about as many
+// items, of at least kMinTileChunks chunks (2048 tokens of the 8B heads make 512 tiles;
+// 1536 over 14336 420 -> 374 us, but 1664 409 -> 427); the merge and its launch cost what five
 // chunks do, so tiles of few chunks stay whole (8B heads: 16 new tokens over 100000
 // 1549 -> 67 us, 128 over 14336 250 -> 52, 1024 over 14336 297 -> 268; a least split of
 // 16 chunks instead of 8: 1 over 3000 21 -> 28, 128 over 4000 34 -> 37, 512 over 1500 43
 // -> 41; of 15 chunks 8 and 7 each instead of the whole: 22 -> 23).  Heads that share a
 // tile read their keys once and waste fewer rows of short chunks, but make fewer tiles:
 // as many of them as leave a workgroup per CU.
-constexpr int64_t kTileSlots = 512, kMinTileChunks = 8;
+constexpr int64_t kTileSlots = 512, kSplitTiles = 384, kMinTileChunks = 8;
 void choose_tiles(const mx_batch* b, const mx_attn_shape* s, Plan& p) {
   for (p.pack = std::min(p.group & -p.group, kPrefillTileRows);; p.pack /= 2) {
     p.units = s->n_q_heads / p.pack;
@@ -261,7 +262,7 @@ void choose_tiles(const mx_batch* b, const mx_attn_shape* s, Plan& p) {
       const int64_t rows = (int64_t)q.n_new * p.pack;
       for (int64_t row = 0; row < rows; row += kPrefillTileRows) {
         tiles += p.units;
-        if (tiles >= kTileSlots) return;
+        if (tiles > kSplitTiles) return;
         chunks += p.units * ((q.ctx_len + std::min(row + kPrefillTileRows, rows) / p.pack) / 64 + 1);
       }
     }
@@ -1465,9 +1466,8 @@ MX_EXPORT size_t mx_workspace_bytes_f8(const mx_attn_shape* shape, int32_t track
   // (prefill tiles of fewer heads each than the group has: at most n_q_heads of a request
   // beside the full ones)
   const int64_t tiles = max_tokens * nq / kPrefillTileRows + max_reqs * nq;
-  // splits of prefill tiles: none unless there are fewer than kTileSlots, and then at most
-  // that many more than tiles
-  const int64_t split_tiles = std::min(tiles, kTileSlots),
+  // splits of prefill tiles: at most kTileSlots more than tiles
+  const int64_t split_tiles = std::min(tiles, kSplitTiles),
                 per_tile = ceil_div(max_pages / 4 + 1, kMinTileChunks),
                 tile_parts = per_tile > 1 ? std::min(split_tiles + kTileSlots, split_tiles * per_tile) : 0;
   const int64_t items = splits * nkv * ceil_div(group, 16) + tiles + tile_parts;
