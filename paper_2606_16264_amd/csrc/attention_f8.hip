@@ -1112,13 +1112,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
       }
   }
   float acc[4][4] = {};
-  // Row blocks from the first that sees one of the 256 keys on, this part's share of
-  // them; from `whole` on the rows see them all.
+  // Row blocks from the first that sees one of the 256 keys on, this part's share of them.
   const int first_key = it.start * 16, blocks = (rq.n_new + kWeightRows - 1) / kWeightRows;
   const int blk0 = max(0, first_key - rq.ctx_len) / kWeightRows;
   const int share = (blocks - blk0 + p.parts - 1) / p.parts;
   const int begin = blk0 + part * share, end = min(begin + share, blocks);
-  const int whole = (max(0, first_key + 255 - rq.ctx_len) + kWeightRows - 1) / kWeightRows;
 
   // this thread's pieces of a block of rows, and a row's log-sum (infinite past the last
   // row, which then adds 0)
@@ -1185,8 +1183,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void w
       const int row0 = kWeightRows * blk;
 #pragma unroll
       for (int sub = 0; sub < kWeightRows / 16; sub++) {
-        if (blk < whole) add(std::integral_constant<bool, true>{}, buf, row0, sub);
-        else add(std::integral_constant<bool, false>{}, buf, row0, sub);
+        // (how far the first row's position is past the wave's first key)
+        const int past = rq.ctx_len + row0 + 16 * sub - page0 * 16;
+        if (past >= 63) add(std::integral_constant<bool, false>{}, buf, row0, sub);
+        else if (past > -16) add(std::integral_constant<bool, true>{}, buf, row0, sub);
       }
       if (nblk < end) put(buf ^ 1);
       __syncthreads();

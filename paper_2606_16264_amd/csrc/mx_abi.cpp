@@ -1379,7 +1379,7 @@ LayoutF8 make_layout_f8(int64_t R, int64_t T, int64_t n_pages, int64_t n_items, 
 }
 
 // Workgroups of 256 keys, one KV head and a part of the rows that the weights of prompt
-// chunks are computed by: as many parts as it takes for two per CU.
+// chunks are computed by: as many parts as two per CU allow.
 constexpr int64_t kWeightUnits = 512;
 
 // The metadata of a call without splits, closely packed.
@@ -1411,7 +1411,7 @@ void build_plan_f8(const mx_batch* b, const mx_attn_shape* s, bool track, PlanF8
       }
     }
   const int64_t units = f.n_pre * s->n_kv_heads;
-  f.parts = units > 0 ? (int)ceil_div(kWeightUnits, std::min(units, kWeightUnits)) : 1;
+  f.parts = units > 0 ? (int)std::max<int64_t>(kWeightUnits / units, 1) : 1;
   f.L = make_layout_f8(f.p.R, f.p.T, f.p.n_pages, f.p.n_items, (int64_t)f.p.merges.size(),
                        (int64_t)f.p.tile_merges.size(), f.p.n_parts, f.n_dec, f.n_pre, f.n_scores,
                        f.parts > 1 ? 256 * f.parts * units : 0, s, track);
