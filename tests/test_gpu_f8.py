@@ -447,6 +447,25 @@ def test_nan_values_of_later_tokens(d, weight):
         check_weights(c, c.hw, reqs, weights, worst)
 
 
+@pytest.mark.parametrize("weight", [False, True])
+def test_nan_in_split_tiles(weight):
+    """A NaN key or value of any split reaches the rows that attend to it, of its heads and dim."""
+    c, reqs, q = make_case(8, 2, 128, [(0, 40, 3000), (0, 3, 2000)], 24, weight)
+    start = [0, 40]
+    exp, mag, _, _ = attend_ref(c, 8, reqs, q.double().numpy())
+    bad = np.zeros(exp.shape, bool)
+    for r, pos, g, e in [(0, 700, 0, 5), (0, 3010, 1, 77), (1, 2001, 0, 3)]:
+        table, first = reqs[r][3], max(0, pos - reqs[r][2])
+        c.hv[table[pos // 16], g, pos % 16, e] = NAN
+        bad[start[r] + first:start[r] + reqs[r][1], 4 * g:4 * g + 4, e] = True
+    c.hk[reqs[1][3][60], 1, 2, 7] = NAN
+    bad[40:, 4:] = True
+    c.upload()
+    got = run_attn(c, 8, reqs, q.cuda())[0].cpu()
+    assert (got.isnan().numpy() == bad).all()
+    check_out(got.masked_fill(torch.from_numpy(bad), 0), np.where(bad, 0, exp), mag)
+
+
 def test_shared_prefix_weights_add_up():
     """Requests that read the same cached pages: each key receives the sum over all of them."""
     c, reqs, q = make_case(8, 2, 64, [(1, 1, 90), (0, 33, 64)], 7, True)
