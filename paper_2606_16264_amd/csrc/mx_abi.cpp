@@ -244,21 +244,28 @@ TileSplit split_tile(const Plan& p, int ctx_len, int start) {
 // The chip holds 512 of their workgroups, and two on a CU take 1.7 us for a chunk of
 // keys each where one takes 1.1, so up to kSplitTiles tiles are split to about as many
 // items, of at least kMinTileChunks chunks (2048 tokens of the 8B heads make 512 tiles;
-// 1536 over 14336 420 -> 374 us, but 1664 409 -> 427); the merge and its launch cost what five
+// 1536 over 14336 420 -> 374 us, but 1664 409 -> 427), and to half as many more beside
+// kMixedDecodes KV heads of decodes, which fill the CUs unevenly (128 tokens over 14336
+// beside 32 decodes 329 -> 85 us, 256 over 4000 beside 128 149 -> 99 -> 88, 512 over 2000
+// beside 8 84 -> 66 -> 63; without decodes 512 over 14336 130 -> 143); the merge and its launch cost what five
 // chunks do, so tiles of few chunks stay whole (8B heads: 16 new tokens over 100000
 // 1549 -> 67 us, 128 over 14336 250 -> 52, 1024 over 14336 297 -> 268; a least split of
 // 16 chunks instead of 8: 1 over 3000 21 -> 28, 128 over 4000 34 -> 37, 512 over 1500 43
 // -> 41; of 15 chunks 8 and 7 each instead of the whole: 22 -> 23).  Heads that share a
 // tile read their keys once and waste fewer rows of short chunks, but make fewer tiles:
 // as many of them as leave a workgroup per CU.
-constexpr int64_t kTileSlots = 512, kSplitTiles = 384, kMinTileChunks = 8;
+constexpr int64_t kTileSlots = 512, kTileSlotsMixed = 768, kMixedDecodes = 64, kSplitTiles = 384,
+                  kMinTileChunks = 8;
 void choose_tiles(const mx_batch* b, const mx_attn_shape* s, Plan& p) {
   for (p.pack = std::min(p.group & -p.group, kPrefillTileRows);; p.pack /= 2) {
     p.units = s->n_q_heads / p.pack;
-    int64_t tiles = 0, chunks = 0;
+    int64_t tiles = 0, chunks = 0, decodes = 0;
     for (int r = 0; r < b->num_reqs; r++) {
       const mx_request& q = b->reqs[r];
-      if (q.phase != MX_PREFILL) continue;
+      if (q.phase != MX_PREFILL) {
+        decodes += s->n_kv_heads;
+        continue;
+      }
       const int64_t rows = (int64_t)q.n_new * p.pack;
       for (int64_t row = 0; row < rows; row += kPrefillTileRows) {
         tiles += p.units;
@@ -267,7 +274,8 @@ void choose_tiles(const mx_batch* b, const mx_attn_shape* s, Plan& p) {
       }
     }
     if (p.pack > 1 && std::max(tiles, chunks / kMinTileChunks) < kCUs) continue;
-    p.tile_chunks = (int)std::max(kMinTileChunks, ceil_div(chunks, kTileSlots));
+    const int64_t slots = decodes < kMixedDecodes ? kTileSlots : kTileSlotsMixed;
+    p.tile_chunks = (int)std::max(kMinTileChunks, ceil_div(chunks, slots));
     return;
   }
 }
@@ -1466,10 +1474,10 @@ MX_EXPORT size_t mx_workspace_bytes_f8(const mx_attn_shape* shape, int32_t track
   // (prefill tiles of fewer heads each than the group has: at most n_q_heads of a request
   // beside the full ones)
   const int64_t tiles = max_tokens * nq / kPrefillTileRows + max_reqs * nq;
-  // splits of prefill tiles: at most kTileSlots more than tiles
+  // splits of prefill tiles: at most kTileSlotsMixed more than tiles
   const int64_t split_tiles = std::min(tiles, kSplitTiles),
                 per_tile = ceil_div(max_pages / 4 + 1, kMinTileChunks),
-                tile_parts = per_tile > 1 ? std::min(split_tiles + kTileSlots, split_tiles * per_tile) : 0;
+                tile_parts = per_tile > 1 ? std::min(split_tiles + kTileSlotsMixed, split_tiles * per_tile) : 0;
   const int64_t items = splits * nkv * ceil_div(group, 16) + tiles + tile_parts;
   return std::max(make_layout_f8(max_reqs, max_tokens, max_pages, items, max_reqs, tile_parts,
                                  splits * nq + tile_parts * kPrefillTileRows,
