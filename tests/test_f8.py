@@ -161,6 +161,17 @@ def test_empty_calls_are_no_ops():
     assert mx.mx_workspace_bytes_f8_for(empty, s) > 0
 
 
+def test_rows_of_a_chunk_fit_32_bits():
+    """New tokens times the q heads of a KV head are numbered in 32 bits."""
+    s = shape(32767, 1, 64, 5000)
+    for n_new, ok in ((65000, True), (65540, False)):
+        b = mx.Batch([mx.MX_PREFILL], [n_new], [0], [np.arange(-(-n_new // 16))])
+        need = mx.lib().mx_workspace_bytes_f8_for(b.ptr, ctypes.byref(s), 0)
+        assert (need > 0) == ok
+        if not ok:
+            assert attn(b, s, raw_cache()) == mx.MX_ERR_TOO_LARGE
+
+
 def test_binding_checks_the_cache():
     s = shape()
     c = cache(s)
