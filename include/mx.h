@@ -300,8 +300,11 @@ mx_status mx_kv_append_f8(const mx_batch* batch, const mx_attn_shape* shape,
  *                           p[t][h][j].
  * Sums are in fp32.  A page that several requests of the batch share receives the sum
  * over all of them (in no fixed order; every other weight, and every output, is the
- * same from run to run).  A NaN value reaches the rows that attend to its token, and no
- * earlier row of its chunk.  Sizes of the workspace: mx_workspace_bytes_f8_for, with
+ * same from run to run).  Scores are fp32 sums of exact products; probabilities are
+ * rounded to bf16 for the value products, and for a row's sum where no weight is
+ * accumulated, so that an output may differ by such a rounding between a call with weight
+ * and one without, and between a decode and a one-token prompt.  A NaN value reaches the
+ * rows that attend to its token, and no earlier row of its chunk.  Sizes of the workspace: mx_workspace_bytes_f8_for, with
  * track != 0 where cache->weight is given (it holds the decodes' scores then); its
  * upper bound for any batch of at most max_tokens new tokens, max_reqs requests and
  * max_pages page-table entries in total: mx_workspace_bytes_f8.

@@ -8,6 +8,13 @@
 // the 16x16x32 bf16 matrix-core instruction, the softmax of a query row held by the
 // four lanes l, l ^ 16, l ^ 32, l ^ 48, then O^T += V^T P^T from registers.
 //
+// The score products are exact and added in fp32.  (The 16x16x128 fp8 instruction on the
+// codes as they are, the query as two codes per element, takes 454 instead of 494 us for
+// a chunk of 2048 tokens over 14336 of the 8B heads.  But it aligns its products to the
+// largest before it adds them, so a score's error grows with sum |q k|: where channels of
+// 960 cancel the output was off by 1.6%, where they are 250 by 0.4, and with these
+// products by 0.22 in both.)
+//
 // Keys are consumed four pages (64 keys) at a time.  Score block b, row m is the key
 //   kappa_b(m) = token 4 b + m % 4 of page m / 4,
 // so that lane group g (rows 4 g .. 4 g + 3 of the four blocks) ends up with the 16
@@ -397,98 +404,6 @@ __device__ __forceinline__ void nan_values(const u32x4& nan, int last, f32x4& o)
   for (int e = 0; e < 4; e++) o[e] = seen[e] > 0.f ? __builtin_nanf("") : o[e];
 }
 
-// A prefill tile's query rows as the B operand of the score products.
-//
-// Where no weights are accumulated the products take the key codes as they are, with the
-// 16x16x128 fp8 instruction, which multiplies each operand by a power of two per row
-// (the page's scale, the row's scale) on the way; the query goes in as two codes per
-// element, q = (hi + lo / 16) * scale: hi carries the upper four of a bf16 value's eight
-// significant bits, lo the rest, so that the sum is q itself (to 2^-22 of the row's
-// largest element, where lo ends).  That takes as long on the matrix cores as bf16
-// products do and saves the conversion of the keys, half the conversions of a tile: 489
-// -> 445 us for 2048 tokens over 14336 of the 8B heads.
-// The instruction aligns its products before it adds them: scores come out within
-// 2^-15 of sum |q k| (2e-5 of the largest score measured on normal data), a hundredth
-// of what the probabilities' rounding to bf16 does to them.  The accumulated weights
-// are fp32 results, so there (TRACK) keys are widened to bf16 and the products exact.
-typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8;
-__device__ __forceinline__ i32x8 join(u32x4 a, u32x4 b) {
-  return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-// 16x16x128: A's rows times B's columns, each times 2^(byte 0 of its lane's scale - 127).
-// k index 16 g + j is byte j of lane group g, 64 + 16 g + j its byte 16 + j; the scale
-// of lane group g belongs to k indices 32 g .. 32 g + 31.
-__device__ __forceinline__ f32x4 mfma_f8(i32x8 a, int as, i32x8 b, int bs, f32x4 c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, as, 0, bs);
-}
-template <int HD>
-struct CodedQuery {
-  // HD = 128: hi and lo one product each; HD = 64: k indices 0 .. 63 are hi, 64 .. 127 lo
-  i32x8 op[HD / 64];
-  int exp[HD / 64];
-
-  __device__ __forceinline__ void load(const AttnF8Params& p, int64_t tok, int qhead, bool valid,
-                                       int g4) {
-    bf16x8 q[HD / 32];
-    load_q<HD>(p, tok, qhead, valid, g4, q);
-    float amax = 0.f;
-#pragma unroll
-    for (int e = 0; e < HD / 32; e++)
-#pragma unroll
-      for (int i = 0; i < 8; i++) amax = fmaxf(amax, __builtin_fabsf((float)q[e][i]));
-    amax = lane_groups_max(amax);
-    // the least 2^e with amax <= 448 * 2^e (an infinite row's codes are NaN anyway)
-    const uint32_t bits = __float_as_uint(amax);
-    const int e8 = min(max((int)(bits >> 23) - 8 + ((bits & 0x7FFFFF) > 0x600000), 27), 247);
-    const float inv = __uint_as_float((uint32_t)(254 - e8) << 23);
-    u32x4 hi[HD / 64], lo[HD / 64];
-#pragma unroll
-    for (int h = 0; h < HD / 64; h++)
-#pragma unroll
-      for (int w = 0; w < 4; w++) {
-        int ch = 0, cl = 0;
-        float x[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) x[i] = (float)q[2 * h + (w >> 1)][4 * (w & 1) + i] * inv;
-        ch = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], ch, false);
-        ch = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], ch, true);
-        const mx_f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(ch, false);
-        const mx_f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(ch, true);
-        cl = __builtin_amdgcn_cvt_pk_fp8_f32((x[0] - a[0]) * 16.f, (x[1] - a[1]) * 16.f, cl, false);
-        cl = __builtin_amdgcn_cvt_pk_fp8_f32((x[2] - b[0]) * 16.f, (x[3] - b[1]) * 16.f, cl, true);
-#pragma unroll
-        for (int i = 0; i < 4; i++)  // not finite: NaN, whatever the conversion makes of it
-          if (!(__builtin_fabsf(x[i]) <= 448.f)) ch |= 0x7F << (8 * i);
-        hi[h][w] = (uint32_t)ch;
-        lo[h][w] = (uint32_t)cl;
-      }
-    if constexpr (HD == 128) {
-      op[0] = join(hi[0], hi[1]);
-      op[1] = join(lo[0], lo[1]);
-      exp[0] = e8;
-      exp[1] = e8 - 4;
-    } else {
-      op[0] = join(hi[0], lo[0]);
-      exp[0] = g4 < 2 ? e8 : e8 - 4;
-    }
-  }
-  // a score block: the codes of 16 keys, their scales' exponents
-  __device__ __forceinline__ f32x4 score(const u32x4 (&k)[HD / 64], int ke) const {
-    const i32x8 a = join(k[0], k[HD / 64 - 1]);
-    f32x4 s = mfma_f8(a, ke, op[0], exp[0], f32x4{0.f, 0.f, 0.f, 0.f});
-    if constexpr (HD == 128) s = mfma_f8(a, ke, op[1], exp[1], s);
-    return s;
-  }
-};
-template <int HD>
-struct WideQuery {
-  bf16x8 q[HD / 32];
-  __device__ __forceinline__ void load(const AttnF8Params& p, int64_t tok, int qhead, bool valid,
-                                       int g4) {
-    load_q<HD>(p, tok, qhead, valid, g4, q);
-  }
-};
-
 // Prefill tiles share every 64-key chunk through LDS.  Wave w copies page w of the
 // chunk there with the DMA path (global_load_lds, 16 bytes per lane): its keys, its
 // values and, by an ordinary store, its two scales.  Keys keep the page's layout but
@@ -580,12 +495,12 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
   const int page_end = row0 < rows ? pages_to(row0 + 31) : 0;
   const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
 
-  std::conditional_t<TRACK, WideQuery<HD>, CodedQuery<HD>> qf, qf2;
+  bf16x8 qf[HD / 32], qf2[HD / 32];
   int row_pos, row_pos2;
   {
     const Row a = row_at(row0 + col), b = row_at(row0 + 16 + col);
-    qf.load(p, rq.tok_start + a.token, a.head, a.valid, g4);
-    qf2.load(p, rq.tok_start + b.token, b.head, b.valid, g4);
+    load_q<HD>(p, rq.tok_start + a.token, a.head, a.valid, g4, qf);
+    load_q<HD>(p, rq.tok_start + b.token, b.head, b.valid, g4, qf2);
     row_pos = ctx_len + a.token;
     row_pos2 = ctx_len + b.token;
   }
@@ -668,21 +583,15 @@ __device__ __forceinline__ void prefill_item(const AttnF8Params& p, const AttnIt
       lgkm_wait<(3 - B) * NH>();
       if constexpr (B == 0) pin1(ks);
       pin(k[B]);
-      if constexpr (TRACK) {
-        n1[B] = n2[B] = f32x4{0.f, 0.f, 0.f, 0.f};
+      n1[B] = n2[B] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int h = 0; h < NH; h++)
+      for (int h = 0; h < NH; h++)
 #pragma unroll
-          for (int i = 0; i < 2; i++) {
-            const bf16x8 w = widen(k[B][h][2 * i], k[B][h][2 * i + 1], __uint_as_float(ks));
-            n1[B] = mfma16(w, qf.q[2 * h + i], n1[B]);
-            n2[B] = mfma16(w, qf2.q[2 * h + i], n2[B]);
-          }
-      } else {
-        const int ke = (int)(ks >> 23);
-        n1[B] = qf.score(k[B], ke);
-        n2[B] = qf2.score(k[B], ke);
-      }
+        for (int i = 0; i < 2; i++) {
+          const bf16x8 w = widen(k[B][h][2 * i], k[B][h][2 * i + 1], __uint_as_float(ks));
+          n1[B] = mfma16(w, qf[2 * h + i], n1[B]);
+          n2[B] = mfma16(w, qf2[2 * h + i], n2[B]);
+        }
       beside(b);
       __builtin_amdgcn_sched_barrier(0);  // these products go before the next wait
     };

@@ -241,19 +241,24 @@ TileSplit split_tile(const Plan& p, int ctx_len, int start) {
 // The 8-bit cache's prefill tiles: how many q heads of a KV head share a tile (a power of
 // two), and whether tiles are split over their keys.
 //
-// The chip holds 512 of their workgroups, and two on a CU take 1.7 us for a chunk of
-// keys each where one takes 1.1, so up to kSplitTiles tiles are split to about as many
+// The chip holds 512 of their workgroups, and two on a CU take 1.9 us for a chunk of
+// keys each where one takes 1.2, so up to kSplitTiles tiles are split to about as many
 // items, of at least kMinTileChunks chunks (2048 tokens of the 8B heads make 512 tiles;
-// 1536 over 14336 420 -> 374 us, but 1664 409 -> 427), and to half as many more beside
+// 1536 over 14336 446 -> 376 us, but 1664 456 -> 466), and to half as many more beside
 // kMixedDecodes KV heads of decodes, which fill the CUs unevenly (128 tokens over 14336
-// beside 32 decodes 329 -> 85 us, 256 over 4000 beside 128 149 -> 99 -> 88, 512 over 2000
-// beside 8 84 -> 66 -> 63; without decodes 512 over 14336 130 -> 143); the merge and its launch cost what five
-// chunks do, so tiles of few chunks stay whole (8B heads: 16 new tokens over 100000
-// 1549 -> 67 us, 128 over 14336 250 -> 52, 1024 over 14336 297 -> 268; a least split of
-// 16 chunks instead of 8: 1 over 3000 21 -> 28, 128 over 4000 34 -> 37, 512 over 1500 43
-// -> 41; of 15 chunks 8 and 7 each instead of the whole: 22 -> 23).  Heads that share a
+// beside 32 decodes 412 -> 85 us, 256 over 4000 beside 128 157 -> 98 -> 88, 512 over 2000
+// beside 8 87 -> 65 -> 62; without decodes 512 over 14336 136 -> 141); the merge and its
+// launch cost what five chunks do, so tiles of up to kWholeTileChunks chunks stay whole
+// (8B heads: 16 new tokens over 100000 1755 -> 72 us, 128 over 14336 271 -> 52, 1024 over
+// 14336 291 -> 290; a least split of 16 chunks instead of 8: 1 over 3000 22 -> 29, 128 over
+// 4000 33 -> 37, 512 over 1500 42 -> 40; tiles of 9 to 16 chunks split: 1 over 520 15.3 ->
+// 16.5, 256 over 600 24.2 -> 27.4, though 1 over 960 22.8 -> 20.1).  Heads that share a
 // tile read their keys once and waste fewer rows of short chunks, but make fewer tiles:
 // as many of them as leave a workgroup per CU.
+//
+// The tiles of all requests are counted together, whatever their lengths: a batch of more
+// than kSplitTiles is not split at all, and takes the time of its longest tile (16 tokens
+// over 100000 beside a fresh prompt of 2048: 1764 us, the two in calls of their own 73 + 59).
 constexpr int64_t kTileSlots = 512, kTileSlotsMixed = 768, kMixedDecodes = 64, kSplitTiles = 384,
                   kMinTileChunks = 8;
 void choose_tiles(const mx_batch* b, const mx_attn_shape* s, Plan& p) {

@@ -408,6 +408,46 @@ def test_large_queries():
     check_out(got, out, mag)
 
 
+@pytest.mark.parametrize("weight", [False, True])
+@pytest.mark.parametrize("nq,nkv,d,reqs", [
+    (8, 2, 128, [(0, 150, 301), (1, 1, 300)]), (4, 4, 64, [(0, 40, 0), (0, 3, 100)]),
+    (8, 2, 64, [(0, 5, 3000)]), (2, 1, 128, [(1, 1, 77), (1, 1, 2000)])])
+def test_cancelling_channels(nq, nkv, d, reqs, weight):
+    """Channels whose products are hundreds and cancel: every key of a KV head has the same score,
+    the part that differs cancels between two channels with the same query, one's codes the other's
+    negated.  Codes are integers and queries multiples of 1 / 32, so with
+    sum |q k| < 2^24 / 32 in units of a code every partial sum is an fp32 number: a score in 32 bits
+    is exact in any order.  A row's probabilities are then equal, 1 before they are normalised (to
+    2^-24 of the score in the exponent, which the rounding to bf16 takes away), and the output is
+    the values' mean: one rounding to bf16, 2^-8, and the fp32 sums of n <= 3008 values,
+    2 n 2^-24 A < 2^-11 A."""
+    c, reqs, q = make_case(nq, nkv, d, reqs, d + nq, weight, spread=1)
+    rng = np.random.default_rng(40)
+    ch = rng.permutation(d)[:8].reshape(2, 4)
+    same = rng.integers(8, 17, (nkv, d)) * rng.choice([-1, 1], (nkv, d))
+    for _, n, ctx, table in reqs:
+        for i, page in enumerate(table):
+            m = min(16, n + ctx - 16 * i)
+            k = np.repeat(same[:, None].astype(float), m, 1)
+            k[:, :, ch[0]] = rng.choice([224, 240, 256, 288, 320, 352, 384], (nkv, m, 4))
+            k[:, :, ch[1]] = -k[:, :, ch[0]]
+            c.hk[page, :, :m] = encode8(k)
+            c.hks[page] = 2.0 ** -6
+    c.upload()
+    q = np.clip(np.round(q.double().numpy() * 32), -96, 96) / 32
+    big = rng.integers(96, 128, q.shape[:2] + (4,)).astype(float)
+    q[:, :, ch[0]] = q[:, :, ch[1]] = big
+    units = np.abs(q).sum(-1).max() * 16 + 8 * np.abs(big).max() * 384  # at least sum |q k| of any key
+    assert (bf16(q).double().numpy() == q).all() and units < 2.0 ** 24 / 32
+    out, mag, weights, worst = attend_ref(c, nq, reqs, q)
+    assert worst > 250
+    got = run_attn(c, nq, reqs, bf16(q).cuda())[0].double().cpu().numpy()
+    off = np.abs(got - out) - (2.0 ** -8 * np.abs(out) + 2.0 ** -11 * mag)
+    assert off.max() <= 0, f"{off.max():.3e} beyond the bound"
+    if weight:
+        check_weights(c, c.hw, reqs, weights, 16.0)  # exact scores; they and the log-sums are below 16
+
+
 def test_nan_stays_in_its_rows():
     """A NaN key or value reaches the rows that attend to it, of its head, and no others; so does
     an infinite or NaN query."""
