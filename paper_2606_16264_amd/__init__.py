@@ -193,7 +193,8 @@ class CacheF8:
                 raise ValueError(f"{name} must be contiguous, {size} byte(s) per element")
         heads, d = tuple(k_scale.shape), v_pool.shape[2]  # (pages, KV heads), head_dim
         self._dims = heads + (d,)
-        self._device = k_pool.device.index  # None: not on a GPU
+        # None: not on a GPU (its sizes can be asked for, no call takes it)
+        self._device = k_pool.device.index if k_pool.device.type == "cuda" else None
         if self._device is not None:
             import torch
             self._current_device = torch.cuda.current_device
@@ -211,14 +212,15 @@ class CacheF8:
 
     def stream(self, stream):
         """The handle of a stream, by default the current one of the cache's device."""
-        return _stream(stream) if self._device is None or stream is not None \
-            else self._current_stream(self._device)
+        return _stream(stream) if stream is not None else self._current_stream(self._device)
 
     def ptr(self, shape: AttnShape):
         """The C struct, for calls of `shape`."""
         if self._dims != (shape.pool_pages, shape.n_kv_heads, shape.head_dim):
             raise ValueError("the cache is not of this attention shape")
-        if self._device is not None and self._device != self._current_device():
+        if self._device is None:
+            raise ValueError("the cache is not on a GPU")
+        if self._device != self._current_device():
             raise ValueError(f"the cache is on device {self._device}, not the current one")
         return ctypes.byref(self._cache)
 

@@ -200,6 +200,19 @@ def test_binding_checks_sizes():
         mx.mx_kv_evict_f8(mx.EvictBatch([4], [2], [1], [[1]], [[2]]), s, c, Raw(n=3), Raw(), stream=0)
 
 
+def test_binding_refuses_a_cache_in_host_memory():
+    """With valid arguments otherwise: the calls would hand host addresses to a kernel."""
+    s = shape()
+    c, e = cache(s), mx.EvictBatch([4], [2], [1], [[1]], [[2]])
+    bf = lambda *n: torch.zeros(n, dtype=torch.bfloat16)  # noqa: E731
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    for call in (lambda: mx.mx_kv_append_f8(one(), s, bf(4, 2, 64), bf(4, 2, 64), c, stream=0),
+                 lambda: mx.mx_paged_attn_f8(one(), s, bf(4, 4, 64), c, bf(4, 4, 64), ws, stream=0),
+                 lambda: mx.mx_kv_evict_f8(e, s, c, torch.zeros(4, dtype=torch.int32), ws, stream=0)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+
+
 @pytest.mark.parametrize("track", [False, True])
 def test_workspace_bound_covers_batches(track):
     rng = np.random.default_rng(5)
