@@ -187,16 +187,20 @@ class CacheF8:
     the tensors alive."""
 
     def __init__(self, k_pool, v_pool, k_scale, v_scale, weight=None):
-        for name, t, size in (("k_pool", k_pool, 1), ("v_pool", v_pool, 1), ("k_scale", k_scale, 4),
-                              ("v_scale", v_scale, 4), ("weight", weight, 4)):
-            if t is not None and (t.element_size() != size or not t.is_contiguous()):
-                raise ValueError(f"{name} must be contiguous, {size} byte(s) per element")
+        import torch
+        codes, fp32 = (torch.uint8, torch.float8_e4m3fn), (torch.float32,)
+        for name, t, types in (("k_pool", k_pool, codes), ("v_pool", v_pool, codes),
+                               ("k_scale", k_scale, fp32), ("v_scale", v_scale, fp32),
+                               ("weight", weight, fp32)):
+            if t is not None and (t.dtype not in types or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous, of type {_names(types)}")
+        # of the calls' tensors (uint16: the bits of bf16)
+        self._bf16, self._int32 = (torch.bfloat16, torch.uint16), (torch.int32,)
         heads, d = tuple(k_scale.shape), v_pool.shape[2]  # (pages, KV heads), head_dim
         self._dims = heads + (d,)
         # None: not on a GPU (its sizes can be asked for, no call takes it)
         self._device = k_pool.device.index if k_pool.device.type == "cuda" else None
         if self._device is not None:
-            import torch
             self._current_device = torch.cuda.current_device
             self._current_stream = torch._C._cuda_getCurrentRawStream
         if any(t is not None and t.device != k_pool.device for t in (v_pool, k_scale, v_scale, weight)):
@@ -264,14 +268,20 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _check_tensor(cache: CacheF8, name: str, t, n: int, size: int) -> None:
-    """t has n elements; where the cache is on a GPU, of `size` bytes each, on that GPU, in order."""
+def _names(types) -> str:
+    return " or ".join(str(x).replace("torch.", "") for x in types)
+
+
+def _check_tensor(cache: CacheF8, name: str, t, n: int, types=None) -> None:
+    """t has n elements; where the cache is on a GPU, of one of `types` (None: any of one byte),
+    on that GPU, in order."""
     if t.numel() < n:
         raise ValueError(f"{name} has {t.numel()} elements, the call needs {n}")
     device = cache._device
-    if device is not None and (t.get_device() != device or t.element_size() != size
-                               or not t.is_contiguous()):
-        raise ValueError(f"{name} must be contiguous, {size} byte(s) per element, on device {device}")
+    if device is not None and (t.get_device() != device or not t.is_contiguous()
+                               or (t.dtype not in types if types else t.element_size() != 1)):
+        raise ValueError(f"{name} must be contiguous, of type {_names(types or ('uint8',))}, "
+                         f"on device {device}")
 
 
 def _stream(stream) -> Optional[int]:
@@ -360,8 +370,8 @@ def mx_kv_append_f8(batch: Batch, shape: AttnShape, k_new, v_new, cache: CacheF8
                     stream=None) -> None:
     """The new tokens' keys and values into the 8-bit cache."""
     n = batch.T * shape.n_kv_heads * shape.head_dim
-    _check_tensor(cache, "k_new", k_new, n, 2)
-    _check_tensor(cache, "v_new", v_new, n, 2)
+    _check_tensor(cache, "k_new", k_new, n, cache._bf16)
+    _check_tensor(cache, "v_new", v_new, n, cache._bf16)
     _check(_lib.mx_kv_append_f8(batch.ptr, ctypes.byref(shape), _ptr(k_new), _ptr(v_new),
                                 cache.ptr(shape), cache.stream(stream)))
 
@@ -386,9 +396,9 @@ def mx_paged_attn_f8(batch: Batch, shape: AttnShape, q, cache: CacheF8, out, ws,
                      stream=None) -> None:
     """Attention over the 8-bit cache; adds to cache.weight where it has one."""
     n = batch.T * shape.n_q_heads * shape.head_dim
-    _check_tensor(cache, "q", q, n, 2)
-    _check_tensor(cache, "out", out, n, 2)
-    _check_tensor(cache, "ws", ws, 0, 1)
+    _check_tensor(cache, "q", q, n, cache._bf16)
+    _check_tensor(cache, "out", out, n, cache._bf16)
+    _check_tensor(cache, "ws", ws, 0)
     _check(_lib.mx_paged_attn_f8(batch.ptr, ctypes.byref(shape), _ptr(q), cache.ptr(shape), _ptr(out),
                                  _ptr(ws), ws.numel(), cache.stream(stream)))
 
@@ -404,8 +414,8 @@ def mx_kv_evict_f8(batch: EvictBatch, shape: AttnShape, cache: CacheF8, kept, ws
                    stream=None) -> None:
     """Copies the tokens that stay to the destination pages; kept (int32, n_kv_heads *
     batch.total_keep elements) receives their indices."""
-    _check_tensor(cache, "kept", kept, shape.n_kv_heads * batch.total_keep, 4)
-    _check_tensor(cache, "ws", ws, 0, 1)
+    _check_tensor(cache, "kept", kept, shape.n_kv_heads * batch.total_keep, cache._int32)
+    _check_tensor(cache, "ws", ws, 0)
     _check(_lib.mx_kv_evict_f8(batch.R, batch.ptr, ctypes.byref(shape), cache.ptr(shape), _ptr(kept),
                                _ptr(ws), ws.numel(), cache.stream(stream)))
 

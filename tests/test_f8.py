@@ -213,6 +213,61 @@ def test_binding_refuses_a_cache_in_host_memory():
             call()
 
 
+def test_binding_refuses_a_cache_of_other_types():
+    """Types of the right size too, whose bytes would be read as something else."""
+    c = cache(shape())
+    names = ("k_pool", "v_pool", "k_scale", "v_scale", "weight")
+    tensors = dict(zip(names, (c.k_pool, c.v_pool, c.k_scale, c.v_scale, c.weight)))
+    mx.CacheF8(**dict(tensors, k_pool=c.k_pool.view(torch.float8_e4m3fn)))
+    for name in names:
+        wrong = ((torch.int8, torch.bool, torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz)
+                 if "pool" in name else (torch.int32, torch.uint8, torch.float64))
+        for t in wrong:
+            with pytest.raises(ValueError, match=name):
+                mx.CacheF8(**dict(tensors, **{name: torch.zeros(tensors[name].shape, dtype=t)}))
+
+
+class OnGpu:
+    """Stands for a tensor on device 0."""
+
+    def __init__(self, dtype, n=1 << 40):
+        self.dtype, self.n = dtype, n
+
+    def data_ptr(self):
+        raise AssertionError("the call went past its checks")
+
+    def numel(self):
+        return self.n
+
+    def get_device(self):
+        return 0
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return True
+
+
+def test_binding_refuses_tensors_of_other_types():
+    """Types of the right size too.  No launch: each call has one wrong tensor."""
+    s, e = shape(), mx.EvictBatch([4], [2], [1], [[1]], [[2]])
+    c = cache(s)
+    c._device, c._current_device = 0, lambda: 0
+    calls = {
+        "k_new": lambda t: mx.mx_kv_append_f8(one(), s, t, OnGpu(torch.bfloat16), c, stream=0),
+        "v_new": lambda t: mx.mx_kv_append_f8(one(), s, OnGpu(torch.uint16), t, c, stream=0),
+        "q": lambda t: mx.mx_paged_attn_f8(one(), s, t, c, OnGpu(torch.bfloat16), OnGpu(torch.uint8), stream=0),
+        "out": lambda t: mx.mx_paged_attn_f8(one(), s, OnGpu(torch.bfloat16), c, t, OnGpu(torch.uint8), stream=0),
+        "kept": lambda t: mx.mx_kv_evict_f8(e, s, c, t, OnGpu(torch.uint8), stream=0)}
+    for name, call in calls.items():
+        wrong = ((torch.float32, torch.uint32, torch.int64) if name == "kept"
+                 else (torch.float16, torch.int16, torch.float32, torch.uint8))
+        for t in wrong:
+            with pytest.raises(ValueError, match=f"^{name} must"):
+                call(OnGpu(t))
+
+
 @pytest.mark.parametrize("track", [False, True])
 def test_workspace_bound_covers_batches(track):
     rng = np.random.default_rng(5)

@@ -758,6 +758,29 @@ def test_binding_refuses_other_tensors():
     c.check("refused")
 
 
+def test_binding_refuses_other_types_of_the_same_size():
+    """fp16 and int16 for bf16, fp32 for int32: refused before anything runs; the bits of bf16 as
+    uint16 are taken."""
+    c, reqs, q = make_case(4, 2, 64, [(0, 5, 3)], 31, False)
+    b, s, q = batch_of(reqs), c.shape(4), q.cuda()
+    kv = torch.zeros(5, 2, 64, dtype=torch.bfloat16, device="cuda")
+    want, ws = run_attn(c, 4, reqs, q)
+    for t in (torch.float16, torch.int16):
+        for args in ((kv.view(t), kv), (kv, kv.view(t))):
+            with pytest.raises(ValueError):
+                mx.mx_kv_append_f8(b, s, *args, c.mx)
+        for args in ((q.view(t), c.mx, q.clone()), (q, c.mx, q.clone().view(t))):
+            with pytest.raises(ValueError):
+                mx.mx_paged_attn_f8(b, s, *args, ws)
+    e = mx.EvictBatch([8], [4], [1], [reqs[0][3]], [[p for p in range(c.pages) if p not in reqs[0][3]][:1]])
+    with pytest.raises(ValueError):
+        mx.mx_kv_evict_f8(e, s, c.mx, torch.zeros(8, device="cuda"), ws)
+    c.check("refused")
+    out = torch.zeros(q.shape, dtype=torch.uint16, device="cuda")
+    mx.mx_paged_attn_f8(b, s, q.view(torch.uint16), c.mx, out, ws)
+    assert torch.equal(out.view(torch.bfloat16), want)
+
+
 def test_pages_beyond_4_gib():
     """Pages whose byte offsets pass 2^32 in every pool, against the same requests in low pages."""
     nq, nkv, d = 16, 8, 128
