@@ -184,7 +184,10 @@ class Batch:
 class CacheF8:
     """A layer's 8-bit cache: device tensors in the layouts of mx_cache_f8, the pools
     one byte per element (uint8 or float8_e4m3fn), scales and weight float32.  Holds
-    the tensors alive."""
+    the tensors alive, the same ones for good: their addresses are taken once."""
+
+    k_pool, v_pool, k_scale, v_scale, weight = (
+        property(lambda self, i=i: self._tensors[i]) for i in range(5))
 
     def __init__(self, k_pool, v_pool, k_scale, v_scale, weight=None):
         import torch
@@ -210,9 +213,8 @@ class CacheF8:
                                ("weight", weight, heads + (16,))):
             if t is not None and tuple(t.shape) != shape:
                 raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-        self.k_pool, self.v_pool, self.k_scale, self.v_scale = k_pool, v_pool, k_scale, v_scale
-        self.weight = weight
-        self._cache = _CacheF8(*(_ptr(t) for t in (k_pool, v_pool, k_scale, v_scale, weight)))
+        self._tensors = (k_pool, v_pool, k_scale, v_scale, weight)
+        self._cache = _CacheF8(*(_ptr(t) for t in self._tensors))
 
     def stream(self, stream):
         """The handle of a stream, by default the current one of the cache's device."""

@@ -227,6 +227,19 @@ def test_binding_refuses_a_cache_of_other_types():
                 mx.CacheF8(**dict(tensors, **{name: torch.zeros(tensors[name].shape, dtype=t)}))
 
 
+def test_binding_keeps_the_tensors_of_a_cache():
+    """The calls use the addresses taken when the cache was made: a tensor put in the place of one
+    would not be used, and the one it replaces might be freed."""
+    c = cache(shape())
+    for name in ("k_pool", "v_pool", "k_scale", "v_scale", "weight"):
+        t = getattr(c, name)
+        with pytest.raises(AttributeError):
+            setattr(c, name, torch.zeros_like(t))
+        assert getattr(c, name) is t
+        assert t.data_ptr() == getattr(c._cache, name)
+    assert cache(shape(), weight=False).weight is None
+
+
 class OnGpu:
     """Stands for a tensor on device 0."""
 
