@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import conftest
 import paper_2606_16264_amd as mx
 from test_host_runtime import fake_hip, run  # noqa: F401  (fake_hip is a fixture)
 
@@ -124,6 +125,29 @@ def test_append_refuses_a_page_of_two_requests():
     # a shared prefix page that only one of them writes is fine as far as the host sees
     b = mx.Batch([1, 1], [1, 1], [16, 3], [[5, 6], [7]])
     assert append(b, shape(), raw_cache()) in (mx.MX_OK, mx.MX_ERR_HIP)
+
+
+def test_append_takes_pages_of_one_request_each(fake_hip):  # noqa: F811
+    """What the test above checks, on the stand-in runtime, where no kernel runs on the pointers."""
+    r = run(fake_hip, """
+        import ctypes
+        s = mx.attn_shape(4, 2, 64, 64)
+        c = mx._CacheF8(1 << 20, 2 << 20, 3 << 20, 4 << 20, 5 << 20)
+        append = lambda b: mx.lib().mx_kv_append_f8(b.ptr, ctypes.byref(s), A(0), A(1), ctypes.byref(c), None)
+        st = [append(mx.Batch([1, 1], [1, 1], [3, 4], [[5], [5]]))]
+        refused = len(log())
+        st.append(append(mx.Batch([1, 1], [1, 1], [16, 3], [[5, 6], [7]])))
+        print(json.dumps(dict(st=st, refused=refused, launches=[l[0] for l in log()])))
+        """)
+    assert r["st"] == [mx.MX_ERR_INVALID, mx.MX_OK] and r["refused"] == 0
+    assert len(r["launches"]) == 1 and "small_append_f8" in r["launches"][0]
+
+
+def test_invented_pointers_are_kept_from_a_gpu():
+    node = "tests/test_f8.py::test_append_refuses_a_page_of_two_requests"
+    assert conftest.kept_from_a_gpu(node, True) and not conftest.kept_from_a_gpu(node, False)
+    assert not conftest.kept_from_a_gpu("tests/test_f8.py::test_bad_batches[0]", True)
+    assert test_append_refuses_a_page_of_two_requests.__name__ == node.split("::")[1]
 
 
 @pytest.mark.parametrize("args,status", [
