@@ -304,10 +304,13 @@ mx_status mx_kv_append_f8(const mx_batch* batch, const mx_attn_shape* shape,
  * rounded to bf16 for the value products, and for a row's sum where no weight is
  * accumulated, so that an output may differ by such a rounding between a call with weight
  * and one without, and between a decode and a one-token prompt.  A NaN value reaches the
- * rows that attend to its token, and no earlier row of its chunk.  Sizes of the workspace: mx_workspace_bytes_f8_for, with
- * track != 0 where cache->weight is given (it holds the decodes' scores then); its
- * upper bound for any batch of at most max_tokens new tokens, max_reqs requests and
- * max_pages page-table entries in total: mx_workspace_bytes_f8.
+ * rows that attend to its token, and no earlier row of its chunk; weights do not see it.
+ * A NaN key, or a query with a NaN or an infinity, makes its rows' sums NaN: then every
+ * token that such a row attends to has a NaN weight of that KV head, for good.
+ * Sizes of the workspace: mx_workspace_bytes_f8_for, with track != 0 where cache->weight
+ * is given (it holds the decodes' scores then); its upper bound for any batch of at most
+ * max_tokens new tokens, max_reqs requests and max_pages page-table entries in total:
+ * mx_workspace_bytes_f8.
  */
 size_t mx_workspace_bytes_f8_for(const mx_batch* batch, const mx_attn_shape* shape, int32_t track);
 size_t mx_workspace_bytes_f8(const mx_attn_shape* shape, int32_t track, int32_t max_tokens,
@@ -331,7 +334,8 @@ typedef struct {
  * Eviction by accumulated attention weight.  For every request and KV head by itself:
  * the last `recent` tokens stay, and of the others the (keep - recent) with the largest
  * weight (equal weights: the lower index first; a NaN counts as larger than any
- * number).  The tokens that stay are copied, in their order, to tokens 0 .. keep - 1 of
+ * number, and NaNs as equal, so that of a head whose weights are all NaN the first tokens
+ * stay).  The tokens that stay are copied, in their order, to tokens 0 .. keep - 1 of
  * dst_pages, codes, scales and weights; a destination page's scale is the largest of
  * the scales its tokens come from, and codes of a smaller one become
  * code * source / destination scale, rounded to nearest even.  The indices that stay go

@@ -506,6 +506,32 @@ def test_nan_in_split_tiles(weight):
     check_out(got.masked_fill(torch.from_numpy(bad), 0), np.where(bad, 0, exp), mag)
 
 
+@pytest.mark.parametrize("nq,nkv,d", [(8, 2, 128), (4, 4, 64)])
+def test_nan_weights(nq, nkv, d):
+    """A NaN key or a query that is not finite makes the weight of every token that its rows attend
+    to NaN, of that KV head, and no other; a NaN value changes no weight.  Chunks whole and split
+    over their keys, decodes whole and split, more weights added in a second call."""
+    c, reqs, q = make_case(nq, nkv, d, [(0, 40, 3000), (0, 150, 20), (0, 3, 8), (1, 1, 5000), (1, 1, 70),
+                                        (1, 1, 90), (0, 20, 30)], 25, True)
+    group = nq // nkv
+    start = np.cumsum([0] + [r[1] for r in reqs])
+    _, _, weights, worst = attend_ref(c, nq, reqs, q.double().numpy())
+    for r, pos, g in [(0, 700, 1), (1, 100, 0), (3, 4321, 0), (4, 3, 1)]:  # keys
+        table = reqs[r][3]
+        c.hk[table[pos // 16], g, pos % 16, 7] = NAN
+        weights[r][g] = math.nan  # the last row attends to the token, and to all others
+    for r, row, h, x in [(0, 11, 0, math.nan), (2, 1, nq - 1, math.inf), (5, 0, 1, math.nan)]:  # queries
+        q[start[r] + row, h, 5] = x
+        weights[r][h // group, :reqs[r][2] + row + 1] = math.nan
+    for r, pos, g in [(6, 35, 0), (4, 50, 0)]:  # values
+        c.hv[reqs[r][3][pos // 16], g, pos % 16, 9] = 0xFF
+    c.upload()
+    run_attn(c, nq, reqs, q.cuda())
+    before = check_weights(c, c.hw, reqs, weights, worst)
+    run_attn(c, nq, reqs, q.cuda())
+    check_weights(c, before, reqs, weights, worst)
+
+
 def test_shared_prefix_weights_add_up():
     """Requests that read the same cached pages: each key receives the sum over all of them."""
     c, reqs, q = make_case(8, 2, 64, [(1, 1, 90), (0, 33, 64)], 7, True)
