@@ -351,6 +351,28 @@ def test_chunk_weights_without_parts():
     check_weights(c, c.hw, reqs, weights, worst)
 
 
+@pytest.mark.parametrize("weight", [False, True])
+@pytest.mark.parametrize("nq,nkv,d,reqs", [
+    # 8 heads of a tile, 408 and 440 tiles, whole ones of up to 70 chunks; beside decodes
+    (64, 8, 128, [(0, 1 + r % 17, 40 * r % 900) for r in range(44)] + [(0, 70, 4400)]),
+    (64, 8, 128, [(0, 33, 20 * r) for r in range(18)] + [(1, 1, 2100), (0, 9, 2950), (1, 1, 5)]),
+    # one head a tile, 448 tiles; an odd group, 396 tiles
+    (64, 64, 64, [(0, n, x) for n, x in ((3, 0), (1, 17), (16, 1500), (128, 1), (130, 1100), (2, 5))]),
+    (36, 4, 64, [(0, 128, 3), (0, 1, 1700), (0, 4, 60)] + [(0, 5, 10 * r) for r in range(8)]),
+    # 8 and 16 heads of a tile, split over keys
+    (64, 8, 64, [(0, 5, 16500)]), (32, 2, 128, [(0, 200, 9000), (1, 1, 800), (0, 2, 1300)])])
+def test_attention_many_and_wide_tiles(nq, nkv, d, reqs, weight):
+    """More prefill tiles than are split over their keys, long ones among them, and tiles of 8 and
+    more q heads."""
+    c, reqs, q = make_case(nq, nkv, d, reqs, nq + nkv, weight)
+    out, mag, weights, worst = attend_ref(c, nq, reqs, q.double().numpy())
+    got, _ = run_attn(c, nq, reqs, q.cuda())
+    check_out(got, out, mag)
+    if weight:
+        check_weights(c, c.hw, reqs, weights, worst)
+    assert torch.equal(run_attn(c, nq, reqs, q.cuda())[0], got)
+
+
 def test_small_calls_give_what_large_ones_give():
     """The same requests in one call, whose metadata is staged, and one by one, where it goes with
     the kernel's arguments: append, attention and eviction, bit for bit."""
