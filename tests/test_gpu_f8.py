@@ -755,6 +755,56 @@ def test_same_results_on_any_stream_and_thread():
     assert all(torch.equal(r, want) for r in results)
 
 
+def test_streams_and_threads_of_all_calls():
+    """Append, attention with weights and eviction in turn, in small calls and staged ones, by four
+    threads at once, each on a stream and a cache of its own: bit for bit what they give alone."""
+    nq, nkv, d, pages = 8, 2, 128, 1500
+
+    def state(seed):
+        rng = np.random.default_rng(seed)
+        c = Cache(pages, nkv, d, poison=False)
+        R = [3, 120, 5, 90][seed % 4]  # requests; the larger batches' metadata are staged
+        ctx = rng.integers(1, 150, R)
+        ctx[0] = 3000
+        news = np.where(np.arange(R) % 2 == 0, 1, rng.integers(1, 20, R))
+        tabs = tables(rng, pages, [int(n) for n in ctx + news] + [10] * R)
+        for t, n in zip(tabs, ctx):
+            fill(c, rng, t[:-(-int(n) // 16)], int(n))
+        c.upload()
+        reqs = [(i % 2 == 0, int(n), int(x), t) for i, (n, x, t) in enumerate(zip(news, ctx, tabs))]
+        T = int(news.sum())
+        kv = bf16(rng.normal(0, 1, (2, T, nkv, d))).cuda()
+        q = bf16(rng.normal(0, 1, (T, nq, d))).cuda()
+        ev = [(n + x, min(10, n + x), 1, t, tabs[R + i]) for i, (_, n, x, t) in enumerate(reqs)]
+        return c, reqs, kv, q, ev
+
+    def work(s, stream=None):
+        c, reqs, kv, q, ev = s
+        res = []
+        for _ in range(6):
+            mx.mx_kv_append_f8(batch_of(reqs), c.shape(nq), kv[0], kv[1], c.mx, stream=stream)
+            out, ws = run_attn(c, nq, reqs, q, stream=stream)
+            kept, ws2 = run_evict(c, ev, stream=stream)
+            res += [out, kept, ws, ws2]  # (the workspaces stay until the stream is done)
+        return res[0::4] + res[1::4] + [c.k, c.v, c.ks, c.vs, c.w], res
+
+    want = [work(state(i))[0] for i in range(4)]
+    states, got = [state(i) for i in range(4)], [None] * 4
+    torch.cuda.synchronize()
+
+    def thread(i):
+        st = torch.cuda.Stream()
+        with torch.cuda.stream(st):
+            got[i] = work(states[i], st)
+        st.synchronize()
+
+    threads = [threading.Thread(target=thread, args=(i,)) for i in range(4)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    for g, w in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(g[0], w))
+
+
 def test_captured_streams_are_refused():
     c, reqs, q = make_case(4, 2, 64, [(1, 1, 90)], 22, True)
     s, b, q = c.shape(4), batch_of(reqs), q.cuda()
