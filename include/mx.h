@@ -307,6 +307,8 @@ mx_status mx_kv_append_f8(const mx_batch* batch, const mx_attn_shape* shape,
  * rows that attend to its token, and no earlier row of its chunk; weights do not see it.
  * A NaN key, or a query with a NaN or an infinity, makes its rows' sums NaN: then every
  * token that such a row attends to has a NaN weight of that KV head, for good.
+ * out may be q itself where no weight is given; any other overlap of the two is refused
+ * (MX_ERR_INVALID).
  * Sizes of the workspace: mx_workspace_bytes_f8_for, with track != 0 where cache->weight
  * is given (it holds the decodes' scores then); its upper bound for any batch of at most
  * max_tokens new tokens, max_reqs requests and max_pages page-table entries in total:

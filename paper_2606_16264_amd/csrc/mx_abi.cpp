@@ -1544,6 +1544,11 @@ MX_EXPORT mx_status mx_paged_attn_f8(const mx_batch* batch, const mx_attn_shape*
     if ((st = check_aligned({q, out, ws})) != MX_OK) return st;
     if ((st = check_rows(batch, shape)) != MX_OK) return st;
     const bool track = cache->weight != nullptr;
+    // a tile reads the rows and heads that it writes, before; a chunk's weights read all of q after
+    const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(out);
+    const uintptr_t bytes = (uintptr_t)T * shape->n_q_heads * shape->head_dim * 2;
+    if (o0 < q0 + bytes && q0 < o0 + bytes && (o0 != q0 || track))
+      return fail(MX_ERR_INVALID, "out overlaps q");
     PlanF8 f;
     build_plan_f8(batch, shape, track, f);
     const LayoutF8& L = f.L;

@@ -185,6 +185,19 @@ def test_empty_calls_are_no_ops():
     assert mx.mx_workspace_bytes_f8_for(empty, s) > 0
 
 
+@pytest.mark.parametrize("weight", [0x200000, None])
+def test_attention_refuses_an_output_over_the_query(weight):
+    """A chunk's weights read the query again behind its output.  (The calls that are not refused
+    here stop at a workspace too small.)"""
+    c, n = raw_cache(weight=weight), 4 * 4 * 64 * 2
+    for out in (0x100000 - n + 16, 0x100000 - 16, 0x100010, 0x100000 + n - 16):
+        assert attn(one(), shape(), c, out=out, n=255) == mx.MX_ERR_INVALID, hex(out)
+        assert "overlaps" in mx.last_error()
+    assert attn(one(), shape(), c, out=0x100000, n=255) == (mx.MX_ERR_INVALID if weight else mx.MX_ERR_TOO_LARGE)
+    for out in (0x100000 - n, 0x100000 + n):
+        assert attn(one(), shape(), c, out=out, n=255) == mx.MX_ERR_TOO_LARGE
+
+
 def test_rows_of_a_chunk_fit_32_bits():
     """New tokens times the q heads of a KV head are numbered in 32 bits."""
     s = shape(32767, 1, 64, 5000)

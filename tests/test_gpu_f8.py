@@ -351,6 +351,17 @@ def test_chunk_weights_without_parts():
     check_weights(c, c.hw, reqs, weights, worst)
 
 
+def test_output_in_place_of_the_query():
+    """Without weights the output may be the query itself: whole and split decodes and tiles."""
+    for reqs in ([(1, 1, 70), (0, 150, 40), (1, 1, 5000), (0, 20, 3000)], [(0, 33, 10)], [(1, 1, 4000)],
+                 [(0, 70, 64)] + [(1, 1, 9)] * 70):
+        c, reqs, q = make_case(8, 2, 128, reqs, 41, False)
+        q = q.cuda()
+        want, ws = run_attn(c, 8, reqs, q)
+        mx.mx_paged_attn_f8(batch_of(reqs), c.shape(8), q, c.mx, q, ws)
+        assert torch.equal(q, want)
+
+
 @pytest.mark.parametrize("weight", [False, True])
 @pytest.mark.parametrize("nq,nkv,d,reqs", [
     # 8 heads of a tile, 408 and 440 tiles, whole ones of up to 70 chunks; beside decodes
