@@ -246,6 +246,65 @@ mx_status mx_layer_step(const mx_batch* batch, const mx_layer_cfg* cfg, const vo
                         const uint16_t* x, uint16_t* y, uint16_t* k_pool, uint16_t* v_pool,
                         void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------- attention over parts of the keys
+ *
+ * Two forms of mx_paged_attn, over the bf16 cache, for batches of either phase.  Both keep
+ * its conventions (batch, pools, rounding of the probabilities to bf16, splits that are
+ * merged in a fixed order: bit-identical from run to run) and differ as follows.  They read
+ * host staging buffers, or hand their metadata over with the launch, and refuse a stream
+ * that is being captured into a graph (MX_ERR_UNSUPPORTED).  out may be q itself; any other
+ * overlap of the two is refused (MX_ERR_INVALID).  A key or value reaches the rows that see
+ * its token, and no other: what masked slots hold (NaN and infinities among it) stays out.
+ *
+ * mx_paged_attn_window: a sliding window and sinks.  The token at position p sees the
+ * positions j <= p with j > p - window or j < sinks:
+ *   out[t][h] = sum_j softmax_j(scale * q[t][h] . K_r[j][g]) V_r[j][g] over those j.
+ * window >= 1 and sinks >= 0, else MX_ERR_INVALID; with window > p every key is seen.  Page
+ * table entries of pages in which no new token of the call sees a position are neither
+ * checked nor read (they may hold anything: pages that have left the window can be freed and
+ * used again); the table's length is as for mx_paged_attn.
+ * Workspace: mx_workspace_bytes_window_for, and for any batch of at most max_tokens new
+ * tokens, max_reqs requests and max_pages page-table entries in total
+ * mx_workspace_bytes_window.
+ */
+size_t mx_workspace_bytes_window_for(const mx_batch* batch, const mx_attn_shape* shape,
+                                     int32_t window, int32_t sinks);
+size_t mx_workspace_bytes_window(const mx_attn_shape* shape, int32_t max_tokens, int32_t max_reqs,
+                                 int64_t max_pages);
+mx_status mx_paged_attn_window(const mx_batch* batch, const mx_attn_shape* shape, int32_t window,
+                               int32_t sinks, const uint16_t* q, const uint16_t* k_pool,
+                               const uint16_t* v_pool, uint16_t* out, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+
+/*
+ * mx_paged_attn_shared: mx_paged_attn for a batch whose requests share pages of their
+ * caches.  A run says that requests first_req .. first_req + num_reqs - 1 hold the same
+ * n_pages pages, behind the pages of the runs before it that they belong to: the first
+ * run of a request starts at its page 0, its next one where that ends, and so on (a system
+ * prompt shared by all, examples shared by some).  The keys and values of a run are read
+ * once for all of its requests (a prompt chunk that fills its tiles by itself reads them
+ * for its own rows).  The result is mx_paged_attn's up to the order of sums and the
+ * rounding of the probabilities.
+ * MX_ERR_INVALID where a run has no request or no page, names a request that is not there,
+ * has requests that differ in where it starts or in the pages' ids, or reaches past the
+ * cached tokens of one (16 * pages <= ctx_len).
+ * Workspace: mx_workspace_bytes_shared_for, and for any batch within the bounds above whose
+ * requests belong to at most max_depth runs each mx_workspace_bytes_shared.
+ */
+typedef struct {
+  int32_t first_req, num_reqs; /* the requests that share it */
+  int32_t n_pages;             /* >= 1 */
+} mx_shared_run;
+
+size_t mx_workspace_bytes_shared_for(const mx_batch* batch, const mx_attn_shape* shape,
+                                     int32_t num_runs, const mx_shared_run* runs);
+size_t mx_workspace_bytes_shared(const mx_attn_shape* shape, int32_t max_tokens, int32_t max_reqs,
+                                 int64_t max_pages, int32_t max_depth);
+mx_status mx_paged_attn_shared(const mx_batch* batch, const mx_attn_shape* shape, int32_t num_runs,
+                               const mx_shared_run* runs, const uint16_t* q, const uint16_t* k_pool,
+                               const uint16_t* v_pool, uint16_t* out, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+
 /* ---------------------------------------------------------------- 8-bit cache
  *
  * A layer's keys and values in 8 bits: twice the tokens in the same memory, half

@@ -33,6 +33,8 @@ EXPORTED = [
     "mx_debug_reduce_residual_rmsnorm", "mx_paged_attn_static", "mx_paged_attn_static_max_bytes",
     "mx_profile_enable", "mx_profile_read", "mx_kv_append_f8", "mx_workspace_bytes_f8_for",
     "mx_workspace_bytes_f8", "mx_paged_attn_f8", "mx_kv_evict_f8_ws_bytes", "mx_kv_evict_f8",
+    "mx_workspace_bytes_window_for", "mx_workspace_bytes_window", "mx_paged_attn_window",
+    "mx_workspace_bytes_shared_for", "mx_workspace_bytes_shared", "mx_paged_attn_shared",
 ]
 
 
@@ -73,6 +75,11 @@ class _EvictRequest(ctypes.Structure):
                 ("dst_pages", ctypes.POINTER(ctypes.c_int32))]
 
 
+class _SharedRun(ctypes.Structure):
+    _fields_ = [("first_req", ctypes.c_int32), ("num_reqs", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32)]
+
+
 class _Weights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("ln1_g", "w_qkv", "w_o", "ln2_g", "w_gate_up", "w_down")]
 
@@ -93,6 +100,7 @@ def _load() -> ctypes.CDLL:
     SP = ctypes.POINTER(AttnShape)
     CP = ctypes.POINTER(LayerCfg)
     FP, EP = ctypes.POINTER(_CacheF8), ctypes.POINTER(_EvictRequest)
+    RP = ctypes.POINTER(_SharedRun)
     sig = {
         "mx_status_str": ([ctypes.c_int], ctypes.c_char_p),
         "mx_last_error": ([], ctypes.c_char_p),
@@ -113,6 +121,12 @@ def _load() -> ctypes.CDLL:
         "mx_paged_attn_f8": ([BP, SP, P, FP, P, P, SZ, P], ctypes.c_int),
         "mx_kv_evict_f8_ws_bytes": ([I32, EP, SP], SZ),
         "mx_kv_evict_f8": ([I32, EP, SP, FP, P, P, SZ, P], ctypes.c_int),
+        "mx_workspace_bytes_window_for": ([BP, SP, I32, I32], SZ),
+        "mx_workspace_bytes_window": ([SP, I32, I32, I64], SZ),
+        "mx_paged_attn_window": ([BP, SP, I32, I32, P, P, P, P, P, SZ, P], ctypes.c_int),
+        "mx_workspace_bytes_shared_for": ([BP, SP, I32, RP], SZ),
+        "mx_workspace_bytes_shared": ([SP, I32, I32, I64, I32], SZ),
+        "mx_paged_attn_shared": ([BP, SP, I32, RP, P, P, P, P, P, SZ, P], ctypes.c_int),
         "mx_layer_workspace_offsets": ([BP, CP, ctypes.POINTER(SZ)], ctypes.c_int),
         "mx_debug_token_map": ([BP, SP, P, P, P, P, SZ, P], ctypes.c_int),
         "mx_debug_gather": ([BP, SP, I32, P, P, P, P, P, SZ, P], ctypes.c_int),
@@ -256,6 +270,19 @@ class EvictBatch:
         return self._reqs
 
 
+class SharedRuns:
+    """Runs of pages that requests of a batch share, in the C layout: (first request,
+    requests, pages) each, outer runs first."""
+
+    def __init__(self, runs: Sequence[Sequence[int]]):
+        self._runs = (_SharedRun * max(len(runs), 1))(*((int(a), int(n), int(k)) for a, n, k in runs))
+        self.n = len(runs)
+
+    @property
+    def ptr(self):
+        return self._runs
+
+
 def attn_shape(n_q_heads, n_kv_heads, head_dim, pool_pages, scale=0.0, page_size=16) -> AttnShape:
     return AttnShape(n_q_heads, n_kv_heads, head_dim, page_size, int(pool_pages), float(scale))
 
@@ -277,13 +304,47 @@ def _names(types) -> str:
 def _check_tensor(cache: CacheF8, name: str, t, n: int, types=None) -> None:
     """t has n elements; where the cache is on a GPU, of one of `types` (None: any of one byte),
     on that GPU, in order."""
+    _check_tensor_on(cache._device, name, t, n, types)
+
+
+def _check_tensor_on(device: Optional[int], name: str, t, n: int, types=None) -> None:
     if t.numel() < n:
         raise ValueError(f"{name} has {t.numel()} elements, the call needs {n}")
-    device = cache._device
     if device is not None and (t.get_device() != device or not t.is_contiguous()
                                or (t.dtype not in types if types else t.element_size() != 1)):
         raise ValueError(f"{name} must be contiguous, of type {_names(types or ('uint8',))}, "
                          f"on device {device}")
+
+
+def _size(n: int) -> int:
+    if n == 0:
+        raise MxError(MX_ERR_INVALID, last_error())
+    return int(n)
+
+
+def _check_attn(batch: Batch, shape: AttnShape, q, k_pool, v_pool, out, ws) -> int:
+    """The tensors of an attention call over the bf16 cache: bf16 (or its bits), contiguous, large
+    enough, on one GPU that is the current one; its index."""
+    import torch
+    device = q.get_device()
+    if device < 0:
+        raise ValueError("q is not on a GPU")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"q is on device {device}, not the current one")
+    bf16 = (torch.bfloat16, torch.uint16)
+    rows = batch.T * shape.n_q_heads * shape.head_dim
+    pool = shape.pool_pages * shape.n_kv_heads * shape.head_dim * shape.page_size
+    _check_tensor_on(device, "q", q, rows, bf16)
+    _check_tensor_on(device, "k_pool", k_pool, pool, bf16)
+    _check_tensor_on(device, "v_pool", v_pool, pool, bf16)
+    _check_tensor_on(device, "out", out, rows, bf16)
+    _check_tensor_on(device, "ws", ws, 0)
+    return device
+
+
+def _stream_of(device: int, stream) -> Optional[int]:
+    import torch
+    return _stream(stream) if stream is not None else torch._C._cuda_getCurrentRawStream(device)
 
 
 def _stream(stream) -> Optional[int]:
@@ -420,6 +481,45 @@ def mx_kv_evict_f8(batch: EvictBatch, shape: AttnShape, cache: CacheF8, kept, ws
     _check_tensor(cache, "ws", ws, 0)
     _check(_lib.mx_kv_evict_f8(batch.R, batch.ptr, ctypes.byref(shape), cache.ptr(shape), _ptr(kept),
                                _ptr(ws), ws.numel(), cache.stream(stream)))
+
+
+def mx_workspace_bytes_window_for(batch: Batch, shape: AttnShape, window: int, sinks: int = 0) -> int:
+    """Workspace of mx_paged_attn_window for this batch."""
+    return _size(_lib.mx_workspace_bytes_window_for(batch.ptr, ctypes.byref(shape), window, sinks))
+
+
+def mx_workspace_bytes_window(shape: AttnShape, max_tokens: int, max_reqs: int, max_pages: int) -> int:
+    return _size(_lib.mx_workspace_bytes_window(ctypes.byref(shape), max_tokens, max_reqs, max_pages))
+
+
+def mx_paged_attn_window(batch: Batch, shape: AttnShape, window: int, sinks: int, q, k_pool, v_pool,
+                         out, ws, stream=None) -> None:
+    """Attention in which a token sees the last `window` positions up to its own and the
+    first `sinks`; table entries of pages that no new token sees are not looked at."""
+    device = _check_attn(batch, shape, q, k_pool, v_pool, out, ws)
+    _check(_lib.mx_paged_attn_window(batch.ptr, ctypes.byref(shape), window, sinks, _ptr(q),
+                                     _ptr(k_pool), _ptr(v_pool), _ptr(out), _ptr(ws), ws.numel(),
+                                     _stream_of(device, stream)))
+
+
+def mx_workspace_bytes_shared_for(batch: Batch, shape: AttnShape, runs: SharedRuns) -> int:
+    """Workspace of mx_paged_attn_shared for this batch and these runs."""
+    return _size(_lib.mx_workspace_bytes_shared_for(batch.ptr, ctypes.byref(shape), runs.n, runs.ptr))
+
+
+def mx_workspace_bytes_shared(shape: AttnShape, max_tokens: int, max_reqs: int, max_pages: int,
+                              max_depth: int) -> int:
+    return _size(_lib.mx_workspace_bytes_shared(ctypes.byref(shape), max_tokens, max_reqs, max_pages,
+                                                max_depth))
+
+
+def mx_paged_attn_shared(batch: Batch, shape: AttnShape, runs: SharedRuns, q, k_pool, v_pool, out, ws,
+                         stream=None) -> None:
+    """mx_paged_attn where requests share runs of pages, whose keys are read once."""
+    device = _check_attn(batch, shape, q, k_pool, v_pool, out, ws)
+    _check(_lib.mx_paged_attn_shared(batch.ptr, ctypes.byref(shape), runs.n, runs.ptr, _ptr(q),
+                                     _ptr(k_pool), _ptr(v_pool), _ptr(out), _ptr(ws), ws.numel(),
+                                     _stream_of(device, stream)))
 
 
 def mx_layer_workspace_offsets(batch: Batch, cfg: LayerCfg) -> dict:

@@ -17,7 +17,9 @@
 #include <vector>
 
 #include "mx.h"
+#include "attention_span.h"
 #include "mx_kernels.h"
+#include "span_plan.h"
 
 #define MX_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -110,7 +112,10 @@ mx_status duplicate_slot(const mx_batch* b, int64_t T) {
               it == slots.end() ? -1ll : (long long)*it);
 }
 
-mx_status validate_batch(const mx_batch* b, const mx_attn_shape* s, int64_t* T_out) {
+// (window > 0: only the pages that a new token sees through the window and the sinks are
+// looked at)
+mx_status validate_batch(const mx_batch* b, const mx_attn_shape* s, int64_t* T_out, int32_t window = 0,
+                         int32_t sinks = 0) {
   if (!b) return fail(MX_ERR_NULL, "batch is NULL");
   mx_status st = validate_shape(s);
   if (st != MX_OK) return st;
@@ -134,13 +139,18 @@ mx_status validate_batch(const mx_batch* b, const mx_attn_shape* s, int64_t* T_o
     if (!q.pages) return fail(MX_ERR_NULL, "request %d: pages is NULL", r);
     // one branch-free pass over the ids (a negative one is a large unsigned one)
     const uint32_t limit = (uint32_t)std::min<int64_t>(s->pool_pages, (int64_t)1 << 31);
+    SeenPages seen{0, 0, q.n_pages};
+    if (window > 0) seen = seen_pages(q.ctx_len, q.n_new, window, sinks);
     bool bad = s->pool_pages < 0;
-    for (int i = 0; i < q.n_pages; i++) bad |= (uint32_t)q.pages[i] >= limit;
+    for (int i = 0; i < seen.sink_pages; i++) bad |= (uint32_t)q.pages[i] >= limit;
+    for (int i = seen.sink_pages + seen.skip; i < seen.end; i++) bad |= (uint32_t)q.pages[i] >= limit;
     if (bad)
-      for (int i = 0; i < q.n_pages; i++)
+      for (int i = 0; i < seen.end; i++) {
+        if (i == seen.sink_pages) i += seen.skip;
         if (q.pages[i] < 0 || q.pages[i] >= s->pool_pages)
           return fail(MX_ERR_INVALID, "request %d: page id %d outside [0, %lld)", r, q.pages[i],
                       (long long)s->pool_pages);
+      }
     touched += (kv_len - 1) / 16 - q.ctx_len / 16 + 1;
     T += q.n_new;
     if (T > INT32_MAX / 2) return fail(MX_ERR_TOO_LARGE, "too many tokens");
@@ -1717,6 +1727,257 @@ MX_EXPORT mx_status mx_kv_evict_f8(int32_t num_reqs, const mx_evict_request* req
     });
     if (e != hipSuccess) return hip_fail(e, "eviction launch");
     return MX_OK;
+  });
+}
+
+// ------------------------------------------------------------------ parts of the keys
+namespace {
+
+struct LayoutSpan {
+  size_t rows = 0, pages = 0, tokens = 0, items = 0, merge_tokens = 0, merges = 0, sources = 0,
+         meta_end = 0, part_o = 0, part_ml = 0, total = 0;
+};
+LayoutSpan make_layout_span(int64_t n_rows, int64_t n_pages, int64_t n_tokens, int64_t n_items,
+                            int64_t n_merge_tokens, int64_t n_merges, int64_t n_sources,
+                            int64_t n_parts, int head_dim) {
+  LayoutSpan L;
+  size_t o = 0;
+  auto take = [&](int64_t n, size_t size) {
+    const size_t at = o;
+    o = (o + n * size + 15) / 16 * 16;
+    return at;
+  };
+  L.rows = take(n_rows, sizeof(SpanRows));
+  L.items = take(n_items, sizeof(SpanItem));
+  L.pages = take(n_pages, sizeof(int32_t));
+  L.tokens = take(n_tokens, sizeof(int32_t));
+  L.merge_tokens = take(n_merge_tokens, sizeof(SpanToken));
+  L.merges = take(n_merges, sizeof(SpanMerge));
+  L.sources = take(n_sources, sizeof(SpanSource));
+  L.meta_end = o;
+  o = align_up(o);
+  L.part_o = o; o = align_up(o + n_parts * head_dim * 4);
+  L.part_ml = o; o = align_up(o + n_parts * 8);
+  L.total = std::max(o, kAlign);
+  return L;
+}
+LayoutSpan layout_span(const SpanPlan& p, const mx_attn_shape* s) {
+  return make_layout_span((int64_t)p.rows.size(), p.n_pages, (int64_t)p.tokens.size(),
+                          (int64_t)p.items.size(), (int64_t)p.merge_tokens.size(),
+                          (int64_t)p.merges.size(), (int64_t)p.sources.size(), p.n_parts, s->head_dim);
+}
+
+// The bound for requests that belong to at most `depth` runs each: every request has a part
+// of its own, and belongs to that many others.
+size_t span_bound(const mx_attn_shape* s, int32_t max_tokens, int32_t max_reqs, int64_t max_pages,
+                  int32_t depth) {
+  if (validate_shape(s) != MX_OK) return 0;
+  if (max_tokens < 0 || max_reqs < 0 || max_pages < 0 || depth < 0) {
+    fail(MX_ERR_INVALID, "negative bound");
+    return 0;
+  }
+  const int64_t nkv = s->n_kv_heads, group = s->n_q_heads / nkv;
+  const int64_t parts = (int64_t)max_reqs * (depth + 1), tokens = (int64_t)max_tokens * (depth + 1);
+  const int64_t streams = max_pages / plan::kMinSplitPages + parts;
+  const int64_t items = streams * nkv * ceil_div(group, 16) +
+                        (ceil_div(tokens * group, kSpanTileRows) + parts) * nkv + plan::kExtraTiles;
+  return make_layout_span(parts, max_pages, tokens, items, max_tokens, max_reqs, parts,
+                          streams * nkv * std::max<int64_t>(16, group) + tokens * s->n_q_heads +
+                              (int64_t)plan::kExtraTiles * kSpanTileRows,
+                          s->head_dim)
+      .total;
+}
+
+mx_status validate_window(int32_t window, int32_t sinks) {
+  if (window < 1) return fail(MX_ERR_INVALID, "window %d < 1", window);
+  if (sinks < 0) return fail(MX_ERR_INVALID, "sinks %d < 0", sinks);
+  return MX_OK;
+}
+
+mx_status validate_runs(const mx_batch* b, int32_t num_runs, const mx_shared_run* runs) {
+  if (num_runs < 0) return fail(MX_ERR_INVALID, "num_runs %d < 0", num_runs);
+  if (num_runs > 0 && !runs) return fail(MX_ERR_NULL, "runs is NULL");
+  std::vector<int64_t> start(b->num_reqs, 0);
+  for (int i = 0; i < num_runs; i++) {
+    const mx_shared_run& run = runs[i];
+    if (run.num_reqs < 1 || run.n_pages < 1)
+      return fail(MX_ERR_INVALID, "run %d: %d requests, %d pages", i, run.num_reqs, run.n_pages);
+    if (run.first_req < 0 || (int64_t)run.first_req + run.num_reqs > b->num_reqs)
+      return fail(MX_ERR_INVALID, "run %d: requests %d .. %lld of %d", i, run.first_req,
+                  (long long)run.first_req + run.num_reqs - 1, b->num_reqs);
+    const int64_t first = start[run.first_req];
+    const mx_request& lead = b->reqs[run.first_req];
+    for (int r = run.first_req; r < run.first_req + run.num_reqs; r++) {
+      const mx_request& q = b->reqs[r];
+      if (start[r] != first)
+        return fail(MX_ERR_INVALID, "run %d starts at page %lld of request %d, at %lld of request %d", i,
+                    (long long)first, run.first_req, (long long)start[r], r);
+      if (16 * (first + run.n_pages) > q.ctx_len)
+        return fail(MX_ERR_INVALID, "run %d ends at page %lld, request %d has %d cached tokens", i,
+                    (long long)first + run.n_pages, r, q.ctx_len);
+      if (memcmp(lead.pages + first, q.pages + first, (size_t)run.n_pages * sizeof(int32_t)))
+        return fail(MX_ERR_INVALID, "run %d: requests %d and %d differ in their pages", i, run.first_req, r);
+      start[r] = first + run.n_pages;
+    }
+  }
+  return MX_OK;
+}
+
+mx_status check_span_plan(const SpanPlan& p) {
+  if (p.n_parts > INT32_MAX || p.n_pages > INT32_MAX || p.items.size() > (size_t)INT32_MAX)
+    return fail(MX_ERR_TOO_LARGE, "%lld partial rows, %zu work items", (long long)p.n_parts, p.items.size());
+  return MX_OK;
+}
+
+void pack_meta_span(const SpanPlan& p, const LayoutSpan& L, char* h) {
+  auto put = [&](size_t at, const auto& v) {
+    if (!v.empty()) memcpy(h + at, v.data(), v.size() * sizeof(v[0]));
+  };
+  put(L.rows, p.rows);
+  put(L.items, p.items);
+  int32_t* pages = (int32_t*)(h + L.pages);
+  for (const SpanPlan::Table& t : p.tables) {
+    memcpy(pages, t.pages, (size_t)t.n * sizeof(int32_t));
+    pages += t.n;
+  }
+  put(L.tokens, p.tokens);
+  put(L.merge_tokens, p.merge_tokens);
+  put(L.merges, p.merges);
+  put(L.sources, p.sources);
+}
+
+// The call of a planned batch: upload, items, merge.
+mx_status span_attn(const char* tag, const SpanPlan& p, const mx_attn_shape* s, const uint16_t* q,
+                    const uint16_t* k_pool, const uint16_t* v_pool, uint16_t* out, void* ws,
+                    size_t ws_bytes, hipStream_t stream) {
+  mx_status st = check_span_plan(p);
+  if (st != MX_OK) return st;
+  const LayoutSpan L = layout_span(p, s);
+  if (!ws) return fail(MX_ERR_NULL, "workspace is NULL");
+  if (ws_bytes < L.total)
+    return fail(MX_ERR_TOO_LARGE, "workspace %zu bytes < %zu needed", ws_bytes, L.total);
+  if ((st = check_not_capturing(stream)) != MX_OK) return st;
+  SpanParams a = {};
+  a.a.q = q;
+  a.a.q_tok_stride = a.a.out_tok_stride = (int64_t)s->n_q_heads * s->head_dim;
+  a.a.k_pool = k_pool;
+  a.a.v_pool = v_pool;
+  a.a.out = out;
+  a.a.pages = at<int32_t>(ws, L.pages);
+  a.a.part_o = at<float>(ws, L.part_o);
+  a.a.part_ml = at<float>(ws, L.part_ml);
+  a.a.nq = s->n_q_heads;
+  a.a.nkv = s->n_kv_heads;
+  a.a.group = p.group;
+  a.a.scale_log2 = eff_scale(s) * 1.4426950408889634f;
+  a.rows = at<SpanRows>(ws, L.rows);
+  a.items = at<SpanItem>(ws, L.items);
+  a.tokens = at<int32_t>(ws, L.tokens);
+  a.window = p.window;
+  a.sinks = p.sinks;
+  st = staged(
+      L.meta_end, stream, [&](char* h) { pack_meta_span(p, L, h); },
+      [&](const void* dev) { return launch_upload(dev, ws, L.meta_end, stream); });
+  if (st != MX_OK) return st;
+  const hipError_t e = timed(tag, stream, [&] {
+    return launch_span_attn(a, (int)p.items.size(), p.has_tiles, at<SpanToken>(ws, L.merge_tokens),
+                            (int)p.merge_tokens.size(), p.most_parts > 8, at<SpanMerge>(ws, L.merges),
+                            at<SpanSource>(ws, L.sources), s->head_dim, stream);
+  });
+  return e == hipSuccess ? MX_OK : hip_fail(e, "attention launch");
+}
+
+// The checks of the two calls' tensors.
+mx_status check_span_tensors(const mx_attn_shape* s, int64_t T, const uint16_t* q,
+                             const uint16_t* k_pool, const uint16_t* v_pool, const uint16_t* out,
+                             const void* ws) {
+  if (!q || !k_pool || !v_pool || !out) return fail(MX_ERR_NULL, "tensor pointer is NULL");
+  const mx_status st = check_aligned({q, k_pool, v_pool, out, ws});
+  if (st != MX_OK) return st;
+  // an item reads the rows and heads that it writes, before
+  const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(out);
+  const uintptr_t bytes = (uintptr_t)T * s->n_q_heads * s->head_dim * 2;
+  if (o0 != q0 && o0 < q0 + bytes && q0 < o0 + bytes) return fail(MX_ERR_INVALID, "out overlaps q");
+  return MX_OK;
+}
+
+}  // namespace
+
+MX_EXPORT size_t mx_workspace_bytes_window_for(const mx_batch* batch, const mx_attn_shape* shape,
+                                               int32_t window, int32_t sinks) {
+  g_err.clear();
+  return no_throw((size_t)0, [&]() -> size_t {
+    if (validate_window(window, sinks) != MX_OK ||
+        validate_batch(batch, shape, nullptr, window, sinks) != MX_OK || check_rows(batch, shape) != MX_OK)
+      return 0;
+    SpanPlan p;
+    plan_window(batch, shape, window, sinks, p);
+    return check_span_plan(p) == MX_OK ? layout_span(p, shape).total : 0;
+  });
+}
+
+MX_EXPORT size_t mx_workspace_bytes_window(const mx_attn_shape* shape, int32_t max_tokens,
+                                           int32_t max_reqs, int64_t max_pages) {
+  g_err.clear();
+  return span_bound(shape, max_tokens, max_reqs, max_pages, 0);
+}
+
+MX_EXPORT mx_status mx_paged_attn_window(const mx_batch* batch, const mx_attn_shape* shape,
+                                         int32_t window, int32_t sinks, const uint16_t* q,
+                                         const uint16_t* k_pool, const uint16_t* v_pool,
+                                         uint16_t* out, void* ws, size_t ws_bytes,
+                                         hipStream_t stream) {
+  g_err.clear();
+  return no_throw(MX_ERR_TOO_LARGE, [&]() -> mx_status {
+    mx_status st = validate_window(window, sinks);
+    if (st != MX_OK) return st;
+    int64_t T;
+    if ((st = validate_batch(batch, shape, &T, window, sinks)) != MX_OK) return st;
+    if (T == 0) return MX_OK;
+    if ((st = check_span_tensors(shape, T, q, k_pool, v_pool, out, ws)) != MX_OK) return st;
+    if ((st = check_rows(batch, shape)) != MX_OK) return st;
+    SpanPlan p;
+    plan_window(batch, shape, window, sinks, p);
+    return span_attn("paged_attn_window", p, shape, q, k_pool, v_pool, out, ws, ws_bytes, stream);
+  });
+}
+
+MX_EXPORT size_t mx_workspace_bytes_shared_for(const mx_batch* batch, const mx_attn_shape* shape,
+                                               int32_t num_runs, const mx_shared_run* runs) {
+  g_err.clear();
+  return no_throw((size_t)0, [&]() -> size_t {
+    if (validate_batch(batch, shape, nullptr) != MX_OK || check_rows(batch, shape) != MX_OK ||
+        validate_runs(batch, num_runs, runs) != MX_OK)
+      return 0;
+    SpanPlan p;
+    plan_shared(batch, shape, num_runs, runs, p);
+    return check_span_plan(p) == MX_OK ? layout_span(p, shape).total : 0;
+  });
+}
+
+MX_EXPORT size_t mx_workspace_bytes_shared(const mx_attn_shape* shape, int32_t max_tokens,
+                                           int32_t max_reqs, int64_t max_pages, int32_t max_depth) {
+  g_err.clear();
+  return span_bound(shape, max_tokens, max_reqs, max_pages, max_depth);
+}
+
+MX_EXPORT mx_status mx_paged_attn_shared(const mx_batch* batch, const mx_attn_shape* shape,
+                                         int32_t num_runs, const mx_shared_run* runs,
+                                         const uint16_t* q, const uint16_t* k_pool,
+                                         const uint16_t* v_pool, uint16_t* out, void* ws,
+                                         size_t ws_bytes, hipStream_t stream) {
+  g_err.clear();
+  return no_throw(MX_ERR_TOO_LARGE, [&]() -> mx_status {
+    int64_t T;
+    mx_status st = validate_batch(batch, shape, &T);
+    if (st != MX_OK) return st;
+    if ((st = validate_runs(batch, num_runs, runs)) != MX_OK) return st;
+    if (T == 0) return MX_OK;
+    if ((st = check_span_tensors(shape, T, q, k_pool, v_pool, out, ws)) != MX_OK) return st;
+    if ((st = check_rows(batch, shape)) != MX_OK) return st;
+    SpanPlan p;
+    plan_shared(batch, shape, num_runs, runs, p);
+    return span_attn("paged_attn_shared", p, shape, q, k_pool, v_pool, out, ws, ws_bytes, stream);
   });
 }
 
