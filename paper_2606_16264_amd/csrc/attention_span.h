@@ -11,12 +11,19 @@ struct SpanParams {
   const SpanRows* rows;
   const SpanItem* items;
   const int32_t* tokens;
+  const SpanToken* merge_tokens;
+  const SpanMerge* merges;
+  const SpanSource* sources;
   int32_t window, sinks;
+  int32_t n_items;    // of each KV head
+  int32_t heads;      // of a group (span_block)
+  uint32_t group_inv; // 2^32 / group, rounded up (group > 1)
 };
 
-// The items, then the merge of `n_merge` tokens (wide: by a workgroup for each q head).
-hipError_t launch_span_attn(const SpanParams& p, int n_items, bool tiles, const SpanToken* merge,
-                            int n_merge, bool wide, const SpanMerge* merges,
-                            const SpanSource* sources, int head_dim, hipStream_t stream);
+// The items of every head, then the merge of n_merge tokens whose rows have up to
+// most_parts partials.  meta, where given, holds the metadata (the pointers into it are
+// offsets there), handed over with the kernels' arguments.
+hipError_t launch_span_attn(const SpanParams& p, const InlineMeta* meta, bool tiles, int n_merge,
+                            int most_parts, int head_dim, hipStream_t stream);
 
 }  // namespace mx

@@ -28,22 +28,19 @@ __device__ __forceinline__ RowState span_row_start() { return RowState{kLowest, 
 
 // Where an item's pages lie, and what a position sees of them.
 struct Span {
-  int sink_pages, skip_table, skip_real, page_end, window, sinks;
-  __device__ __forceinline__ Span(const SpanParams& p, const SpanItem& it, const SpanRows& rw)
-      : sink_pages(rw.sink_pages), skip_table(it.skip), skip_real(it.skip + rw.skip),
-        page_end(it.page_end), window(p.window), sinks(p.sinks) {}
+  int sink_pages, skip_table, skip_real, page0, page_end, window, sinks;
+  __device__ __forceinline__ Span(const SpanParams& p, const SpanPages& pg, const SpanRows& rw)
+      : sink_pages(rw.sink_pages), skip_table(pg.skip), skip_real(pg.skip + rw.skip), page0(pg.page0),
+        page_end(pg.page1), window(p.window), sinks(p.sinks) {}
   __device__ __forceinline__ int entry(int v) const { return v < sink_pages ? v : v + skip_table; }
   __device__ __forceinline__ int first_key(int v) const {  // of page v, as a position
     return 16 * (v < sink_pages ? v : v + skip_real);
   }
-  __device__ __forceinline__ bool sees(int pos, int key) const {
-    return key <= pos && (key < sinks || key > pos - window);
-  }
-  // pages v and v + 1 are in the item, and all their keys seen from pos0 .. pos1
-  __device__ __forceinline__ bool all_seen(int v, int pos0, int pos1) const {
+  // pages v and v + 1 are in the item, and all their keys seen from pos
+  __device__ __forceinline__ bool all_seen(int v, int pos) const {
     if (v + 1 >= page_end) return false;
     const int first = first_key(v), last = first_key(v + 1) + 15;
-    return last <= pos0 && (first > pos1 - window || last < sinks);
+    return last <= pos && (first > pos - window || last < sinks);
   }
   // some key of the pages may be seen from pos0 .. pos1
   __device__ __forceinline__ bool some_seen(int v, int pos0, int pos1) const {
@@ -52,23 +49,27 @@ struct Span {
   }
 };
 
-// Which of the lane group's eight keys (all of one page) the row at pos sees, as bits.
+// Which of the lane group's eight keys of pages v0 and v0 + 1 (all of one page) the row at
+// pos sees, as bits.
 __device__ __forceinline__ unsigned seen_keys(const Span& s, int v0, int pos, int g4) {
   const int v = v0 + (g4 >> 1);
-  if (v >= s.page_end) return 0;
   const int j0 = s.first_key(v) + 8 * (g4 & 1);
-  unsigned m = 0;
-#pragma unroll
-  for (int e = 0; e < 8; e++) m |= s.sees(pos, j0 + e) ? 1u << e : 0u;
-  return m;
+  auto below = [](int n) { return (1u << min(max(n, 0), 8)) - 1; };  // keys j0 .. j0 + n - 1
+  // (unsigned: a window of 2^31 - 1 and a position before j0 pass the 32 bits, and see nothing)
+  const int low = (int)((unsigned)pos - (unsigned)s.window + 1u - (unsigned)j0);
+  const unsigned m = below(pos - j0 + 1) & (~below(low) | below(s.sinks - j0));
+  return v < s.page_end ? m : 0;
 }
+// The scores of these keys, -inf where the row does not see one (its bit as a word of its
+// own, and a select by it), and their max.
 __device__ __forceinline__ float mask_scores(const f32x4 (&s)[2], float (&sv)[2][4], unsigned seen) {
   float mx = -kInf;
 #pragma unroll
   for (int b = 0; b < 2; b++)
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      sv[b][i] = seen >> (4 * b + i) & 1 ? s[b][i] : -kInf;
+      const uint32_t on = (uint32_t)((int)(seen << (31 - 4 * b - i)) >> 31);
+      sv[b][i] = __uint_as_float((on & __float_as_uint(s[b][i])) | (~on & 0xFF800000u));
       mx = fmaxf(mx, sv[b][i]);
     }
   return mx;
@@ -93,9 +94,11 @@ __device__ __forceinline__ void value_mask(unsigned seen, uint32_t (&keep)[4]) {
 
 // Values that are no numbers, where only some rows see their keys: a probability of 0 would
 // not keep them out of the other rows' sums, so they are taken out of the products and come
-// back through products of their own, of their places with the keys that a row sees (ones).
-// Needed in chunks on the edge of what a tile's rows see; a search over their values there
-// (two instructions a word) finds when.
+// back at the item's end through products of their own, of their places with the keys that a
+// row sees (ones).  Needed in chunks on the edge of what a tile's rows see; a search over
+// their values there (two instructions a word) finds when.  (Brought back at once, the branch
+// took so many registers from the loop that some of them went to memory, and each of those
+// back behind the copies in flight.)
 __device__ __forceinline__ bool some_not_finite(const u32x4& v) {
   uint32_t t = 0;
 #pragma unroll
@@ -108,47 +111,59 @@ __device__ __forceinline__ bf16x8 seen_ones(unsigned seen) {
   return as_bf16x8(u32x4{keep[0] & 0x3F803F80u, keep[1] & 0x3F803F80u, keep[2] & 0x3F803F80u,
                          keep[3] & 0x3F803F80u});
 }
-__device__ __forceinline__ void put_not_finite(const u32x4& v, unsigned seen, f32x4& o) {
-  u32x4 nan, up, down;
+// (o: 16 dims of which v holds eight keys a lane; ones: the row's keys.  One kind after the
+// other: beside a tile's registers there is room for no more.)
+__device__ __forceinline__ void put_not_finite(const u32x4& v, bf16x8 ones, f32x4& o) {
+  auto halves = [](uint32_t bits) { return (bits & 0x00010001u) * 0xFFFFu; };  // of bits 0 and 16
+  auto odd = [&](uint32_t x) { return halves(((x & 0x7F807F80u) + 0x00800080u) >> 15); };
+  auto fraction = [&](uint32_t x) { return halves(((x & 0x007F007Fu) + 0x007F007Fu) >> 7); };
+  auto minus = [&](uint32_t x) { return halves(x >> 15); };
+  auto add = [&](auto is, uint32_t value) {
+    __builtin_amdgcn_sched_barrier(0);
+    u32x4 at;
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    nan[i] = up[i] = down[i] = 0;
+    for (int i = 0; i < 4; i++) at[i] = odd(v[i]) & is(v[i]) & 0x3F803F80u;
+    const f32x4 n = mfma16(as_bf16x8(at), ones, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-    for (int h = 0; h < 32; h += 16) {
-      const uint32_t x = v[i] >> h & 0xFFFFu;
-      nan[i] |= (x & 0x7FFFu) > 0x7F80u ? 0x3F80u << h : 0u;
-      up[i] |= x == 0x7F80u ? 0x3F80u << h : 0u;
-      down[i] |= x == 0xFF80u ? 0x3F80u << h : 0u;
-    }
-  }
-  const bf16x8 ones = seen_ones(seen);
-  const f32x4 zero = f32x4{0.f, 0.f, 0.f, 0.f};
-  const f32x4 n = mfma16(as_bf16x8(nan), ones, zero), u = mfma16(as_bf16x8(up), ones, zero),
-              d = mfma16(as_bf16x8(down), ones, zero);
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    if (n[i] > 0.f) o[i] = __builtin_nanf("");
-    if (u[i] > 0.f) o[i] += kInf;
-    if (d[i] > 0.f) o[i] -= kInf;
-  }
+    for (int i = 0; i < 4; i++)  // (n > 0, as a mask)
+      o[i] += __uint_as_float((uint32_t)((int)(0u - __float_as_uint(n[i])) >> 31) & value);
+  };
+  add([&](uint32_t x) { return ~fraction(x) & ~minus(x); }, 0x7F800000u);
+  add([&](uint32_t x) { return ~fraction(x) & minus(x); }, 0xFF800000u);
+  add([&](uint32_t x) { return fraction(x); }, 0x7FC00000u);
+  __builtin_amdgcn_sched_barrier(0);
 }
 __device__ __forceinline__ void drop_not_finite(u32x4& v) {
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    if ((v[i] & 0x7F80u) == 0x7F80u) v[i] &= 0xFFFF0000u;
-    if ((v[i] & 0x7F800000u) == 0x7F800000u) v[i] &= 0xFFFFu;
-  }
+  for (int i = 0; i < 4; i++)
+    v[i] &= ~(((((v[i] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu);
 }
 
+// Rows of an item by their place in it: the token (of the record's) and the q head.
+struct ItemRows {
+  int tok0, rest, group;
+  uint32_t inv;
+  __device__ __forceinline__ ItemRows(const SpanParams& p, const SpanItem& it)
+      : tok0(it.tok0), rest(it.row0 - it.tok0 * p.a.group), group(p.a.group), inv(p.group_inv) {}
+  __device__ __forceinline__ int token(int i) const {  // (exact for rest + i < 2^16)
+    return tok0 + (group == 1 ? i : (int)__umulhi((unsigned)(rest + i), inv));
+  }
+  __device__ __forceinline__ int head(int i, int token) const { return rest + i - (token - tok0) * group; }
+};
 // A row's place in the batch.
 struct RowAt {
   int64_t tok;
   int head, pos;
 };
-__device__ __forceinline__ RowAt row_at(const SpanParams& p, const SpanRows& rw, int kvh, int row) {
-  const int t = row / p.a.group, h = kvh * p.a.group + row - t * p.a.group;
+__device__ __forceinline__ RowAt row_at(const SpanParams& p, const SpanRows& rw, const ItemRows& rows,
+                                        int kvh, int i) {
+  const int t = rows.token(i), h = kvh * p.a.group + rows.head(i, t);
   if (rw.list) return RowAt{p.tokens[rw.tok + t], h, rw.pos};
   return RowAt{rw.tok + t, h, rw.pos + t};
+}
+// The partial of the item's first row.
+__device__ __forceinline__ int64_t part_of(const SpanRows& rw, const SpanItem& it, int kvh) {
+  return rw.part + ((int64_t)kvh * rw.n_split + it.split) * rw.n_rows + it.row0;
 }
 
 static_assert(kSpanTileRows == 4 * 32, "four waves of two 16-row blocks");
@@ -159,25 +174,25 @@ static_assert(kSpanTileRows == 4 * 32, "four waves of two 16-row blocks");
 // behind (the diagonal, the end) do, and a wave leaves out those that none of its rows sees.
 template <int HD>
 __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& it, const SpanRows& rw,
-                                          char* smem) {
+                                          const SpanPages& pg, int kvh, char* smem) {
   using SC = SharedChunk<HD>;
   constexpr int KB = SC::KBYTES, CB = SC::BYTES, NLD = SC::NLD, ND = HD / 32;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15;  // row of this lane within each block
   const int g4 = lane >> 4;   // lane group
-  const int kvh = it.kvh;
-  const Span span(p, it, rw);
-  const int end_row = it.row0 + it.n_rows;
-  const int row0 = it.row0 + 32 * wave;
-  const int first_page = it.page0, page_end = it.page_end;
+  const Span span(p, pg, rw);
+  const ItemRows rows(p, it);
+  const int n_rows = it.n_rows;
+  const int row0 = 32 * wave;  // the wave's first row, of the item's
+  const int first_page = pg.page0, page_end = pg.page1;
   const int n_chunks = (page_end - first_page + 1) / 2;
 
   bf16x8 qf[ND], qf2[ND];
   int pos, pos2;
   {
     auto load = [&](int row, bf16x8 (&f)[ND], int& at) {
-      const RowAt r = row_at(p, rw, kvh, min(row, end_row - 1));
+      const RowAt r = row_at(p, rw, rows, kvh, min(row, n_rows - 1));
       const uint16_t* qp = p.a.q + r.tok * p.a.q_tok_stride + (int64_t)r.head * HD + 8 * g4;
 #pragma unroll
       for (int ds = 0; ds < ND; ds++) f[ds] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ds * 32));
@@ -194,9 +209,9 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
 
   // positions of the tile's rows and of the wave's
   auto pos_of = [&](int row) {
-    return rw.list ? rw.pos : rw.pos + min(row, end_row - 1) / p.a.group;
+    return rw.list ? rw.pos : rw.pos + rows.token(min(row, n_rows - 1));
   };
-  const int tile_pos0 = pos_of(it.row0), tile_pos1 = pos_of(end_row - 1);
+  const int tile_pos0 = pos_of(0), tile_pos1 = pos_of(n_rows - 1);
   const int wave_pos0 = pos_of(row0), wave_pos1 = pos_of(row0 + 31);
 
   // the chunks that need no mask: first_whole .. end_whole - 1
@@ -249,34 +264,30 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
     kaddr[ds] = lds0 + (unsigned)(key0 * (HD * 2) + (((4 * ds + g4) ^ ksw<HD>(key0)) << 4));
   const unsigned vaddr = lds0 + (unsigned)(KB + (g4 >> 1) * (HD * 32) + col * 32 + ((g4 & 1) << 4));
 
+  // Fragments of chunk c (slot: c % 4 as a constant, which then is part of the read
+  // instructions, or -1): its keys' score blocks, its values' dims in two halves.
+  u32x4 k0[ND], k1[ND];
+  auto read_keys = [&](auto slot, int c) {
+    constexpr int S = decltype(slot)::value, OFF = S >= 0 ? S * CB : 0;
+    const unsigned sb = S >= 0 ? 0u : (unsigned)((c & 3) * CB);
+#pragma unroll
+    for (int ds = 0; ds < ND; ds++) k0[ds] = lds_read16_at<OFF>(sb + kaddr[ds]);
+#pragma unroll
+    for (int ds = 0; ds < ND; ds++) k1[ds] = lds_read16_at<OFF + 4 * HD * 2>(sb + kaddr[ds]);
+  };
+  auto read_values = [&](auto slot, auto half, int c, u32x4 (&v)[ND]) {
+    constexpr int S = decltype(slot)::value, OFF = S >= 0 ? S * CB : 0;
+    lds_read_run<0, ND, OFF + decltype(half)::value * ND * 512, 512>(
+        S >= 0 ? vaddr : vaddr + (unsigned)((c & 3) * CB), v);
+  };
+  using First = std::integral_constant<int, 0>;
+  using Second = std::integral_constant<int, 1>;
+
+  // this lane's raw scores of a chunk, their max, and whether some lane of the wave is above
+  // its row's threshold
   float sv1[2][4], sv2[2][4], mx1 = -kInf, mx2 = -kInf;
-  auto scores = [&](auto mask, auto slot, int c) -> bool {
-    constexpr bool MASK = decltype(mask)::value;
-    u32x4 k0[ND], k1[ND];
-    if constexpr (decltype(slot)::value >= 0) {
-      constexpr int OFF = decltype(slot)::value * CB;
-#pragma unroll
-      for (int ds = 0; ds < ND; ds++) k0[ds] = lds_read16_at<OFF>(kaddr[ds]);
-#pragma unroll
-      for (int ds = 0; ds < ND; ds++) k1[ds] = lds_read16_at<OFF + 4 * HD * 2>(kaddr[ds]);
-    } else {
-      const unsigned sb = (unsigned)((c & 3) * CB);
-#pragma unroll
-      for (int ds = 0; ds < ND; ds++) k0[ds] = lds_read16(sb + kaddr[ds]);
-#pragma unroll
-      for (int ds = 0; ds < ND; ds++) k1[ds] = lds_read16_at<4 * HD * 2>(sb + kaddr[ds]);
-    }
-    f32x4 s1[2], s2[2];
-    lgkm_wait<ND>();
-    pin(k0);
-    s1[0] = score_block<HD>(k0, qf);
-    s2[0] = score_block<HD>(k0, qf2);
-    __builtin_amdgcn_sched_barrier(0);  // these products go before the second wait
-    lgkm_wait<0>();
-    pin(k1);
-    s1[1] = score_block<HD>(k1, qf);
-    s2[1] = score_block<HD>(k1, qf2);
-    if constexpr (MASK) {
+  auto take = [&](auto mask, const f32x4 (&s1)[2], const f32x4 (&s2)[2], int c) -> bool {
+    if constexpr (decltype(mask)::value) {
       mx1 = mask_scores(s1, sv1, seen_keys(span, first_page + 2 * c, pos, g4));
       mx2 = mask_scores(s2, sv2, seen_keys(span, first_page + 2 * c, pos2, g4));
     } else {
@@ -285,54 +296,49 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
     }
     return __any(mx1 > r1.thr || mx2 > r2.thr) != 0;
   };
-  auto values = [&](auto mask, auto slot, int c, bf16x8 pb1, bf16x8 pb2) {
-    constexpr bool MASK = decltype(mask)::value;
-    constexpr int OFF = decltype(slot)::value >= 0 ? decltype(slot)::value * CB : 0;
-    const unsigned va = decltype(slot)::value >= 0 ? vaddr : vaddr + (unsigned)((c & 3) * CB);
+  auto scores = [&](int c) -> bool {  // of a chunk on its own, masked
+    read_keys(std::integral_constant<int, -1>{}, c);
+    lgkm_wait<0>();
+    pin(k0);
+    pin(k1);
+    const f32x4 s1[2] = {score_block<HD>(k0, qf), score_block<HD>(k1, qf)};
+    const f32x4 s2[2] = {score_block<HD>(k0, qf2), score_block<HD>(k1, qf2)};
+    return take(std::integral_constant<bool, true>{}, s1, s2, c);
+  };
+  const uint32_t no_mask[4] = {};
+  auto add_values = [&](auto half, const u32x4 (&v)[ND], bf16x8 pb1, bf16x8 pb2) {
+    constexpr int DB0 = decltype(half)::value * ND;
+    values_part<HD, DB0, ND, false>(v, o, pb1, no_mask);
+    values_part<HD, DB0, ND, false>(v, o2, pb2, no_mask);
+  };
+  // the values of a chunk that not every row sees whole (no branch may come between a read
+  // and its wait); some that are no numbers are left out until the end
+  bool left_out = false;
+  auto edge_values = [&](int c, bf16x8 pb1, bf16x8 pb2) {
     u32x4 v0[ND], v1[ND];
-    lds_read_run<0, ND, OFF, 512>(va, v0);
-    lds_read_run<0, ND, OFF + ND * 512, 512>(va, v1);
-    const uint32_t none[4] = {};
-    auto part = [&](auto first, u32x4 (&v)[ND]) {
-      constexpr int DB0 = decltype(first)::value;
-      if constexpr (MASK) {
-        bool some = false;
-#pragma unroll
-        for (int e = 0; e < ND; e++) some |= some_not_finite(v[e]);
-        if (__any(some)) {
-          const unsigned n1 = seen_keys(span, first_page + 2 * c, pos, g4);
-          const unsigned n2 = seen_keys(span, first_page + 2 * c, pos2, g4);
-#pragma unroll
-          for (int e = 0; e < ND; e++) {
-            put_not_finite(v[e], n1, o[DB0 + e]);
-            put_not_finite(v[e], n2, o2[DB0 + e]);
-            drop_not_finite(v[e]);
-          }
-        }
-      }
-      values_part<HD, DB0, ND, false>(v, o, pb1, none);
-      values_part<HD, DB0, ND, false>(v, o2, pb2, none);
-    };
-    // (no branch may come between a read and its wait)
-    lgkm_wait<MASK ? 0 : ND>();
+    read_values(std::integral_constant<int, -1>{}, First{}, c, v0);
+    read_values(std::integral_constant<int, -1>{}, Second{}, c, v1);
+    lgkm_wait<0>();
     pin(v0);
-    if constexpr (MASK) pin(v1);
-    part(std::integral_constant<int, 0>{}, v0);
-    if constexpr (!MASK) {
-      __builtin_amdgcn_sched_barrier(0);  // these products go before the second wait
-      lgkm_wait<0>();
-      pin(v1);
+    pin(v1);
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < ND; e++) some |= some_not_finite(v0[e]) || some_not_finite(v1[e]);
+    if (__any(some)) {
+      left_out = true;
+#pragma unroll
+      for (int e = 0; e < ND; e++) {
+        drop_not_finite(v0[e]);
+        drop_not_finite(v1[e]);
+      }
     }
-    part(std::integral_constant<int, ND>{}, v1);
+    add_values(First{}, v0, pb1, pb2);
+    add_values(Second{}, v1, pb1, pb2);
   };
   auto raise_rows = [&]() {
     raise_max(r1, mx1, scale, inv_scale, o);
     raise_max(r2, mx2, scale, inv_scale, o2);
   };
-  using Masked = std::integral_constant<bool, true>;
-  using Unmasked = std::integral_constant<bool, false>;
-  using AnySlot = std::integral_constant<int, -1>;
-
   int ua, fa = 0;  // page of the chunk the next copy is for, and of the one after
   {
     const int a0 = page_of(0), a1 = page_of(1), a2 = page_of(2);
@@ -341,30 +347,29 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
     ua = page_of(3);
     copy(2, a2);
   }
-  // top of iteration kt: this wave's copies of chunk kt + 1 have landed, then everyone's,
-  // and every read of chunk kt - 1 is done; chunk kt + 3 goes out
-  auto top = [&](int kt, int& use, int& fill) {
+  // Top of iteration kt: this wave's copies of chunk kt + 1 have landed, then everyone's, and
+  // every read of chunk kt - 1 is done; chunk kt + 3 goes out.  Scalar loads return in any
+  // order, so a use of the last iteration's page id behind the issue of the next would wait
+  // for that too: the empty statement takes it first.
+  auto wait_top = [&](int& use) {
     vm_wait<NLD>();
+    asm volatile("" : "+s"(use));
     wg_barrier();
+  };
+  auto copy_top = [&](int kt, int use, int& fill) {
     fill = page_of(kt + 4);
     copy(kt + 3, use);
   };
   auto run = [&](int kt0, int kt1, auto body) {  // iterations kt0 .. kt1 - 1
-    for (int kt = kt0; kt < kt1; kt += 2) {
-      top(kt, ua, fa);
+    for (int kt = kt0; kt < kt1; kt++) {
+      wait_top(ua);
+      copy_top(kt, ua, fa);
       body(kt);
-      if (kt + 1 >= kt1) {  // an odd count: the next iteration uses fa
-        const int t = ua;
-        ua = fa;
-        fa = t;
-        break;
-      }
-      top(kt + 1, fa, ua);
-      body(kt + 1);
+      ua = fa;
     }
   };
 
-  if (row0 >= end_row) {
+  if (row0 >= n_rows) {
     // no rows here: this wave only copies its quarter of every chunk
     vm_wait<2 * NLD>();
     wg_barrier();
@@ -377,62 +382,107 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
   };
   vm_wait<2 * NLD>();  // chunk 0 has landed; chunks 1 and 2 may be in flight
   wg_barrier();
-  if (takes(0) && scores(Masked{}, AnySlot{}, 0)) raise_rows();
+  if (takes(0) && scores(0)) raise_rows();
 
-  // Iteration kt holds the scores of chunk kt (of the previous iteration), takes its
-  // softmax and values, and the scores of chunk kt + 1.
+  // Iteration kt holds the scores of chunk kt (of the previous iteration) and takes its
+  // softmax, its values and the scores of chunk kt + 1.
   auto edge = [&](int kt) {
     if (takes(kt)) {
       const bf16x8 pb1 = probs(sv1, r1, scale);
       const bf16x8 pb2 = probs(sv2, r2, scale);
-      values(Masked{}, AnySlot{}, kt, pb1, pb2);
+      edge_values(kt, pb1, pb2);
     }
-    if (takes(kt + 1) && scores(Masked{}, AnySlot{}, kt + 1)) raise_rows();
+    if (takes(kt + 1) && scores(kt + 1)) raise_rows();
   };
-  // the scores of chunk kt + 1 and the softmax of chunk kt in one basic block, then the
-  // values of chunk kt; no masks
-  auto step = [&](auto slot, int kt) {  // slot: kt % 4 or -1
+  // The same without masks, where both chunks are whole: the keys of chunk kt + 1 are on
+  // their way from LDS during the exponentials of chunk kt, the values of chunk kt during
+  // the score products.  slot: kt % 4, or -1.
+  auto step = [&](auto slot, int kt, int& use, int& fill) {
     constexpr int S = decltype(slot)::value, S1 = S < 0 ? -1 : (S + 1) % 4;
+    wait_top(use);
+    read_keys(std::integral_constant<int, S1>{}, kt + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    copy_top(kt, use, fill);
     const bf16x8 pb1 = probs(sv1, r1, scale);
     const bf16x8 pb2 = probs(sv2, r2, scale);
-    const bool raise = scores(Unmasked{}, std::integral_constant<int, S1>{}, kt + 1);
-    values(Unmasked{}, slot, kt, pb1, pb2);
+    u32x4 v0[ND], v1[ND];
+    f32x4 s1[2], s2[2];
+    lgkm_wait<ND>();
+    pin(k0);
+    s1[0] = score_block<HD>(k0, qf);
+    s2[0] = score_block<HD>(k0, qf2);
+    __builtin_amdgcn_sched_barrier(0);  // these products go before the next wait
+    read_values(slot, First{}, kt, v0);
+    lgkm_wait<ND>();
+    pin(k1);
+    s1[1] = score_block<HD>(k1, qf);
+    s2[1] = score_block<HD>(k1, qf2);
+    __builtin_amdgcn_sched_barrier(0);
+    read_values(slot, Second{}, kt, v1);
+    lgkm_wait<ND>();
+    pin(v0);
+    add_values(First{}, v0, pb1, pb2);
+    const bool raise = take(std::integral_constant<bool, false>{}, s1, s2, kt + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    lgkm_wait<0>();
+    pin(v1);
+    add_values(Second{}, v1, pb1, pb2);
     if (raise) raise_rows();
   };
   // the whole chunks' iterations: both kt and kt + 1 are whole, from a multiple of four on
   // four at a time, whose ring slots are constants in the fragment reads
   const int main0 = first_whole, main1 = max(end_whole - 1, main0);
   const int four0 = min((main0 + 3) & ~3, main1), four1 = four0 + ((main1 - four0) & ~3);
+  using AnySlot = std::integral_constant<int, -1>;
+  auto steps = [&](int kt0, int kt1) {
+    for (int kt = kt0; kt < kt1; kt++) {
+      step(AnySlot{}, kt, ua, fa);
+      ua = fa;
+    }
+  };
   run(0, main0, edge);
-  run(main0, four0, [&](int kt) { step(AnySlot{}, kt); });
+  steps(main0, four0);
   for (int kt = four0; kt < four1; kt += 4) {
-    top(kt, ua, fa);
-    step(std::integral_constant<int, 0>{}, kt);
-    top(kt + 1, fa, ua);
-    step(std::integral_constant<int, 1>{}, kt + 1);
-    top(kt + 2, ua, fa);
-    step(std::integral_constant<int, 2>{}, kt + 2);
-    top(kt + 3, fa, ua);
-    step(std::integral_constant<int, 3>{}, kt + 3);
+    step(std::integral_constant<int, 0>{}, kt, ua, fa);
+    step(std::integral_constant<int, 1>{}, kt + 1, fa, ua);
+    step(std::integral_constant<int, 2>{}, kt + 2, ua, fa);
+    step(std::integral_constant<int, 3>{}, kt + 3, fa, ua);
   }
-  run(four1, main1, [&](int kt) { step(AnySlot{}, kt); });
+  steps(four1, main1);
   run(main1, n_chunks, edge);
   vm_wait<0>();  // no copy may land in LDS after the workgroup has ended
+  if (left_out) {  // (of the wave) their values once more, from memory
+    for (int c = 0; c < n_chunks; c++) {
+      if (c == main0) c = main1;
+      if (!takes(c)) continue;
+      const int v0 = first_page + 2 * c;
+      const bf16x8 ones1 = seen_ones(seen_keys(span, v0, pos, g4));
+      const bf16x8 ones2 = seen_ones(seen_keys(span, v0, pos2, g4));
+      const int64_t page = p.a.pages[rw.pages + span.entry(min(v0 + (g4 >> 1), page_end - 1))];
+      const uint16_t* at = p.a.v_pool + (page * p.a.nkv + kvh) * (16 * HD) + col * 16 + 8 * (g4 & 1);
+#pragma unroll
+      for (int e = 0; e < HD / 16; e++) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(at + e * 256);
+        put_not_finite(v, ones1, o[e]);
+        put_not_finite(v, ones2, o2[e]);
+      }
+    }
+  }
 
   // the rows' sums over their four lane groups (every lane takes part)
   const float l1 = lane_groups_sum(r1.l), l2 = lane_groups_sum(r2.l);
   const int64_t step32 = p.a.out_tiled ? 512 : 32;
   auto store = [&](int row, float l, const RowState& st, const f32x4 (&acc)[HD / 16]) {
-    if (row >= end_row) return;
-    if (it.part >= 0) {
-      const int64_t part = (int64_t)it.part + row - it.row0;
+    if (row >= n_rows) return;
+    if (rw.part >= 0) {
+      const int64_t part = part_of(rw, it, kvh) + row;
 #pragma unroll
       for (int db = 0; db < HD / 16; db++)
         *reinterpret_cast<f32x4*>(p.a.part_o + part * HD + 16 * db + 4 * g4) = acc[db];
       if (g4 == 0) *reinterpret_cast<float2*>(p.a.part_ml + 2 * part) = float2{st.m, l};
       return;
     }
-    const RowAt r = row_at(p, rw, kvh, row);
+    const RowAt r = row_at(p, rw, rows, kvh, row);
     const float inv = 1.f / l;
     uint16_t* op = out_ptr(p.a, r.tok, r.head * HD + 4 * g4);
 #pragma unroll
@@ -448,20 +498,21 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
 }
 
 // Stream: up to 16 rows of one position (a decode's q heads; or rows that see a whole run);
-// the four waves stride over the item's 32-key chunks, keys and values straight to
+// its waves stride over the item's 32-key chunks, keys and values straight to
 // registers, and combine through LDS.  Keys that the rows do not see are taken out by
 // select, scores and values, so what their slots hold stays out.
-template <int HD, bool NT>
+template <int HD, bool NT, int WAVES>
 __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem& it, const SpanRows& rw,
-                                            char* smem) {
+                                            const SpanPages& pg, int kvh, char* smem) {
   const int lane = threadIdx.x & 63;
   const int wave = threadIdx.x >> 6;
   const int col = lane & 15;  // row of this lane
   const int g4 = lane >> 4;   // lane group
-  const int kvh = it.kvh, page_end = it.page_end;
-  const Span span(p, it, rw);
-  const RowAt at = row_at(p, rw, kvh, it.row0 + min(col, it.n_rows - 1));
-  const int pos = rw.list ? rw.pos : rw.pos + it.row0 / p.a.group;  // of every row
+  const int page_end = pg.page1;
+  const Span span(p, pg, rw);
+  const ItemRows rows(p, it);
+  const RowAt at = row_at(p, rw, rows, kvh, min(col, it.n_rows - 1));
+  const int pos = rw.list ? rw.pos : rw.pos + it.tok0;  // of every row
   RowState r = span_row_start();
   const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
   f32x4 o[HD / 16];
@@ -479,7 +530,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
     const f32x4 s[2] = {score_block<HD>(c.k[0], qf), score_block<HD>(c.k[1], qf)};
     float sv[2][4];
     float mx = take_scores(s, sv);
-    if (!span.all_seen(v, pos, pos)) {
+    if (!span.all_seen(v, pos)) {
       const unsigned seen = seen_keys(span, v, pos, g4);
       mx = mask_scores(s, sv, seen);
       uint32_t keep[4];
@@ -496,9 +547,9 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
   };
   // two chunk buffers in turn, a chunk's loads issued only where it exists (decode_item of
   // the bf16 attention tells why)
-  constexpr int STEP = 8;
+  constexpr int STEP = 2 * WAVES;
   Chunk<HD> ca, cb;
-  int v = it.page0 + 2 * wave;
+  int v = pg.page0 + 2 * wave;
   if (v < page_end) {
     int n0 = pid(v + STEP), n1 = pid(v + STEP + 1);
     load_chunk<HD, NT>(ca, p.a, kvh, pid(v), pid(v + 1), 0, col, g4);
@@ -529,9 +580,11 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
     }
   }
 
+  // (a row's output in SEGS threads of EL dims each)
+  constexpr int SEGS = WAVES * 4, EL = HD / SEGS;
   float(*s_o)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(smem);
-  float(*s_m)[16] = reinterpret_cast<float(*)[16]>(smem + 4 * 16 * (HD + 4) * 4);
-  float(*s_l)[16] = reinterpret_cast<float(*)[16]>(smem + 4 * 16 * (HD + 4) * 4 + 4 * 16 * 4);
+  float(*s_m)[16] = reinterpret_cast<float(*)[16]>(smem + WAVES * 16 * (HD + 4) * 4);
+  float(*s_l)[16] = s_m + WAVES;
 #pragma unroll
   for (int db = 0; db < HD / 16; db++)
     *reinterpret_cast<f32x4*>(&s_o[wave][col][db * 16 + 4 * g4]) = o[db];
@@ -541,97 +594,132 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
     s_l[wave][col] = l;
   }
   __syncthreads();
-  const int row = threadIdx.x >> 4;  // 16 rows
-  const int dseg = (threadIdx.x & 15) * (HD / 16);
+  const int row = threadIdx.x / SEGS, seg = threadIdx.x % SEGS;
+  const int dseg = seg * EL;
   if (row >= it.n_rows) return;
   float M = kLowest;
 #pragma unroll
-  for (int w = 0; w < 4; w++) M = fmaxf(M, s_m[w][row]);
-  float wt[4], L = 0.f;
+  for (int w = 0; w < WAVES; w++) M = fmaxf(M, s_m[w][row]);
+  float wt[WAVES], L = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; w++) {
+  for (int w = 0; w < WAVES; w++) {
     wt[w] = exp2f(s_m[w][row] - M);
     L += s_l[w][row] * wt[w];
   }
-  float acc[HD / 16];
+  float acc[EL];
 #pragma unroll
-  for (int e = 0; e < HD / 16; e++) {
+  for (int e = 0; e < EL; e++) {
     float a = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; w++) a += s_o[w][row][dseg + e] * wt[w];
+    for (int w = 0; w < WAVES; w++) a += s_o[w][row][dseg + e] * wt[w];
     acc[e] = a;
   }
-  if (it.part < 0) {
-    const RowAt to = row_at(p, rw, kvh, it.row0 + row);
+  if (rw.part < 0) {
+    const RowAt to = row_at(p, rw, rows, kvh, row);
     const float inv = 1.f / L;
-    uint16_t* op = out_ptr(p.a, to.tok, to.head * HD + dseg);  // HD / 16 dims within a 32-column block
+    uint16_t* op = out_ptr(p.a, to.tok, to.head * HD + dseg);  // EL dims within a 32-column block
 #pragma unroll
-    for (int e = 0; e < HD / 16; e += 2)
+    for (int e = 0; e < EL; e += 2)
       *reinterpret_cast<uint32_t*>(op + e) = pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
   } else {
-    const int64_t part = (int64_t)it.part + row;
+    const int64_t part = part_of(rw, it, kvh) + row;
     float* po = p.a.part_o + part * HD + dseg;
 #pragma unroll
-    for (int e = 0; e < HD / 16; e += 4)
-      *reinterpret_cast<f32x4*>(po + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-    if ((threadIdx.x & 15) == 0) *reinterpret_cast<float2*>(p.a.part_ml + 2 * part) = float2{M, L};
+    for (int e = 0; e < EL; e += 2) *reinterpret_cast<float2*>(po + e) = float2{acc[e], acc[e + 1]};
+    if (seg == 0) *reinterpret_cast<float2*>(p.a.part_ml + 2 * part) = float2{M, L};
   }
 }
 
 // An item without pages: partials that count as nothing.
 template <int HD>
-__device__ __forceinline__ void empty_item(const SpanParams& p, const SpanItem& it) {
-  for (int i = threadIdx.x; i < it.n_rows * (HD / 4); i += 256)
-    *reinterpret_cast<f32x4*>(p.a.part_o + (int64_t)it.part * HD + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ void empty_item(const SpanParams& p, const SpanItem& it, int64_t part) {
+  for (int i = threadIdx.x; i < it.n_rows * (HD / 4); i += blockDim.x)
+    *reinterpret_cast<f32x4*>(p.a.part_o + part * HD + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
   if ((int)threadIdx.x < it.n_rows)
-    *reinterpret_cast<float2*>(p.a.part_ml + 2 * ((int64_t)it.part + threadIdx.x)) = float2{kLowest, 0.f};
+    *reinterpret_cast<float2*>(p.a.part_ml + 2 * (part + threadIdx.x)) = float2{kLowest, 0.f};
 }
 
-template <int HD>
-constexpr int combine_bytes() {
-  return (4 * 16 * (HD + 4) + 2 * 4 * 16) * 4;
+// The parameters with the metadata's pointers into the argument block.
+struct SmallSpan {
+  SpanParams p;
+  InlineMeta meta;
+};
+static_assert(sizeof(SmallSpan) <= 4096, "a launch's arguments");
+__device__ __forceinline__ SpanParams inline_params(const SmallSpan& s) {
+  SpanParams p = s.p;
+  constexpr size_t M = offsetof(SmallSpan, meta);
+  p.rows = inline_meta(M, p.rows);
+  p.items = inline_meta(M, p.items);
+  p.a.pages = inline_meta(M, p.a.pages);
+  p.tokens = inline_meta(M, p.tokens);
+  p.merge_tokens = inline_meta(M, p.merge_tokens);
+  p.merges = inline_meta(M, p.merges);
+  p.sources = inline_meta(M, p.sources);
+  return p;
 }
-template <int HD, bool TILES>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void span_attn_kernel(SpanParams p) {
-  __shared__ __attribute__((aligned(16))) char smem[TILES ? smem_bytes<HD>() : combine_bytes<HD>()];
-  const SpanItem it = p.items[blockIdx.x];
+
+template <int HD, int WAVES>
+constexpr int combine_bytes() {
+  return (WAVES * 16 * (HD + 4) + 2 * WAVES * 16) * 4;
+}
+template <int HD, bool TILES, int WAVES>
+constexpr int span_smem() {
+  return TILES ? smem_bytes<HD>() : combine_bytes<HD, WAVES>();
+}
+template <int HD, bool TILES, int WAVES>
+__device__ __forceinline__ void span_item(const SpanParams& p, char* smem) {
+  const SpanBlock b = span_block(blockIdx.x, p.n_items, p.a.nkv, p.heads);
+  const SpanItem it = p.items[b.item];
   const SpanRows rw = p.rows[it.rows];
-  if (it.page0 >= it.page_end) {
-    empty_item<HD>(p, it);
+  const int tok1 = ItemRows(p, it).token(it.n_rows - 1);
+  const SpanPages pg = span_split(span_seen(rw, it.tok0, tok1, p.window), it.split, rw.n_split);
+  if (pg.page0 >= pg.page1) {
+    empty_item<HD>(p, it, part_of(rw, it, b.kvh));
     return;
   }
   if constexpr (TILES) {
-    if (it.kind == 1) tile_item<HD>(p, it, rw, smem);
-    else stream_item<HD, false>(p, it, rw, smem);
+    if (it.kind == 1) tile_item<HD>(p, it, rw, pg, b.kvh, smem);
+    else stream_item<HD, false, WAVES>(p, it, rw, pg, b.kvh, smem);
   } else {
-    stream_item<HD, true>(p, it, rw, smem);
+    stream_item<HD, true, WAVES>(p, it, rw, pg, b.kvh, smem);
   }
+}
+template <int HD, bool TILES, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void span_attn_kernel(
+    SpanParams p) {
+  __shared__ __attribute__((aligned(16))) char smem[span_smem<HD, TILES, WAVES>()];
+  span_item<HD, TILES, WAVES>(p, smem);
+}
+template <int HD, bool TILES, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void small_span_kernel(
+    SmallSpan s) {
+  __shared__ __attribute__((aligned(16))) char smem[span_smem<HD, TILES, WAVES>()];
+  span_item<HD, TILES, WAVES>(inline_params(s), smem);
 }
 
 // The merge: HD / 4 threads hold a row; a workgroup takes 8 (HD = 128) or 16 q heads of a
 // token, or (WIDE) one q head, whose partials its groups of threads read side by side.
 template <int HD, bool WIDE>
-__global__ __launch_bounds__(kMergeThreads) void span_merge_kernel(SpanParams p, const SpanToken* tokens,
-                                                                   const SpanMerge* merges,
-                                                                   const SpanSource* sources) {
+__device__ __forceinline__ void span_merge(const SpanParams& p) {
   constexpr int TPR = HD / 4, G = kMergeThreads / TPR;
-  const SpanToken tk = tokens[blockIdx.x];
-  const SpanMerge mg = merges[tk.merge];
+  const SpanToken tk = p.merge_tokens[blockIdx.x];
+  const SpanMerge mg = p.merges[tk.merge];
   const int g = threadIdx.x / TPR, d = 4 * (threadIdx.x % TPR);
   const int h = WIDE ? (int)blockIdx.y : (int)blockIdx.y * G + g;
   if (!WIDE && h >= p.a.nq) return;
-  const int kvh = h / p.a.group;
-  const int64_t in = (int64_t)(tk.tok - mg.tok) * p.a.group + h - kvh * p.a.group;
+  const int kvh = h / p.a.group, in_group = h - kvh * p.a.group;
   float m = kLowest, l = 0.f;
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
   int first = WIDE ? g : 0;  // of the next source's splits
   for (int s = 0; s < mg.n_src; s++) {
-    const SpanSource src = sources[mg.src + s];
-    const int64_t base = in + src.base + (int64_t)kvh * src.kvh_stride;
+    const SpanSource src = p.sources[mg.src + s];
+    const SpanRows rw = p.rows[src.rows];
+    const int64_t base = rw.part + (int64_t)kvh * rw.n_split * rw.n_rows +
+                         (int64_t)(src.tok + tk.tok - mg.tok) * p.a.group + in_group;
     int k = first;
 #pragma unroll 4
-    for (; k < src.n_split; k += WIDE ? G : 1) {
-      const int64_t at = base + (int64_t)k * src.split_stride;
+    for (; k < rw.n_split; k += WIDE ? G : 1) {
+      const int64_t at = base + (int64_t)k * rw.n_rows;
       const float2 ml = *reinterpret_cast<const float2*>(p.a.part_ml + 2 * at);
       const f32x4 o = *reinterpret_cast<const f32x4*>(p.a.part_o + at * HD + d);
       const float mn = fmaxf(m, ml.x);
@@ -640,7 +728,7 @@ __global__ __launch_bounds__(kMergeThreads) void span_merge_kernel(SpanParams p,
       l = l * a + ml.y * w;
       m = mn;
     }
-    if (WIDE) first = k - src.n_split;
+    if (WIDE) first = k - rw.n_split;
   }
   if constexpr (WIDE) {
     __shared__ float s_acc[G][HD], s_m[G], s_l[G];
@@ -665,36 +753,61 @@ __global__ __launch_bounds__(kMergeThreads) void span_merge_kernel(SpanParams p,
     *reinterpret_cast<uint32_t*>(out_ptr(p.a, tk.tok, h * HD + 2 * threadIdx.x)) =
         pack_bf16x2(a0 / L, a1 / L);
   } else {
+    const float inv = 1.f / l;
     u32x2 w;
-    w[0] = pack_bf16x2(acc[0] / l, acc[1] / l);
-    w[1] = pack_bf16x2(acc[2] / l, acc[3] / l);
+    w[0] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    w[1] = pack_bf16x2(acc[2] * inv, acc[3] * inv);
     *reinterpret_cast<u32x2*>(out_ptr(p.a, tk.tok, h * HD + d)) = w;
   }
 }
+template <int HD, bool WIDE>
+__global__ __launch_bounds__(kMergeThreads) void span_merge_kernel(SpanParams p) {
+  span_merge<HD, WIDE>(p);
+}
+template <int HD, bool WIDE>
+__global__ __launch_bounds__(kMergeThreads) void small_span_merge_kernel(SmallSpan s) {
+  span_merge<HD, WIDE>(inline_params(s));
+}
 
+// Streams alone in few workgroups: eight waves each, so that a wave takes half the keys.
+constexpr int kCUs = 256;
 template <int HD>
-hipError_t launch(const SpanParams& p, int n_items, bool tiles, const SpanToken* merge, int n_merge,
-                  bool wide, const SpanMerge* merges, const SpanSource* sources, hipStream_t stream) {
-  if (n_items > 0) {
-    if (tiles) span_attn_kernel<HD, true><<<n_items, 256, 0, stream>>>(p);
-    else span_attn_kernel<HD, false><<<n_items, 256, 0, stream>>>(p);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+hipError_t launch(const SpanParams& p, const InlineMeta* meta, bool tiles, int n_merge, int most_parts,
+                  hipStream_t stream) {
+  const int n = p.n_items * p.a.nkv;
+  if (n == 0) return hipSuccess;
+  if (meta) {
+    const SmallSpan s{p, *meta};
+    if (tiles) small_span_kernel<HD, true, 4><<<n, 256, 0, stream>>>(s);
+    else if (n <= kCUs) small_span_kernel<HD, false, 8><<<n, 512, 0, stream>>>(s);
+    else small_span_kernel<HD, false, 4><<<n, 256, 0, stream>>>(s);
+  } else {
+    if (tiles) span_attn_kernel<HD, true, 4><<<n, 256, 0, stream>>>(p);
+    else if (n <= kCUs) span_attn_kernel<HD, false, 8><<<n, 512, 0, stream>>>(p);
+    else span_attn_kernel<HD, false, 4><<<n, 256, 0, stream>>>(p);
   }
-  if (n_merge == 0) return hipSuccess;
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || n_merge == 0) return e;
   constexpr int G = kMergeThreads / (HD / 4);
-  if (wide) span_merge_kernel<HD, true><<<dim3(n_merge, p.a.nq), kMergeThreads, 0, stream>>>(p, merge, merges, sources);
-  else span_merge_kernel<HD, false><<<dim3(n_merge, (p.a.nq + G - 1) / G), kMergeThreads, 0, stream>>>(p, merge, merges, sources);
+  const bool wide = most_parts > 8;
+  const dim3 grid(n_merge, wide ? p.a.nq : (p.a.nq + G - 1) / G);
+  if (meta) {
+    const SmallSpan s{p, *meta};
+    if (wide) small_span_merge_kernel<HD, true><<<grid, kMergeThreads, 0, stream>>>(s);
+    else small_span_merge_kernel<HD, false><<<grid, kMergeThreads, 0, stream>>>(s);
+  } else {
+    if (wide) span_merge_kernel<HD, true><<<grid, kMergeThreads, 0, stream>>>(p);
+    else span_merge_kernel<HD, false><<<grid, kMergeThreads, 0, stream>>>(p);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_span_attn(const SpanParams& p, int n_items, bool tiles, const SpanToken* merge,
-                            int n_merge, bool wide, const SpanMerge* merges,
-                            const SpanSource* sources, int head_dim, hipStream_t stream) {
+hipError_t launch_span_attn(const SpanParams& p, const InlineMeta* meta, bool tiles, int n_merge,
+                            int most_parts, int head_dim, hipStream_t stream) {
   const auto call = head_dim == 128 ? launch<128> : launch<64>;
-  return call(p, n_items, tiles, merge, n_merge, wide, merges, sources, stream);
+  return call(p, meta, tiles, n_merge, most_parts, stream);
 }
 
 }  // namespace mx

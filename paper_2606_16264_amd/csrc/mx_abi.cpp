@@ -1779,11 +1779,11 @@ size_t span_bound(const mx_attn_shape* s, int32_t max_tokens, int32_t max_reqs, 
   const int64_t nkv = s->n_kv_heads, group = s->n_q_heads / nkv;
   const int64_t parts = (int64_t)max_reqs * (depth + 1), tokens = (int64_t)max_tokens * (depth + 1);
   const int64_t streams = max_pages / plan::kMinSplitPages + parts;
-  const int64_t items = streams * nkv * ceil_div(group, 16) +
-                        (ceil_div(tokens * group, kSpanTileRows) + parts) * nkv + plan::kExtraTiles;
+  const int64_t items = streams * ceil_div(group, kSpanStreamRows) +
+                        ceil_div(tokens * group, kSpanTileRows) + parts + plan::kExtraTiles;
   return make_layout_span(parts, max_pages, tokens, items, max_tokens, max_reqs, parts,
-                          streams * nkv * std::max<int64_t>(16, group) + tokens * s->n_q_heads +
-                              (int64_t)plan::kExtraTiles * kSpanTileRows,
+                          streams * nkv * std::max<int64_t>(kSpanStreamRows, group) +
+                              tokens * s->n_q_heads + (int64_t)plan::kExtraTiles * kSpanTileRows,
                           s->head_dim)
       .total;
 }
@@ -1824,8 +1824,9 @@ mx_status validate_runs(const mx_batch* b, int32_t num_runs, const mx_shared_run
 }
 
 mx_status check_span_plan(const SpanPlan& p) {
-  if (p.n_parts > INT32_MAX || p.n_pages > INT32_MAX || p.items.size() > (size_t)INT32_MAX)
-    return fail(MX_ERR_TOO_LARGE, "%lld partial rows, %zu work items", (long long)p.n_parts, p.items.size());
+  if (p.n_parts > INT32_MAX || p.n_pages > INT32_MAX || p.blocks() > INT32_MAX / 2)
+    return fail(MX_ERR_TOO_LARGE, "%lld partial rows, %lld work items", (long long)p.n_parts,
+                (long long)p.blocks());
   return MX_OK;
 }
 
@@ -1863,26 +1864,40 @@ mx_status span_attn(const char* tag, const SpanPlan& p, const mx_attn_shape* s, 
   a.a.k_pool = k_pool;
   a.a.v_pool = v_pool;
   a.a.out = out;
-  a.a.pages = at<int32_t>(ws, L.pages);
   a.a.part_o = at<float>(ws, L.part_o);
   a.a.part_ml = at<float>(ws, L.part_ml);
   a.a.nq = s->n_q_heads;
   a.a.nkv = s->n_kv_heads;
   a.a.group = p.group;
   a.a.scale_log2 = eff_scale(s) * 1.4426950408889634f;
-  a.rows = at<SpanRows>(ws, L.rows);
-  a.items = at<SpanItem>(ws, L.items);
-  a.tokens = at<int32_t>(ws, L.tokens);
   a.window = p.window;
   a.sinks = p.sinks;
-  st = staged(
-      L.meta_end, stream, [&](char* h) { pack_meta_span(p, L, h); },
-      [&](const void* dev) { return launch_upload(dev, ws, L.meta_end, stream); });
-  if (st != MX_OK) return st;
+  a.n_items = (int32_t)p.items.size();
+  a.heads = p.heads;
+  a.group_inv = p.group > 1 ? (uint32_t)((((uint64_t)1 << 32) + p.group - 1) / p.group) : 0;
+  // a small call's metadata goes with the kernels' arguments: no upload (each workgroup reads
+  // it from host memory, so only where there are few)
+  const bool small = L.meta_end <= sizeof(InlineMeta) && p.blocks() <= plan::kSlots;
+  void* meta = small ? nullptr : ws;  // what the pointers into the metadata count from
+  a.rows = at<SpanRows>(meta, L.rows);
+  a.items = at<SpanItem>(meta, L.items);
+  a.a.pages = at<int32_t>(meta, L.pages);
+  a.tokens = at<int32_t>(meta, L.tokens);
+  a.merge_tokens = at<SpanToken>(meta, L.merge_tokens);
+  a.merges = at<SpanMerge>(meta, L.merges);
+  a.sources = at<SpanSource>(meta, L.sources);
+  alignas(16) InlineMeta inlined;
+  if (small) {
+    pack_meta_span(p, L, inlined.b);
+  } else {
+    st = staged(
+        L.meta_end, stream, [&](char* h) { pack_meta_span(p, L, h); },
+        [&](const void* dev) { return launch_upload(dev, ws, L.meta_end, stream); });
+    if (st != MX_OK) return st;
+  }
   const hipError_t e = timed(tag, stream, [&] {
-    return launch_span_attn(a, (int)p.items.size(), p.has_tiles, at<SpanToken>(ws, L.merge_tokens),
-                            (int)p.merge_tokens.size(), p.most_parts > 8, at<SpanMerge>(ws, L.merges),
-                            at<SpanSource>(ws, L.sources), s->head_dim, stream);
+    return launch_span_attn(a, small ? &inlined : nullptr, p.has_tiles, (int)p.merge_tokens.size(),
+                            p.most_parts, s->head_dim, stream);
   });
   return e == hipSuccess ? MX_OK : hip_fail(e, "attention launch");
 }

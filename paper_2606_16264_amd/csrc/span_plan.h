@@ -28,10 +28,16 @@ inline SeenPages seen_pages(int ctx, int n, int window, int sinks) {
   return s;
 }
 
+// Joining the parts of a row costs a launch, partials written and read: runs are left to
+// their requests where less than this would be read once instead of several times.
+constexpr int64_t kMinSharedBytes = 24 << 20;
+
 struct SpanPlan {
+  int64_t min_shared_bytes = kMinSharedBytes;
   int group = 1, nkv = 1;
+  int64_t page_bytes = 0;  // keys and values of one head
   int window = INT32_MAX, sinks = 0;
-  struct Table {  // entries first .. first + n - 1 of a request's page table
+  struct Table {  // entries of a request's page table
     const int32_t* pages;
     int n;
   };
@@ -45,7 +51,9 @@ struct SpanPlan {
   int64_t n_pages = 0, n_parts = 0;
   int most_parts = 0;  // partials of a row
   bool has_tiles = false;
+  int heads = 1;  // of a group of span_block
 
+  int64_t blocks() const { return (int64_t)items.size() * nkv; }
   int add_table(const int32_t* pages, int n) {
     const int at = (int)n_pages;
     tables.push_back(Table{pages, n});
@@ -56,118 +64,131 @@ struct SpanPlan {
 
 namespace plan {
 
-constexpr int kXcds = 8;           // workgroup b runs on die b % 8
-constexpr int64_t kSlots = 512;    // workgroups that the chip holds at once
-constexpr int kMinSplitPages = 16; // of a stream, and of a tile (below)
+constexpr int64_t kSlots = 512;      // workgroups that the chip holds at once
+constexpr int64_t kTileSlots = 256;  // tiles are split to about as many
+constexpr int kMinSplitPages = 16;   // of a stream
+constexpr int kWholePages = 64;      // streams and tiles of up to that many are not split
 constexpr int kMinTilePages = 32;
-constexpr int kExtraTiles = 1024;  // items that splitting tiles adds to a call, at most
+constexpr int kExtraTiles = 1024;    // items that splitting tiles adds to a call, at most
+constexpr int kMostSplits = 4096;
 
-// Rows with the pages that they take, before they are cut into items.
+// A record's rows, before they are cut into items.
 struct Part {
-  int rows;        // SpanRows index
   bool stream;
-  bool partial;    // the rows have other parts
-  int source;      // of a partial part: its SpanSource
+  bool partial;  // its rows have other parts
 };
 
-// The pages of rows row0 .. row0 + n - 1, counted as in SpanItem.
-struct Range {
-  int skip, end;
+// The launch order, both kinds longest first.  Streams are bound by HBM, tiles by the matrix
+// cores, and interleaved they share a CU; but all tiles have to start early enough to end
+// with the rest, so they are dealt out over the first part of the list, the share of it that
+// is left of the whole when one tile's time is taken off its end.
+struct Cost {
+  SpanItem item;
+  int64_t cost;
 };
-inline Range range_of(const SpanPlan& p, const SpanRows& r, int entries, int row0, int n) {
-  if (r.list) return {0, entries};
-  const int pos0 = r.pos + row0 / p.group, pos1 = r.pos + (row0 + n - 1) / p.group;
-  const int first = (int)(std::max<int64_t>(0, (int64_t)pos0 - p.window + 1) / 16);
-  // (of the request's pages; the table has left out r.skip of them already)
-  const int skip = std::max(0, first - r.sink_pages - r.skip);
-  const int last = pos1 / 16 < r.sink_pages ? pos1 / 16 : pos1 / 16 - r.skip;
-  return {skip, std::min(entries, last + 1) - skip};
+constexpr double kStreamPage = 1.6;  // time of a stream's page, in tile pages
+inline void order_items(std::vector<Cost>& tiles, std::vector<Cost>& streams, int nkv,
+                        std::vector<SpanItem>& out) {
+  auto longer = [](const Cost& a, const Cost& b) { return a.cost > b.cost; };
+  double sum[2] = {};
+  std::vector<Cost>* list[2] = {&tiles, &streams};
+  for (int k = 0; k < 2; k++) {
+    if (!std::is_sorted(list[k]->begin(), list[k]->end(), longer))
+      std::stable_sort(list[k]->begin(), list[k]->end(), longer);
+    for (const Cost& c : *list[k]) sum[k] += c.cost * (k ? kStreamPage : 1.0);
+  }
+  const double all = sum[0] + sum[1];
+  const double share = tiles.empty() ? 1.0 : 1.0 - tiles[0].cost * (double)kSlots / (all * nkv);
+  out.reserve(tiles.size() + streams.size());
+  size_t j = 0;
+  double done[2] = {};
+  for (size_t i = 0; i < tiles.size() || j < streams.size();) {
+    const bool tile = i < tiles.size() && (j >= streams.size() || done[0] * share * all <= (done[0] + done[1]) * sum[0]);
+    if (tile) done[0] += tiles[i].cost, out.push_back(tiles[i++].item);
+    else done[1] += streams[j].cost * kStreamPage, out.push_back(streams[j++].item);
+  }
 }
 
 }  // namespace plan
 
-// Cuts the parts into items and orders them.  entries[i]: table entries of rows record i.
-inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts,
-                       const std::vector<int>& entries) {
+// Cuts the records' rows into items and orders them.
+inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
   using namespace plan;
-  // how much there is to do: pages of streams, and of tiles
-  int64_t stream_pages = 0, tile_pages = 0;
-  for (const Part& part : parts) {
-    const SpanRows& r = p.rows[part.rows];
-    const int step = part.stream ? 16 : kSpanTileRows;
+  auto seen = [&](const SpanRows& r, int row, int n) {
+    return span_seen(r, row / p.group, (row + n - 1) / p.group, p.window).page1;
+  };
+  // how much there is to do, in pages of one head
+  int64_t pages[2] = {}, n_items[2] = {};
+  int longest = 0;
+  for (size_t i = 0; i < parts.size(); i++) {
+    const SpanRows& r = p.rows[i];
+    const int tile = !parts[i].stream, step = tile ? kSpanTileRows : kSpanStreamRows;
     for (int row = 0; row < r.n_rows; row += step) {
-      const int64_t n = range_of(p, r, entries[part.rows], row, std::min(step, r.n_rows - row)).end;
-      (part.stream ? stream_pages : tile_pages) += n * p.nkv;
+      const int n = seen(r, row, std::min(step, r.n_rows - row));
+      pages[tile] += n;
+      n_items[tile]++;
+      if (!tile) longest = std::max(longest, n);
     }
   }
-  const int stream_split = (int)std::max<int64_t>(kMinSplitPages, (stream_pages + 1023) / 1024 + 1) & ~1;
-  const int tile_split = (int)std::max<int64_t>(kMinTilePages, (tile_pages + kSlots - 1) / kSlots + 1) & ~1;
-  std::vector<SpanItem> list[2];
+  // Streams run whole where that fills the chip about evenly, and where they are short: a
+  // split costs the merge's launch, which is what a few dozen pages take.
+  const auto even = [](int64_t n) { return (int)(n + 1) & ~1; };
+  const int64_t share = pages[0] * p.nkv / kSlots;  // of a workgroup that the chip holds at once
+  const bool whole = longest <= std::max<int64_t>(kWholePages, share + share / 4);
+  const int stream_split = whole ? longest : even(std::max<int64_t>(kMinSplitPages, share / 2));
+  const int tile_split = even(std::max<int64_t>(kMinTilePages, (pages[1] * p.nkv + kTileSlots - 1) / kTileSlots));
+  std::vector<Cost> list[2];
   int64_t extra = kExtraTiles;
-  for (const Part& part : parts) {
-    const SpanRows& r = p.rows[part.rows];
-    const int step = part.stream ? 16 : kSpanTileRows;
-    // splits: as many for every item of the part, so that a row's partials are found
-    int most = 0;
+  for (size_t i = 0; i < parts.size(); i++) {
+    SpanRows& r = p.rows[i];
+    const int tile = !parts[i].stream, step = tile ? kSpanTileRows : kSpanStreamRows;
+    // as many splits for every item of the record
+    int most = 0, n_split = 1;
     for (int row = 0; row < r.n_rows; row += step)
-      most = std::max(most, range_of(p, r, entries[part.rows], row, std::min(step, r.n_rows - row)).end);
-    int n_split = std::max(1, most / (part.stream ? stream_split : tile_split));
-    if (!part.stream) {
+      most = std::max(most, seen(r, row, std::min(step, r.n_rows - row)));
+    if (!tile) {
+      n_split = std::max(1, (most + stream_split / 2) / std::max(1, stream_split));
+    } else if (most > kWholePages || parts[i].partial) {
+      n_split = std::max(1, most / tile_split);
       const int64_t tiles = (int64_t)((r.n_rows + step - 1) / step) * p.nkv;
       n_split = (int)std::min<int64_t>(n_split, 1 + extra / tiles);
       extra -= (n_split - 1) * tiles;
     }
-    const bool partial = part.partial || n_split > 1;
-    if (partial) {
-      SpanSource& s = p.sources[part.source];
-      s.base = (int32_t)p.n_parts;
-      s.split_stride = r.n_rows;
-      s.kvh_stride = n_split * r.n_rows;
-      s.n_split = n_split;
+    n_split = std::min(n_split, kMostSplits);
+    r.n_split = n_split;
+    r.part = -1;
+    if (parts[i].partial || n_split > 1) {
+      r.part = (int32_t)p.n_parts;
+      p.n_parts += (int64_t)p.nkv * n_split * r.n_rows;
     }
-    for (int g = 0; g < p.nkv; g++)
+    // (tiles that take the same keys follow each other)
+    for (int s = 0; s < n_split; s++)
       for (int row = 0; row < r.n_rows; row += step) {
         const int n = std::min(step, r.n_rows - row);
-        const Range range = range_of(p, r, entries[part.rows], row, n);
-        const int chunks = (range.end + 1) / 2;
-        for (int s = 0; s < n_split; s++) {
-          // (empty where a tile has fewer chunks than splits: its rows' partials are zeros)
-          const int page0 = 2 * (int)((int64_t)chunks * s / n_split);
-          const int page1 = std::min(range.end, 2 * (int)((int64_t)chunks * (s + 1) / n_split));
-          const int64_t part_at = partial ? p.n_parts + ((int64_t)g * n_split + s) * r.n_rows + row : -1;
-          list[part.stream ? 0 : 1].push_back(SpanItem{part.rows, (int16_t)g, (int8_t)(part.stream ? 0 : 1),
-                                                       (uint8_t)n, row, page0, page1, range.skip,
-                                                       (int32_t)part_at, 0});
-        }
+        const int cost = std::max(1, seen(r, row, n) / n_split);
+        list[tile].push_back(Cost{SpanItem{(int32_t)i, row, row / p.group, (uint16_t)s, (uint8_t)tile, (uint8_t)n},
+                                  cost});
       }
-    if (partial) p.n_parts += (int64_t)p.nkv * n_split * r.n_rows;
   }
-  auto longer = [](const SpanItem& a, const SpanItem& b) {
-    return a.page_end - a.page0 > b.page_end - b.page0;
-  };
-  for (auto& l : list) std::stable_sort(l.begin(), l.end(), longer);
   p.has_tiles = !list[1].empty();
-  p.items = std::move(list[1]);
-  p.items.insert(p.items.end(), list[0].begin(), list[0].end());
+  // (streams find nothing in L2, and long tiles of the last heads would start too late)
+  p.heads = list[0].empty() ? std::min(p.nkv, 8) : p.nkv;
+  order_items(list[1], list[0], p.nkv, p.items);
 }
 
-// The merges of the requests' tokens: of each request its sources, whose bases count from
-// its first token.
+// The merges of the requests' tokens.
 struct RequestSources {
   int tok, n_new;
-  std::vector<std::pair<int, int>> from;  // (source, the request's first token in it)
+  std::vector<SpanSource> from;
 };
 inline void plan_merges(SpanPlan& p, const std::vector<RequestSources>& reqs) {
-  std::vector<SpanSource> out;
   for (const RequestSources& q : reqs) {
     int n = 0;
-    SpanMerge m{q.tok, (int)out.size(), 0, 0};
-    for (const auto& f : q.from) {
-      SpanSource s = p.sources[f.first];
-      if (s.n_split == 0) continue;  // the rows went to the output
-      s.base += f.second * p.group;
-      n += s.n_split;
-      out.push_back(s);
+    SpanMerge m{q.tok, (int)p.sources.size(), 0};
+    for (const SpanSource& s : q.from) {
+      if (p.rows[s.rows].part < 0) continue;  // the rows went to the output
+      n += p.rows[s.rows].n_split;
+      p.sources.push_back(s);
       m.n_src++;
     }
     if (m.n_src == 0) continue;
@@ -175,16 +196,19 @@ inline void plan_merges(SpanPlan& p, const std::vector<RequestSources>& reqs) {
     for (int i = 0; i < q.n_new; i++) p.merge_tokens.push_back(SpanToken{q.tok + i, (int)p.merges.size()});
     p.merges.push_back(m);
   }
-  p.sources = std::move(out);
+}
+
+inline void plan_shape(const mx_attn_shape* s, SpanPlan& p) {
+  p.nkv = s->n_kv_heads;
+  p.group = s->n_q_heads / s->n_kv_heads;
+  p.page_bytes = 16 * 2 * 2 * s->head_dim;
 }
 
 inline void plan_window(const mx_batch* b, const mx_attn_shape* s, int window, int sinks, SpanPlan& p) {
-  p.nkv = s->n_kv_heads;
-  p.group = s->n_q_heads / s->n_kv_heads;
+  plan_shape(s, p);
   p.window = window;
   p.sinks = sinks;
   std::vector<plan::Part> parts;
-  std::vector<int> entries;
   std::vector<RequestSources> reqs;
   int tok = 0;
   for (int r = 0; r < b->num_reqs; r++) {
@@ -192,31 +216,27 @@ inline void plan_window(const mx_batch* b, const mx_attn_shape* s, int window, i
     const SeenPages seen = seen_pages(q.ctx_len, q.n_new, window, sinks);
     const int at = p.add_table(q.pages, seen.sink_pages);
     p.add_table(q.pages + seen.sink_pages + seen.skip, seen.entries() - seen.sink_pages);
-    p.rows.push_back(SpanRows{tok, q.n_new * p.group, q.ctx_len, 0, at, seen.sink_pages, seen.skip, 0});
-    entries.push_back(seen.entries());
-    parts.push_back(plan::Part{r, q.n_new == 1, false, r});
+    p.rows.push_back(SpanRows{tok, q.n_new * p.group, q.ctx_len, 0, at, seen.entries(), seen.sink_pages, seen.skip, 1, -1});
+    parts.push_back(plan::Part{q.n_new == 1, false});
     reqs.push_back(RequestSources{tok, q.n_new, {{r, 0}}});
     tok += q.n_new;
   }
-  p.sources.assign(b->num_reqs, SpanSource{0, 0, 0, 0});
-  plan_items(p, parts, entries);
+  plan_items(p, parts);
   plan_merges(p, reqs);
 }
 
-// Shared runs: start[r] of a request's pages belong to runs; first[i] is the first page of
-// run i in its members' tables.
+// A prompt whose rows fill tiles by themselves takes its shared keys with its own: the rows
+// that would be saved, times the keys, against partials for all of its rows.
+constexpr int64_t kWholePromptKeys = 1024;
+
 inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
                         const mx_shared_run* runs, SpanPlan& p) {
-  p.nkv = s->n_kv_heads;
-  p.group = s->n_q_heads / s->n_kv_heads;
+  plan_shape(s, p);
   const int R = b->num_reqs;
   std::vector<plan::Part> parts;
-  std::vector<int> entries;
   std::vector<RequestSources> reqs(R);
-  std::vector<int> start(R, 0), own(R, 0);  // pages before: in runs so far; not the request's own
-  // A prompt whose rows fill tiles by themselves takes its shared keys with its own: the
-  // rows that would be saved, times the keys, against partials for all of its rows.
-  std::vector<char> whole(R, 0);
+  std::vector<int> start(R, 0), own(R, 0);  // pages of the runs so far; of the runs that r takes part in
+  std::vector<char> whole(R, 0);            // takes no part in runs from here on
   for (int i = 0; i < num_runs; i++)
     for (int r = runs[i].first_req; r < runs[i].first_req + runs[i].num_reqs; r++) start[r] += runs[i].n_pages;
   int tok = 0;
@@ -224,13 +244,18 @@ inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
     const mx_request& q = b->reqs[r];
     const int64_t rows = (int64_t)q.n_new * p.group;
     const int64_t spare = (rows + kSpanTileRows - 1) / kSpanTileRows * kSpanTileRows - rows;
-    whole[r] = q.n_new > 1 && spare * start[r] * 16 <= rows * 1024;
+    whole[r] = q.n_new > 1 && spare * start[r] * 16 <= rows * kWholePromptKeys;
     reqs[r] = RequestSources{tok, q.n_new, {}};
     tok += q.n_new;
     start[r] = 0;
   }
-  // how many requests take part in each run; a run of one is that request's own
+  int64_t saved = 0;
   for (int i = 0; i < num_runs; i++) {
+    int takers = 0;
+    for (int r = runs[i].first_req; r < runs[i].first_req + runs[i].num_reqs; r++) takers += !whole[r];
+    if (takers > 1) saved += (takers - 1) * (int64_t)runs[i].n_pages * p.nkv * p.page_bytes;
+  }
+  for (int i = 0; saved >= p.min_shared_bytes && i < num_runs; i++) {
     const mx_shared_run& run = runs[i];
     const int end = run.first_req + run.num_reqs;
     int takers = 0, n_tok = 0, leader = -1;
@@ -247,34 +272,28 @@ inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
       whole[leader] = 1;
       continue;
     }
-    const int rec = (int)p.rows.size(), src = (int)p.sources.size();
-    p.sources.push_back(SpanSource{0, 0, 0, 0});
-    const int list = (int)p.tokens.size();
+    const int rec = (int)p.rows.size(), list = (int)p.tokens.size();
     int at = 0;
     for (int r = run.first_req; r < end; r++) {
       if (whole[r]) continue;
-      reqs[r].from.push_back({src, at});
+      reqs[r].from.push_back(SpanSource{rec, at});
       for (int t = 0; t < b->reqs[r].n_new; t++) p.tokens.push_back(reqs[r].tok + t);
       at += b->reqs[r].n_new;
       own[r] = start[r];
     }
     const int pages = p.add_table(b->reqs[leader].pages + first, run.n_pages);
-    p.rows.push_back(SpanRows{list, n_tok * p.group, INT32_MAX / 2, 1, pages, 0, 0, 0});
-    entries.push_back(run.n_pages);
-    parts.push_back(plan::Part{rec, n_tok * p.group <= 16, true, src});
+    p.rows.push_back(SpanRows{list, n_tok * p.group, INT32_MAX / 2, 1, pages, run.n_pages, 0, 0, 1, -1});
+    parts.push_back(plan::Part{n_tok * p.group <= kSpanStreamRows, true});
   }
   for (int r = 0; r < R; r++) {
     const mx_request& q = b->reqs[r];
     const int end = (q.ctx_len + q.n_new - 1) / 16 + 1;
-    const int rec = (int)p.rows.size(), src = (int)p.sources.size();
-    p.sources.push_back(SpanSource{0, 0, 0, 0});
+    reqs[r].from.push_back(SpanSource{(int)p.rows.size(), 0});
     const int pages = p.add_table(q.pages + own[r], end - own[r]);
-    p.rows.push_back(SpanRows{reqs[r].tok, q.n_new * p.group, q.ctx_len, 0, pages, 0, own[r], 0});
-    entries.push_back(end - own[r]);
-    parts.push_back(plan::Part{rec, q.n_new == 1, own[r] > 0, src});
-    reqs[r].from.push_back({src, 0});
+    p.rows.push_back(SpanRows{reqs[r].tok, q.n_new * p.group, q.ctx_len, 0, pages, end - own[r], 0, own[r], 1, -1});
+    parts.push_back(plan::Part{q.n_new == 1, own[r] > 0});
   }
-  plan_items(p, parts, entries);
+  plan_items(p, parts);
   plan_merges(p, reqs);
 }
 

@@ -49,36 +49,39 @@ static void walk(const Case& c, const SpanPlan& p) {
   std::vector<char> written(p.n_parts, 0);
   std::map<int, std::vector<std::pair<int, int>>> at_part;  // partial -> (page id, first key)
   std::map<int, std::pair<int, int>> part_row;
-  for (const SpanItem& it : p.items) {
+  for (int b = 0; b < p.blocks(); b++) {
+    const SpanBlock at_b = span_block(b, (int)p.items.size(), p.nkv, p.heads);
+    CHECK(at_b.item >= 0 && at_b.item < (int)p.items.size() && at_b.kvh >= 0 && at_b.kvh < p.nkv, "block %d", b);
+    const SpanItem& it = p.items[at_b.item];
     CHECK(it.rows >= 0 && it.rows < (int)p.rows.size(), "rows");
     const SpanRows& rw = p.rows[it.rows];
-    CHECK(it.kvh >= 0 && it.kvh < c.nkv && it.n_rows >= 1, "kvh %d", it.kvh);
-    CHECK(it.row0 + it.n_rows <= rw.n_rows && it.n_rows <= (it.kind ? kSpanTileRows : 16), "rows of an item");
-    CHECK(it.page0 % 2 == 0 && it.page0 >= 0, "page0 %d", it.page0);
-    if (it.page0 >= it.page_end) CHECK(it.part >= 0, "an empty item without partials");
-    if (it.kind == 0) {
-      const int a = it.row0 / group, b = (it.row0 + it.n_rows - 1) / group;
-      CHECK(rw.list || a == b, "a stream's rows are of one position");
-      CHECK(rw.list || a == 0, "a stream's position");
-    }
+    CHECK(it.n_rows >= 1 && it.row0 + it.n_rows <= rw.n_rows, "rows of an item");
+    CHECK(it.n_rows <= (it.kind ? kSpanTileRows : kSpanStreamRows), "rows of an item");
+    CHECK(it.tok0 == it.row0 / group, "tok0");
+    CHECK(it.split < rw.n_split && (rw.n_split == 1 || rw.part >= 0), "split");
+    const SpanPages pg = span_split(span_seen(rw, it.tok0, (it.row0 + it.n_rows - 1) / group, p.window), it.split, rw.n_split);
+    CHECK(pg.page0 % 2 == 0 && pg.page0 >= 0, "page0 %d", pg.page0);
+    if (pg.page0 >= pg.page1) CHECK(rw.part >= 0, "an empty item without partials");
+    if (it.kind == 0 && !rw.list) CHECK(rw.n_rows == group, "a stream's rows are of one position");
     std::vector<std::pair<int, int>> keys;
-    for (int v = it.page0; v < it.page_end; v++) {
-      const int t = v < rw.sink_pages ? v : v + it.skip;
-      const int real = v < rw.sink_pages ? v : v + it.skip + rw.skip;
-      CHECK(rw.pages + t >= 0 && rw.pages + t < (int)flat.size(), "table entry");
+    for (int v = pg.page0; v < pg.page1; v++) {
+      const int t = v < rw.sink_pages ? v : v + pg.skip;
+      const int real = v < rw.sink_pages ? v : v + pg.skip + rw.skip;
+      CHECK(t < rw.entries && rw.pages + t >= 0 && rw.pages + t < (int)flat.size(), "table entry");
       keys.push_back({flat[rw.pages + t], rw.list ? -1 : 16 * real});
     }
     for (int i = 0; i < it.n_rows; i++) {
-      const int row = it.row0 + i, tk = row / group, h = it.kvh * group + row % group;
+      const int row = it.row0 + i, tk = row / group, h = at_b.kvh * group + row % group;
       const int tok = rw.list ? p.tokens.at(rw.tok + tk) : rw.tok + tk;
       CHECK(tok >= 0 && tok < T, "token %d", tok);
       CHECK(rw.list || rw.pos + tk == tok_pos[tok], "position");
-      if (it.part >= 0) {
-        CHECK(it.part + i < p.n_parts, "partial %d of %lld", it.part + i, (long long)p.n_parts);
-        CHECK(!written[it.part + i], "partial %d twice", it.part + i);
-        written[it.part + i] = 1;
-        at_part[it.part + i] = keys;
-        part_row[it.part + i] = {tok, h};
+      if (rw.part >= 0) {
+        const int at = rw.part + (at_b.kvh * rw.n_split + it.split) * rw.n_rows + row;
+        CHECK(at < p.n_parts, "partial %d of %lld", at, (long long)p.n_parts);
+        CHECK(!written[at], "partial %d twice", at);
+        written[at] = 1;
+        at_part[at] = keys;
+        part_row[at] = {tok, h};
       } else {
         got[{tok, h}].parts.push_back({-1, keys});
       }
@@ -92,8 +95,9 @@ static void walk(const Case& c, const SpanPlan& p) {
       const int g = h / group;
       for (int s = 0; s < m.n_src; s++) {
         const SpanSource& src = p.sources.at(m.src + s);
-        for (int k = 0; k < src.n_split; k++) {
-          const int at = (tk.tok - m.tok) * group + h - g * group + src.base + g * src.kvh_stride + k * src.split_stride;
+        const SpanRows& rw = p.rows.at(src.rows);
+        for (int k = 0; k < rw.n_split; k++) {
+          const int at = rw.part + (g * rw.n_split + k) * rw.n_rows + (src.tok + tk.tok - m.tok) * group + h - g * group;
           CHECK(at >= 0 && at < p.n_parts && written[at], "merge reads partial %d", at);
           CHECK(part_row[at] == std::make_pair(tk.tok, h), "partial %d is another row's", at);
           CHECK(used.insert(at).second, "partial %d read twice", at);
@@ -156,7 +160,7 @@ int main(int argc, char** argv) {
         bool same = true;
         for (int r = first; r < first + num; r++) same &= shared[r].size() == shared[first].size();
         if (!same) continue;
-        const int pages = log_in(9);
+        const int pages = log_in(in(0, 3) ? 8 : 12);
         for (int i = 0; i < pages; i++, next++)
           for (int r = first; r < first + num; r++) shared[r].push_back(next);
         c.runs.push_back({first, num, pages});
@@ -180,6 +184,7 @@ int main(int argc, char** argv) {
       if (in(0, 9) == 0) c.window = INT32_MAX;
       plan_window(&b, &shape, c.window, c.sinks, p);
     } else {
+      if (in(0, 3)) p.min_shared_bytes = 0;
       plan_shared(&b, &shape, (int)c.runs.size(), c.runs.data(), p);
     }
     const int before = errors;

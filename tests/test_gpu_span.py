@@ -38,12 +38,11 @@ class Pools:
     def shape(self, nq, scale=0.0):
         return mx.attn_shape(nq, self.nkv, self.d, self.pages, scale)
 
-    def fill(self, rng, table, first, end):
-        """Positions first .. end - 1 of a request with plausible values."""
-        for p in range(first, end):
-            page = table[p // 16]
-            self.hk[page, :, p % 16] = bf16(rng.normal(0, 1, (self.nkv, self.d)))
-            self.hv[page, :, p % 16] = bf16(rng.normal(0, 1, (self.nkv, self.d)))
+    def fill(self, rng, table, j):
+        """The positions j of a request with plausible values."""
+        pg, sl = torch.as_tensor(np.asarray(table)[j // 16]), torch.as_tensor(j % 16)
+        for pool in (self.hk, self.hv):
+            pool[pg, :, sl] = bf16(rng.normal(0, 1, (len(j), self.nkv, self.d)))
 
     def dense(self, table, j):
         pg, sl = np.asarray(table)[j // 16], j % 16
@@ -121,9 +120,10 @@ def window_case(nq, nkv, d, reqs, seed, window, sinks, spread=1.0):
     for decode, n, ctx in reqs:
         see = seen(n, ctx, window, sinks).any(0)
         table = [next(order) if see[16 * i:16 * i + 16].any() else -1 - i for i in range(-(-(n + ctx) // 16))]
-        for p in np.flatnonzero(see):
-            pools.hk[table[p // 16], :, p % 16] = bf16(rng.normal(0, spread, (nkv, d)))
-            pools.hv[table[p // 16], :, p % 16] = bf16(rng.normal(0, 1, (nkv, d)))
+        pools.fill(rng, table, np.flatnonzero(see))
+        if spread != 1.0:
+            pg = torch.as_tensor([p for p in table if p >= 0])
+            pools.hk[pg] = (pools.hk[pg].double() * spread).to(torch.bfloat16)
         full.append((decode, n, ctx, table))
     pools.upload()
     return pools, full, bf16(rng.normal(0, 1, (sum(r[1] for r in reqs), nq, d)))
@@ -223,20 +223,22 @@ def shared_case(nq, nkv, d, reqs, runs, seed):
     pools = Pools(pages, nkv, d)
     for first, n, k in runs:
         ids = [next(order) for _ in range(k)]
-        pools.fill(rng, ids, 0, 16 * k)
+        pools.fill(rng, ids, np.arange(16 * k))
         for r in range(first, first + n):
             tables[r] += ids
     full = []
     for (decode, n, own), t in zip(reqs, tables):
         c = 16 * len(t)
         mine = [next(order) for _ in range(-(-(own + n) // 16))]
-        pools.fill(rng, mine, 0, own + n)
+        pools.fill(rng, mine, np.arange(own + n))
         full.append((decode, n, c + own, t + mine))
     pools.upload()
     return pools, full, bf16(rng.normal(0, 1, (sum(r[1] for r in reqs), nq, d)))
 
 
 D, P = 1, 0
+# (runs are taken apart from their requests where that saves 24 MB of reads: `more` decodes
+# of a run of their own, of as many pages as that takes, go with the requests that follow)
 SHARED = [
     ([(D, 1, 0), (D, 1, 0)], [(0, 2, 1)]),
     ([(D, 1, c) for c in (0, 1, 15, 16, 17, 100, 333)], [(0, 7, 9)]),
@@ -253,10 +255,15 @@ SHARED = [
 ]
 
 
+@pytest.mark.parametrize("more", [0, 24])
 @pytest.mark.parametrize("case", range(len(SHARED)))
 @pytest.mark.parametrize("nq,nkv,d", SHAPES)
-def test_shared(nq, nkv, d, case):
+def test_shared(nq, nkv, d, case, more):
     reqs, runs = SHARED[case]
+    if more:
+        pages = -(-(24 << 20) // ((more - 1) * 64 * d * nkv))
+        runs = runs + [(len(reqs), more, pages)]
+        reqs = reqs + [(D, 1, i) for i in range(more)]
     pools, reqs, q = shared_case(nq, nkv, d, reqs, runs, 17 * case + nq)
     out, mag = reference(pools, nq, reqs, q)
     got, ws = run_shared(pools, nq, reqs, runs, q.cuda())
@@ -282,6 +289,7 @@ def test_shared_not_finite(bad):
     """A value that is no number in a run reaches all of the run's rows; in a chunk's own
     tokens those behind it."""
     reqs, runs = [(D, 1, 20), (P, 30, 0), (D, 1, 4), (D, 1, 9)], [(0, 3, 12), (1, 2, 4)]
+    runs, reqs = runs + [(4, 24, 70)], reqs + [(D, 1, i) for i in range(24)]  # (enough to be taken apart)
     pools, reqs, q = shared_case(8, 2, 128, reqs, runs, 31)
     hk = pools.hv.clone()
     # of request 1: position 100 of the first run (rows of 0, 1, 2), 200 of the second (1, 2)
@@ -314,7 +322,7 @@ def test_rows_behind_stay_and_output_in_place():
     run_window(pools, 8, reqs, buf, 64, 2, out=buf)
     check(buf[:len(q)], out, mag)
     assert (buf[len(q):] == 3).all()
-    reqs, runs = [(D, 1, 20), (P, 30, 0), (P, 400, 7)], [(0, 3, 12)]
+    reqs, runs = [(D, 1, 20), (P, 30, 0), (P, 400, 7)] + [(D, 1, 3)] * 40, [(0, 43, 80)]
     pools, reqs, q = shared_case(8, 2, 64, reqs, runs, 43)
     out, mag = reference(pools, 8, reqs, q)
     buf = torch.full((len(q) + 5, 8, 64), 3.0, dtype=torch.bfloat16, device="cuda")
@@ -345,7 +353,7 @@ def test_pools_beyond_4_gib():
     k = torch.empty((pages, nkv, d // 32, 16, 32), dtype=torch.bfloat16, device="cuda")
     v = torch.empty((pages, nkv, d, 16), dtype=torch.bfloat16, device="cuda")
     small = Pools(80, nkv, d)
-    small.fill(rng, list(range(80)), 0, 1280)
+    small.fill(rng, list(range(80)), np.arange(1280))
     small.upload()
     far = pages - 80
     k[far:], v[far:] = small.k, small.v
@@ -449,8 +457,8 @@ def test_streams_and_threads():
     for i in range(2):
         reqs = [(1, 1, 300 + 100 * i), (0, 60, 40), (1, 1, 1500)]
         pools, reqs, q = window_case(8, 2, 64, reqs, 81 + i, 100, 4)
-        sh, sreqs, sq = shared_case(8, 2, 64, [(D, 1, 9 * k) for k in range(9)], [(0, 9, 50 + i)], 91 + i)
-        cases.append((pools, reqs, q.cuda(), reference(pools, 8, reqs, q, 100, 4), sh, sreqs, [(0, 9, 50 + i)],
+        sh, sreqs, sq = shared_case(8, 2, 64, [(D, 1, 9 * k) for k in range(33)], [(0, 33, 100 + i)], 91 + i)
+        cases.append((pools, reqs, q.cuda(), reference(pools, 8, reqs, q, 100, 4), sh, sreqs, [(0, 33, 100 + i)],
                       sq.cuda(), reference(sh, 8, sreqs, sq)))
     torch.cuda.synchronize()
     errors = []
