@@ -8,11 +8,9 @@ namespace mx {
 
 struct SpanParams {
   AttnParams a;  // reqs, items, split_pages and decode_only unused
-  const SpanRows* rows;
   const SpanItem* items;
   const int32_t* tokens;
   const SpanToken* merge_tokens;
-  const SpanMerge* merges;
   const SpanSource* sources;
   int32_t window, sinks;
   int32_t n_items;    // of each KV head

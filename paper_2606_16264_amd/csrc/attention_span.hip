@@ -29,9 +29,9 @@ __device__ __forceinline__ RowState span_row_start() { return RowState{kLowest, 
 // Where an item's pages lie, and what a position sees of them.
 struct Span {
   int sink_pages, skip_table, skip_real, page0, page_end, window, sinks;
-  __device__ __forceinline__ Span(const SpanParams& p, const SpanPages& pg, const SpanRows& rw)
-      : sink_pages(rw.sink_pages), skip_table(pg.skip), skip_real(pg.skip + rw.skip), page0(pg.page0),
-        page_end(pg.page1), window(p.window), sinks(p.sinks) {}
+  __device__ __forceinline__ Span(const SpanParams& p, const SpanItem& it)
+      : sink_pages(it.sink_pages), skip_table(it.skip_table), skip_real(it.skip_real), page0(it.page0),
+        page_end(it.page1), window(p.window), sinks(p.sinks) {}
   __device__ __forceinline__ int entry(int v) const { return v < sink_pages ? v : v + skip_table; }
   __device__ __forceinline__ int first_key(int v) const {  // of page v, as a position
     return 16 * (v < sink_pages ? v : v + skip_real);
@@ -139,31 +139,35 @@ __device__ __forceinline__ void drop_not_finite(u32x4& v) {
     v[i] &= ~(((((v[i] & 0x7F807F80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xFFFFu);
 }
 
-// Rows of an item by their place in it: the token (of the record's) and the q head.
+// Page ids through the constant address space: uniform reads of tables that nothing writes
+// during the launch, so they are scalar loads.
+typedef const __attribute__((address_space(4))) int32_t* ConstInts;
+
+// An item's rows by their place in it: the token, counted from the first row's, and the q head.
 struct ItemRows {
-  int tok0, rest, group;
+  int rest, group;
   uint32_t inv;
   __device__ __forceinline__ ItemRows(const SpanParams& p, const SpanItem& it)
-      : tok0(it.tok0), rest(it.row0 - it.tok0 * p.a.group), group(p.a.group), inv(p.group_inv) {}
+      : rest(it.rest), group(p.a.group), inv(p.group_inv) {}
   __device__ __forceinline__ int token(int i) const {  // (exact for rest + i < 2^16)
-    return tok0 + (group == 1 ? i : (int)__umulhi((unsigned)(rest + i), inv));
+    return group == 1 ? i : (int)__umulhi((unsigned)(rest + i), inv);
   }
-  __device__ __forceinline__ int head(int i, int token) const { return rest + i - (token - tok0) * group; }
+  __device__ __forceinline__ int head(int i, int token) const { return rest + i - token * group; }
 };
 // A row's place in the batch.
 struct RowAt {
   int64_t tok;
   int head, pos;
 };
-__device__ __forceinline__ RowAt row_at(const SpanParams& p, const SpanRows& rw, const ItemRows& rows,
-                                        int kvh, int i) {
+__device__ __forceinline__ RowAt row_at(const SpanParams& p, const SpanItem& it, int kvh, int i) {
+  const ItemRows rows(p, it);
   const int t = rows.token(i), h = kvh * p.a.group + rows.head(i, t);
-  if (rw.list) return RowAt{p.tokens[rw.tok + t], h, rw.pos};
-  return RowAt{rw.tok + t, h, rw.pos + t};
+  if (it.list) return RowAt{p.tokens[it.tok + t], h, it.pos};
+  return RowAt{it.tok + t, h, it.pos + t};
 }
 // The partial of the item's first row.
-__device__ __forceinline__ int64_t part_of(const SpanRows& rw, const SpanItem& it, int kvh) {
-  return rw.part + ((int64_t)kvh * rw.n_split + it.split) * rw.n_rows + it.row0;
+__device__ __forceinline__ int64_t part_of(const SpanItem& it, int kvh) {
+  return it.part + (int64_t)kvh * it.kvh_stride;
 }
 
 static_assert(kSpanTileRows == 4 * 32, "four waves of two 16-row blocks");
@@ -173,34 +177,20 @@ static_assert(kSpanTileRows == 4 * 32, "four waves of two 16-row blocks");
 // first_whole to end_whole, take no masks; those before (the window's low edge, sinks) and
 // behind (the diagonal, the end) do, and a wave leaves out those that none of its rows sees.
 template <int HD>
-__device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& it, const SpanRows& rw,
-                                          const SpanPages& pg, int kvh, char* smem) {
+__device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& it, int kvh, char* smem) {
   using SC = SharedChunk<HD>;
   constexpr int KB = SC::KBYTES, CB = SC::BYTES, NLD = SC::NLD, ND = HD / 32;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15;  // row of this lane within each block
   const int g4 = lane >> 4;   // lane group
-  const Span span(p, pg, rw);
+  const Span span(p, it);
   const ItemRows rows(p, it);
   const int n_rows = it.n_rows;
   const int row0 = 32 * wave;  // the wave's first row, of the item's
-  const int first_page = pg.page0, page_end = pg.page1;
+  const int first_page = it.page0, page_end = it.page1;
   const int n_chunks = (page_end - first_page + 1) / 2;
 
-  bf16x8 qf[ND], qf2[ND];
-  int pos, pos2;
-  {
-    auto load = [&](int row, bf16x8 (&f)[ND], int& at) {
-      const RowAt r = row_at(p, rw, rows, kvh, min(row, n_rows - 1));
-      const uint16_t* qp = p.a.q + r.tok * p.a.q_tok_stride + (int64_t)r.head * HD + 8 * g4;
-#pragma unroll
-      for (int ds = 0; ds < ND; ds++) f[ds] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ds * 32));
-      at = r.pos;
-    };
-    load(row0 + col, qf, pos);
-    load(row0 + 16 + col, qf2, pos2);
-  }
   RowState r1 = span_row_start(), r2 = span_row_start();
   const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
   f32x4 o[HD / 16], o2[HD / 16];
@@ -209,7 +199,7 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
 
   // positions of the tile's rows and of the wave's
   auto pos_of = [&](int row) {
-    return rw.list ? rw.pos : rw.pos + rows.token(min(row, n_rows - 1));
+    return it.list ? it.pos : it.pos + rows.token(min(row, n_rows - 1));
   };
   const int tile_pos0 = pos_of(0), tile_pos1 = pos_of(n_rows - 1);
   const int wave_pos0 = pos_of(row0), wave_pos1 = pos_of(row0 + 31);
@@ -226,10 +216,7 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
     end_whole = max(end_whole, first_whole);
   }
 
-  // page ids through the constant address space: uniform reads of a table nothing writes
-  // during the launch, so they are scalar loads
-  const __attribute__((address_space(4))) int32_t* ptab =
-      (const __attribute__((address_space(4))) int32_t*)(p.a.pages + rw.pages);
+  const ConstInts ptab = (ConstInts)(p.a.pages + it.pages);
   unsigned off[NLD];  // this lane's shares of the wave's copies, bytes from the page's start
 #pragma unroll
   for (int i = 0; i < NLD; i++) {
@@ -257,6 +244,32 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
   auto page_of = [&](int c) {
     return ptab[span.entry(min(first_page + 2 * c + (wave & 1), page_end - 1))];
   };
+  int ua, fa = 0;  // page of the chunk the next copy is for, and of the one after
+  {
+    const int a0 = page_of(0), a1 = page_of(1), a2 = page_of(2);
+    ua = page_of(3);
+    copy(0, a0);
+    copy(1, a1);
+    copy(2, a2);
+  }
+  // the rows' queries, behind the first copies
+  bf16x8 qf[ND], qf2[ND];
+  int pos, pos2;
+  {
+    auto load = [&](int row, bf16x8 (&f)[ND], int& at) {
+      const RowAt r = row_at(p, it, kvh, min(row, n_rows - 1));
+      const uint16_t* qp = p.a.q + r.tok * p.a.q_tok_stride + (int64_t)r.head * HD + 8 * g4;
+#pragma unroll
+      for (int ds = 0; ds < ND; ds++) f[ds] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ds * 32));
+      at = r.pos;
+    };
+    load(row0 + col, qf, pos);
+    load(row0 + 16 + col, qf2, pos2);
+    // (waited for here: their first use is in loops, where the wait would stay, and would
+    // hold for the copies in flight too)
+#pragma unroll
+    for (int ds = 0; ds < ND; ds++) asm volatile("" : "+v"(qf[ds]), "+v"(qf2[ds]), "+v"(pos), "+v"(pos2));
+  }
   const int key0 = 16 * (col >> 3) + 8 * ((col >> 2) & 1) + (col & 3);
   unsigned kaddr[ND];
 #pragma unroll
@@ -339,14 +352,6 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
     raise_max(r1, mx1, scale, inv_scale, o);
     raise_max(r2, mx2, scale, inv_scale, o2);
   };
-  int ua, fa = 0;  // page of the chunk the next copy is for, and of the one after
-  {
-    const int a0 = page_of(0), a1 = page_of(1), a2 = page_of(2);
-    copy(0, a0);
-    copy(1, a1);
-    ua = page_of(3);
-    copy(2, a2);
-  }
   // Top of iteration kt: this wave's copies of chunk kt + 1 have landed, then everyone's, and
   // every read of chunk kt - 1 is done; chunk kt + 3 goes out.  Scalar loads return in any
   // order, so a use of the last iteration's page id behind the issue of the next would wait
@@ -458,7 +463,7 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
       const int v0 = first_page + 2 * c;
       const bf16x8 ones1 = seen_ones(seen_keys(span, v0, pos, g4));
       const bf16x8 ones2 = seen_ones(seen_keys(span, v0, pos2, g4));
-      const int64_t page = p.a.pages[rw.pages + span.entry(min(v0 + (g4 >> 1), page_end - 1))];
+      const int64_t page = p.a.pages[it.pages + span.entry(min(v0 + (g4 >> 1), page_end - 1))];
       const uint16_t* at = p.a.v_pool + (page * p.a.nkv + kvh) * (16 * HD) + col * 16 + 8 * (g4 & 1);
 #pragma unroll
       for (int e = 0; e < HD / 16; e++) {
@@ -474,15 +479,15 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
   const int64_t step32 = p.a.out_tiled ? 512 : 32;
   auto store = [&](int row, float l, const RowState& st, const f32x4 (&acc)[HD / 16]) {
     if (row >= n_rows) return;
-    if (rw.part >= 0) {
-      const int64_t part = part_of(rw, it, kvh) + row;
+    if (it.part >= 0) {
+      const int64_t part = part_of(it, kvh) + row;
 #pragma unroll
       for (int db = 0; db < HD / 16; db++)
         *reinterpret_cast<f32x4*>(p.a.part_o + part * HD + 16 * db + 4 * g4) = acc[db];
       if (g4 == 0) *reinterpret_cast<float2*>(p.a.part_ml + 2 * part) = float2{st.m, l};
       return;
     }
-    const RowAt r = row_at(p, rw, rows, kvh, row);
+    const RowAt r = row_at(p, it, kvh, row);
     const float inv = 1.f / l;
     uint16_t* op = out_ptr(p.a, r.tok, r.head * HD + 4 * g4);
 #pragma unroll
@@ -502,17 +507,15 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
 // registers, and combine through LDS.  Keys that the rows do not see are taken out by
 // select, scores and values, so what their slots hold stays out.
 template <int HD, bool NT, int WAVES>
-__device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem& it, const SpanRows& rw,
-                                            const SpanPages& pg, int kvh, char* smem) {
+__device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem& it, int kvh, char* smem) {
   const int lane = threadIdx.x & 63;
   const int wave = threadIdx.x >> 6;
   const int col = lane & 15;  // row of this lane
   const int g4 = lane >> 4;   // lane group
-  const int page_end = pg.page1;
-  const Span span(p, pg, rw);
-  const ItemRows rows(p, it);
-  const RowAt at = row_at(p, rw, rows, kvh, min(col, it.n_rows - 1));
-  const int pos = rw.list ? rw.pos : rw.pos + it.tok0;  // of every row
+  const int page_end = it.page1;
+  const Span span(p, it);
+  const RowAt at = row_at(p, it, kvh, min(col, it.n_rows - 1));
+  const int pos = it.pos;  // of every row
   RowState r = span_row_start();
   const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
   f32x4 o[HD / 16];
@@ -524,7 +527,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
 #pragma unroll
     for (int ds = 0; ds < HD / 32; ds++) qf[ds] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ds * 32));
   }
-  const int32_t* ptab = p.a.pages + rw.pages;
+  const int32_t* ptab = p.a.pages + it.pages;
   auto pid = [&](int v) { return ptab[span.entry(min(v, page_end - 1))]; };
   auto proc = [&](Chunk<HD>& c, int v) {
     const f32x4 s[2] = {score_block<HD>(c.k[0], qf), score_block<HD>(c.k[1], qf)};
@@ -549,7 +552,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
   // the bf16 attention tells why)
   constexpr int STEP = 2 * WAVES;
   Chunk<HD> ca, cb;
-  int v = pg.page0 + 2 * wave;
+  int v = it.page0 + 2 * wave;
   if (v < page_end) {
     int n0 = pid(v + STEP), n1 = pid(v + STEP + 1);
     load_chunk<HD, NT>(ca, p.a, kvh, pid(v), pid(v + 1), 0, col, g4);
@@ -614,15 +617,15 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
     for (int w = 0; w < WAVES; w++) a += s_o[w][row][dseg + e] * wt[w];
     acc[e] = a;
   }
-  if (rw.part < 0) {
-    const RowAt to = row_at(p, rw, rows, kvh, row);
+  if (it.part < 0) {
+    const RowAt to = row_at(p, it, kvh, row);
     const float inv = 1.f / L;
     uint16_t* op = out_ptr(p.a, to.tok, to.head * HD + dseg);  // EL dims within a 32-column block
 #pragma unroll
     for (int e = 0; e < EL; e += 2)
       *reinterpret_cast<uint32_t*>(op + e) = pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
   } else {
-    const int64_t part = part_of(rw, it, kvh) + row;
+    const int64_t part = part_of(it, kvh) + row;
     float* po = p.a.part_o + part * HD + dseg;
 #pragma unroll
     for (int e = 0; e < EL; e += 2) *reinterpret_cast<float2*>(po + e) = float2{acc[e], acc[e + 1]};
@@ -648,12 +651,10 @@ static_assert(sizeof(SmallSpan) <= 4096, "a launch's arguments");
 __device__ __forceinline__ SpanParams inline_params(const SmallSpan& s) {
   SpanParams p = s.p;
   constexpr size_t M = offsetof(SmallSpan, meta);
-  p.rows = inline_meta(M, p.rows);
   p.items = inline_meta(M, p.items);
   p.a.pages = inline_meta(M, p.a.pages);
   p.tokens = inline_meta(M, p.tokens);
   p.merge_tokens = inline_meta(M, p.merge_tokens);
-  p.merges = inline_meta(M, p.merges);
   p.sources = inline_meta(M, p.sources);
   return p;
 }
@@ -670,18 +671,13 @@ template <int HD, bool TILES, int WAVES>
 __device__ __forceinline__ void span_item(const SpanParams& p, char* smem) {
   const SpanBlock b = span_block(blockIdx.x, p.n_items, p.a.nkv, p.heads);
   const SpanItem it = p.items[b.item];
-  const SpanRows rw = p.rows[it.rows];
-  const int tok1 = ItemRows(p, it).token(it.n_rows - 1);
-  const SpanPages pg = span_split(span_seen(rw, it.tok0, tok1, p.window), it.split, rw.n_split);
-  if (pg.page0 >= pg.page1) {
-    empty_item<HD>(p, it, part_of(rw, it, b.kvh));
-    return;
-  }
-  if constexpr (TILES) {
-    if (it.kind == 1) tile_item<HD>(p, it, rw, pg, b.kvh, smem);
-    else stream_item<HD, false, WAVES>(p, it, rw, pg, b.kvh, smem);
+  if (it.page0 >= it.page1) {
+    empty_item<HD>(p, it, part_of(it, b.kvh));
+  } else if constexpr (TILES) {
+    if (it.kind == 1) tile_item<HD>(p, it, b.kvh, smem);
+    else stream_item<HD, false, WAVES>(p, it, b.kvh, smem);
   } else {
-    stream_item<HD, true, WAVES>(p, it, rw, pg, b.kvh, smem);
+    stream_item<HD, true, WAVES>(p, it, b.kvh, smem);
   }
 }
 template <int HD, bool TILES, int WAVES>
@@ -703,7 +699,6 @@ template <int HD, bool WIDE>
 __device__ __forceinline__ void span_merge(const SpanParams& p) {
   constexpr int TPR = HD / 4, G = kMergeThreads / TPR;
   const SpanToken tk = p.merge_tokens[blockIdx.x];
-  const SpanMerge mg = p.merges[tk.merge];
   const int g = threadIdx.x / TPR, d = 4 * (threadIdx.x % TPR);
   const int h = WIDE ? (int)blockIdx.y : (int)blockIdx.y * G + g;
   if (!WIDE && h >= p.a.nq) return;
@@ -711,15 +706,13 @@ __device__ __forceinline__ void span_merge(const SpanParams& p) {
   float m = kLowest, l = 0.f;
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
   int first = WIDE ? g : 0;  // of the next source's splits
-  for (int s = 0; s < mg.n_src; s++) {
-    const SpanSource src = p.sources[mg.src + s];
-    const SpanRows rw = p.rows[src.rows];
-    const int64_t base = rw.part + (int64_t)kvh * rw.n_split * rw.n_rows +
-                         (int64_t)(src.tok + tk.tok - mg.tok) * p.a.group + in_group;
+  for (int s = 0; s < tk.n_src; s++) {
+    const SpanSource src = p.sources[tk.src + s];
+    const int64_t base = src.base + (int64_t)kvh * src.kvh_stride + (int64_t)tk.at * p.a.group + in_group;
     int k = first;
 #pragma unroll 4
-    for (; k < rw.n_split; k += WIDE ? G : 1) {
-      const int64_t at = base + (int64_t)k * rw.n_rows;
+    for (; k < src.n_split; k += WIDE ? G : 1) {
+      const int64_t at = base + (int64_t)k * src.split_stride;
       const float2 ml = *reinterpret_cast<const float2*>(p.a.part_ml + 2 * at);
       const f32x4 o = *reinterpret_cast<const f32x4*>(p.a.part_o + at * HD + d);
       const float mn = fmaxf(m, ml.x);
@@ -728,7 +721,7 @@ __device__ __forceinline__ void span_merge(const SpanParams& p) {
       l = l * a + ml.y * w;
       m = mn;
     }
-    if (WIDE) first = k - rw.n_split;
+    if (WIDE) first = k - src.n_split;
   }
   if constexpr (WIDE) {
     __shared__ float s_acc[G][HD], s_m[G], s_l[G];

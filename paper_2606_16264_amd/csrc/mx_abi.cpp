@@ -1734,12 +1734,12 @@ MX_EXPORT mx_status mx_kv_evict_f8(int32_t num_reqs, const mx_evict_request* req
 namespace {
 
 struct LayoutSpan {
-  size_t rows = 0, pages = 0, tokens = 0, items = 0, merge_tokens = 0, merges = 0, sources = 0,
-         meta_end = 0, part_o = 0, part_ml = 0, total = 0;
+  size_t items = 0, pages = 0, tokens = 0, merge_tokens = 0, sources = 0, meta_end = 0, part_o = 0,
+         part_ml = 0, total = 0;
 };
-LayoutSpan make_layout_span(int64_t n_rows, int64_t n_pages, int64_t n_tokens, int64_t n_items,
-                            int64_t n_merge_tokens, int64_t n_merges, int64_t n_sources,
-                            int64_t n_parts, int head_dim) {
+LayoutSpan make_layout_span(int64_t n_items, int64_t n_pages, int64_t n_tokens,
+                            int64_t n_merge_tokens, int64_t n_sources, int64_t n_parts,
+                            int head_dim) {
   LayoutSpan L;
   size_t o = 0;
   auto take = [&](int64_t n, size_t size) {
@@ -1747,12 +1747,10 @@ LayoutSpan make_layout_span(int64_t n_rows, int64_t n_pages, int64_t n_tokens, i
     o = (o + n * size + 15) / 16 * 16;
     return at;
   };
-  L.rows = take(n_rows, sizeof(SpanRows));
   L.items = take(n_items, sizeof(SpanItem));
   L.pages = take(n_pages, sizeof(int32_t));
   L.tokens = take(n_tokens, sizeof(int32_t));
   L.merge_tokens = take(n_merge_tokens, sizeof(SpanToken));
-  L.merges = take(n_merges, sizeof(SpanMerge));
   L.sources = take(n_sources, sizeof(SpanSource));
   L.meta_end = o;
   o = align_up(o);
@@ -1762,9 +1760,9 @@ LayoutSpan make_layout_span(int64_t n_rows, int64_t n_pages, int64_t n_tokens, i
   return L;
 }
 LayoutSpan layout_span(const SpanPlan& p, const mx_attn_shape* s) {
-  return make_layout_span((int64_t)p.rows.size(), p.n_pages, (int64_t)p.tokens.size(),
-                          (int64_t)p.items.size(), (int64_t)p.merge_tokens.size(),
-                          (int64_t)p.merges.size(), (int64_t)p.sources.size(), p.n_parts, s->head_dim);
+  return make_layout_span((int64_t)p.items.size(), (int64_t)p.pages.size(), (int64_t)p.tokens.size(),
+                          (int64_t)p.merge_tokens.size(), (int64_t)p.sources.size(), p.n_parts,
+                          s->head_dim);
 }
 
 // The bound for requests that belong to at most `depth` runs each: every request has a part
@@ -1781,7 +1779,7 @@ size_t span_bound(const mx_attn_shape* s, int32_t max_tokens, int32_t max_reqs, 
   const int64_t streams = max_pages / plan::kMinSplitPages + parts;
   const int64_t items = streams * ceil_div(group, kSpanStreamRows) +
                         ceil_div(tokens * group, kSpanTileRows) + parts + plan::kExtraTiles;
-  return make_layout_span(parts, max_pages, tokens, items, max_tokens, max_reqs, parts,
+  return make_layout_span(items, max_pages, tokens, max_tokens, parts,
                           streams * nkv * std::max<int64_t>(kSpanStreamRows, group) +
                               tokens * s->n_q_heads + (int64_t)plan::kExtraTiles * kSpanTileRows,
                           s->head_dim)
@@ -1824,7 +1822,7 @@ mx_status validate_runs(const mx_batch* b, int32_t num_runs, const mx_shared_run
 }
 
 mx_status check_span_plan(const SpanPlan& p) {
-  if (p.n_parts > INT32_MAX || p.n_pages > INT32_MAX || p.blocks() > INT32_MAX / 2)
+  if (p.n_parts > INT32_MAX || p.pages.size() > (size_t)INT32_MAX || p.blocks() > INT32_MAX / 2)
     return fail(MX_ERR_TOO_LARGE, "%lld partial rows, %lld work items", (long long)p.n_parts,
                 (long long)p.blocks());
   return MX_OK;
@@ -1834,16 +1832,10 @@ void pack_meta_span(const SpanPlan& p, const LayoutSpan& L, char* h) {
   auto put = [&](size_t at, const auto& v) {
     if (!v.empty()) memcpy(h + at, v.data(), v.size() * sizeof(v[0]));
   };
-  put(L.rows, p.rows);
   put(L.items, p.items);
-  int32_t* pages = (int32_t*)(h + L.pages);
-  for (const SpanPlan::Table& t : p.tables) {
-    memcpy(pages, t.pages, (size_t)t.n * sizeof(int32_t));
-    pages += t.n;
-  }
+  put(L.pages, p.pages);
   put(L.tokens, p.tokens);
   put(L.merge_tokens, p.merge_tokens);
-  put(L.merges, p.merges);
   put(L.sources, p.sources);
 }
 
@@ -1879,12 +1871,10 @@ mx_status span_attn(const char* tag, const SpanPlan& p, const mx_attn_shape* s, 
   // it from host memory, so only where there are few)
   const bool small = L.meta_end <= sizeof(InlineMeta) && p.blocks() <= plan::kSlots;
   void* meta = small ? nullptr : ws;  // what the pointers into the metadata count from
-  a.rows = at<SpanRows>(meta, L.rows);
   a.items = at<SpanItem>(meta, L.items);
   a.a.pages = at<int32_t>(meta, L.pages);
   a.tokens = at<int32_t>(meta, L.tokens);
   a.merge_tokens = at<SpanToken>(meta, L.merge_tokens);
-  a.merges = at<SpanMerge>(meta, L.merges);
   a.sources = at<SpanSource>(meta, L.sources);
   alignas(16) InlineMeta inlined;
   if (small) {

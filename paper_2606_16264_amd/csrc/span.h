@@ -33,24 +33,13 @@ struct SpanRows {
   int32_t part;        // -1: the rows go to the output
 };
 
-// A work item, of each KV head a workgroup: `n_rows` rows from row0 on, the first of which
-// belongs to token tok0 of the record.
-//   kind 0 (stream): up to kSpanStreamRows rows of one position
-//   kind 1 (tile):   up to kSpanTileRows rows
-struct SpanItem {
-  int32_t rows;
-  int32_t row0, tok0;
-  uint16_t split;
-  uint8_t kind, n_rows;
-};
-
-// The pages of an item: page0 .. page1 - 1, counted without the `skip` entries of the table
-// from sink_pages on that none of the item's rows sees.
+// The pages of some rows: page0 .. page1 - 1, counted without the `skip` entries of the table
+// from sink_pages on that none of the rows sees.
 struct SpanPages {
   int32_t skip, page0, page1;
 };
 // All that tokens tok0 .. tok1 of a record see.
-MX_SPAN_FN SpanPages span_seen(const SpanRows& r, int tok0, int tok1, int window) {
+inline SpanPages span_seen(const SpanRows& r, int tok0, int tok1, int window) {
   if (r.list) return SpanPages{0, 0, r.entries};
   const int pos0 = r.pos + tok0, pos1 = r.pos + tok1;
   const int low = pos0 < window ? 0 : (pos0 - window + 1) >> 4;  // the first page of the window
@@ -61,7 +50,7 @@ MX_SPAN_FN SpanPages span_seen(const SpanRows& r, int tok0, int tok1, int window
 }
 // Split `split` of `n_split`, in whole chunks of two pages.  (Empty where there are fewer
 // chunks than splits: the rows' partials are zeros.)
-MX_SPAN_FN SpanPages span_split(SpanPages s, int split, int n_split) {
+inline SpanPages span_split(SpanPages s, int split, int n_split) {
   if (n_split == 1) return s;
   const int chunks = (s.page1 + 1) >> 1;
   const int per = chunks / n_split, more = chunks - per * n_split;  // the first `more` take one more
@@ -69,6 +58,24 @@ MX_SPAN_FN SpanPages span_split(SpanPages s, int split, int n_split) {
   const int end = 2 * (first + per + (split < more ? 1 : 0));
   return SpanPages{s.skip, 2 * first, end < s.page1 ? end : s.page1};
 }
+
+// A work item, of each KV head a workgroup: `n_rows` rows of a record, over some of its pages.
+//   kind 0 (stream): up to kSpanStreamRows rows of one position
+//   kind 1 (tile):   up to kSpanTileRows rows
+// All that a workgroup has to know before its first loads stands here: each record read on the
+// way to them costs it most of a microsecond.
+struct SpanItem {
+  int32_t tok;          // batch row, or place in the list, of the first row's token
+  int32_t rest;         // the first row's place among the group rows of its token
+  int32_t pos;          // position of that token; list: of every token
+  int32_t list;
+  int32_t pages, sink_pages;
+  int32_t skip_table, skip_real;  // entries and pages left out from sink_pages on
+  int32_t page0, page1;           // counted without them
+  int32_t part, kvh_stride;       // partial of the first row of KV head 0 (-1: output), of the next head
+  int32_t kind, n_rows;
+  int32_t pad[2];
+};
 
 // The item and KV head of a workgroup.  The heads go by groups of `heads`, of each group all
 // items, each item's heads one after the other.  Workgroup b runs on die b % 8, each die with
@@ -84,15 +91,14 @@ MX_SPAN_FN SpanBlock span_block(int b, int n_items, int nkv, int heads) {
   return SpanBlock{at / here, heads * group + at % here};
 }
 
-// A request whose tokens have partials: in the records of sources src .. src + n_src - 1.
+// Partials of a request's tokens: split s of KV head g, row i of its token t's group at
+// base + g * kvh_stride + s * split_stride + t * group + i.
 struct SpanSource {
-  int32_t rows, tok;  // the record, the request's first token in it
+  int32_t base, kvh_stride, split_stride, n_split;
 };
-struct SpanMerge {
-  int32_t tok, src, n_src;
-};
-struct SpanToken {  // a token to be merged
-  int32_t tok, merge;
+// A token to be merged: its batch row, the sources of its request, its place there.
+struct SpanToken {
+  int32_t tok, src, n_src, at;
 };
 
 }  // namespace mx

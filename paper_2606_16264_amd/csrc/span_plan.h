@@ -37,27 +37,21 @@ struct SpanPlan {
   int group = 1, nkv = 1;
   int64_t page_bytes = 0;  // keys and values of one head
   int window = INT32_MAX, sinks = 0;
-  struct Table {  // entries of a request's page table
-    const int32_t* pages;
-    int n;
-  };
   std::vector<SpanRows> rows;
-  std::vector<Table> tables;  // whose entries follow each other in the flat page array
+  std::vector<int32_t> pages;  // the records' page tables
   std::vector<int32_t> tokens;
   std::vector<SpanItem> items;
   std::vector<SpanSource> sources;
-  std::vector<SpanMerge> merges;
   std::vector<SpanToken> merge_tokens;
-  int64_t n_pages = 0, n_parts = 0;
+  int64_t n_parts = 0;
   int most_parts = 0;  // partials of a row
   bool has_tiles = false;
   int heads = 1;  // of a group of span_block
 
   int64_t blocks() const { return (int64_t)items.size() * nkv; }
-  int add_table(const int32_t* pages, int n) {
-    const int at = (int)n_pages;
-    tables.push_back(Table{pages, n});
-    n_pages += n;
+  int add_table(const int32_t* ids, int n) {
+    const int at = (int)pages.size();
+    pages.insert(pages.end(), ids, ids + n);
     return at;
   }
 };
@@ -164,10 +158,25 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
     // (tiles that take the same keys follow each other)
     for (int s = 0; s < n_split; s++)
       for (int row = 0; row < r.n_rows; row += step) {
-        const int n = std::min(step, r.n_rows - row);
-        const int cost = std::max(1, seen(r, row, n) / n_split);
-        list[tile].push_back(Cost{SpanItem{(int32_t)i, row, row / p.group, (uint16_t)s, (uint8_t)tile, (uint8_t)n},
-                                  cost});
+        const int n = std::min(step, r.n_rows - row), tok0 = row / p.group;
+        const SpanPages all = span_seen(r, tok0, (row + n - 1) / p.group, p.window);
+        const SpanPages pg = span_split(all, s, n_split);
+        SpanItem it = {};
+        it.tok = r.tok + tok0;
+        it.rest = row - tok0 * p.group;
+        it.list = r.list;
+        it.pos = r.list ? r.pos : r.pos + tok0;
+        it.pages = r.pages;
+        it.sink_pages = r.sink_pages;
+        it.skip_table = pg.skip;
+        it.skip_real = pg.skip + r.skip;
+        it.page0 = pg.page0;
+        it.page1 = pg.page1;
+        it.part = r.part < 0 ? -1 : r.part + s * r.n_rows + row;
+        it.kvh_stride = n_split * r.n_rows;
+        it.kind = tile;
+        it.n_rows = n;
+        list[tile].push_back(Cost{it, std::max(1, all.page1 / n_split)});
       }
   }
   p.has_tiles = !list[1].empty();
@@ -176,25 +185,26 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
   order_items(list[1], list[0], p.nkv, p.items);
 }
 
-// The merges of the requests' tokens.
+// The merges of the requests' tokens: of each request the records that its tokens are rows of,
+// and its first token there.
 struct RequestSources {
   int tok, n_new;
-  std::vector<SpanSource> from;
+  std::vector<std::pair<int, int>> from;
 };
 inline void plan_merges(SpanPlan& p, const std::vector<RequestSources>& reqs) {
   for (const RequestSources& q : reqs) {
+    const int src = (int)p.sources.size();
     int n = 0;
-    SpanMerge m{q.tok, (int)p.sources.size(), 0};
-    for (const SpanSource& s : q.from) {
-      if (p.rows[s.rows].part < 0) continue;  // the rows went to the output
-      n += p.rows[s.rows].n_split;
-      p.sources.push_back(s);
-      m.n_src++;
+    for (const auto& f : q.from) {
+      const SpanRows& r = p.rows[f.first];
+      if (r.part < 0) continue;  // the rows went to the output
+      n += r.n_split;
+      p.sources.push_back(SpanSource{r.part + f.second * p.group, r.n_split * r.n_rows, r.n_rows, r.n_split});
     }
-    if (m.n_src == 0) continue;
+    const int n_src = (int)p.sources.size() - src;
+    if (n_src == 0) continue;
     p.most_parts = std::max(p.most_parts, n);
-    for (int i = 0; i < q.n_new; i++) p.merge_tokens.push_back(SpanToken{q.tok + i, (int)p.merges.size()});
-    p.merges.push_back(m);
+    for (int i = 0; i < q.n_new; i++) p.merge_tokens.push_back(SpanToken{q.tok + i, src, n_src, i});
   }
 }
 
@@ -276,7 +286,7 @@ inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
     int at = 0;
     for (int r = run.first_req; r < end; r++) {
       if (whole[r]) continue;
-      reqs[r].from.push_back(SpanSource{rec, at});
+      reqs[r].from.push_back({rec, at});
       for (int t = 0; t < b->reqs[r].n_new; t++) p.tokens.push_back(reqs[r].tok + t);
       at += b->reqs[r].n_new;
       own[r] = start[r];
@@ -288,7 +298,7 @@ inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
   for (int r = 0; r < R; r++) {
     const mx_request& q = b->reqs[r];
     const int end = (q.ctx_len + q.n_new - 1) / 16 + 1;
-    reqs[r].from.push_back(SpanSource{(int)p.rows.size(), 0});
+    reqs[r].from.push_back({(int)p.rows.size(), 0});
     const int pages = p.add_table(q.pages + own[r], end - own[r]);
     p.rows.push_back(SpanRows{reqs[r].tok, q.n_new * p.group, q.ctx_len, 0, pages, end - own[r], 0, own[r], 1, -1});
     parts.push_back(plan::Part{q.n_new == 1, own[r] > 0});

@@ -35,9 +35,7 @@ struct Got {
 
 static void walk(const Case& c, const SpanPlan& p) {
   const int group = c.nq / c.nkv;
-  std::vector<int> flat;
-  for (const auto& t : p.tables) flat.insert(flat.end(), t.pages, t.pages + t.n);
-  CHECK((int64_t)flat.size() == p.n_pages, "pages %zu", flat.size());
+  const std::vector<int>& flat = p.pages;
   std::vector<int> tok_req, tok_pos;
   for (size_t r = 0; r < c.reqs.size(); r++)
     for (int i = 0; i < c.reqs[r].n_new; i++) {
@@ -53,30 +51,25 @@ static void walk(const Case& c, const SpanPlan& p) {
     const SpanBlock at_b = span_block(b, (int)p.items.size(), p.nkv, p.heads);
     CHECK(at_b.item >= 0 && at_b.item < (int)p.items.size() && at_b.kvh >= 0 && at_b.kvh < p.nkv, "block %d", b);
     const SpanItem& it = p.items[at_b.item];
-    CHECK(it.rows >= 0 && it.rows < (int)p.rows.size(), "rows");
-    const SpanRows& rw = p.rows[it.rows];
-    CHECK(it.n_rows >= 1 && it.row0 + it.n_rows <= rw.n_rows, "rows of an item");
+    CHECK(it.n_rows >= 1 && it.rest >= 0 && it.rest < group, "rows of an item");
     CHECK(it.n_rows <= (it.kind ? kSpanTileRows : kSpanStreamRows), "rows of an item");
-    CHECK(it.tok0 == it.row0 / group, "tok0");
-    CHECK(it.split < rw.n_split && (rw.n_split == 1 || rw.part >= 0), "split");
-    const SpanPages pg = span_split(span_seen(rw, it.tok0, (it.row0 + it.n_rows - 1) / group, p.window), it.split, rw.n_split);
-    CHECK(pg.page0 % 2 == 0 && pg.page0 >= 0, "page0 %d", pg.page0);
-    if (pg.page0 >= pg.page1) CHECK(rw.part >= 0, "an empty item without partials");
-    if (it.kind == 0 && !rw.list) CHECK(rw.n_rows == group, "a stream's rows are of one position");
+    CHECK(it.page0 % 2 == 0 && it.page0 >= 0, "page0 %d", it.page0);
+    if (it.page0 >= it.page1) CHECK(it.part >= 0, "an empty item without partials");
+    if (it.kind == 0 && !it.list) CHECK(it.rest + it.n_rows <= group, "a stream's rows are of one position");
     std::vector<std::pair<int, int>> keys;
-    for (int v = pg.page0; v < pg.page1; v++) {
-      const int t = v < rw.sink_pages ? v : v + pg.skip;
-      const int real = v < rw.sink_pages ? v : v + pg.skip + rw.skip;
-      CHECK(t < rw.entries && rw.pages + t >= 0 && rw.pages + t < (int)flat.size(), "table entry");
-      keys.push_back({flat[rw.pages + t], rw.list ? -1 : 16 * real});
+    for (int v = it.page0; v < it.page1; v++) {
+      const int t = v < it.sink_pages ? v : v + it.skip_table;
+      const int real = v < it.sink_pages ? v : v + it.skip_real;
+      CHECK(it.pages + t >= 0 && it.pages + t < (int)flat.size(), "table entry");
+      keys.push_back({flat[it.pages + t], it.list ? -1 : 16 * real});
     }
     for (int i = 0; i < it.n_rows; i++) {
-      const int row = it.row0 + i, tk = row / group, h = at_b.kvh * group + row % group;
-      const int tok = rw.list ? p.tokens.at(rw.tok + tk) : rw.tok + tk;
+      const int tk = (it.rest + i) / group, h = at_b.kvh * group + (it.rest + i) % group;
+      const int tok = it.list ? p.tokens.at(it.tok + tk) : it.tok + tk;
       CHECK(tok >= 0 && tok < T, "token %d", tok);
-      CHECK(rw.list || rw.pos + tk == tok_pos[tok], "position");
-      if (rw.part >= 0) {
-        const int at = rw.part + (at_b.kvh * rw.n_split + it.split) * rw.n_rows + row;
+      CHECK(it.list || it.pos + tk == tok_pos[tok], "position");
+      if (it.part >= 0) {
+        const int at = it.part + at_b.kvh * it.kvh_stride + i;
         CHECK(at < p.n_parts, "partial %d of %lld", at, (long long)p.n_parts);
         CHECK(!written[at], "partial %d twice", at);
         written[at] = 1;
@@ -89,15 +82,13 @@ static void walk(const Case& c, const SpanPlan& p) {
   }
   std::set<int> used;
   for (const SpanToken& tk : p.merge_tokens) {
-    const SpanMerge& m = p.merges.at(tk.merge);
     int n = 0;
     for (int h = 0; h < c.nq; h++) {
       const int g = h / group;
-      for (int s = 0; s < m.n_src; s++) {
-        const SpanSource& src = p.sources.at(m.src + s);
-        const SpanRows& rw = p.rows.at(src.rows);
-        for (int k = 0; k < rw.n_split; k++) {
-          const int at = rw.part + (g * rw.n_split + k) * rw.n_rows + (src.tok + tk.tok - m.tok) * group + h - g * group;
+      for (int s = 0; s < tk.n_src; s++) {
+        const SpanSource& src = p.sources.at(tk.src + s);
+        for (int k = 0; k < src.n_split; k++) {
+          const int at = src.base + g * src.kvh_stride + k * src.split_stride + tk.at * group + h - g * group;
           CHECK(at >= 0 && at < p.n_parts && written[at], "merge reads partial %d", at);
           CHECK(part_row[at] == std::make_pair(tk.tok, h), "partial %d is another row's", at);
           CHECK(used.insert(at).second, "partial %d read twice", at);
