@@ -152,6 +152,12 @@ def _load() -> ctypes.CDLL:
 
 _lib = _load()
 
+import torch  # noqa: E402  (loaded already, before the library)
+
+# what the calls on tensors ask of torch every time
+_BF16 = (torch.bfloat16, torch.uint16)  # uint16: the bits of bf16
+_current_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+
 
 def lib() -> ctypes.CDLL:
     return _lib
@@ -325,26 +331,29 @@ def _size(n: int) -> int:
 def _check_attn(batch: Batch, shape: AttnShape, q, k_pool, v_pool, out, ws) -> int:
     """The tensors of an attention call over the bf16 cache: bf16 (or its bits), contiguous, large
     enough, on one GPU that is the current one; its index."""
-    import torch
     device = q.get_device()
-    if device < 0:
-        raise ValueError("q is not on a GPU")
-    if device != torch.cuda.current_device():
-        raise ValueError(f"q is on device {device}, not the current one")
-    bf16 = (torch.bfloat16, torch.uint16)
-    rows = batch.T * shape.n_q_heads * shape.head_dim
-    pool = shape.pool_pages * shape.n_kv_heads * shape.head_dim * shape.page_size
-    _check_tensor_on(device, "q", q, rows, bf16)
-    _check_tensor_on(device, "k_pool", k_pool, pool, bf16)
-    _check_tensor_on(device, "v_pool", v_pool, pool, bf16)
-    _check_tensor_on(device, "out", out, rows, bf16)
-    _check_tensor_on(device, "ws", ws, 0)
+    heads, d = shape.n_q_heads, shape.head_dim
+    rows, pool = batch.T * heads * d, shape.pool_pages * shape.n_kv_heads * d * shape.page_size
+    # (all at once first, with few look-ups: most of a small call's time in here)
+    if (device < 0 or device != _current_device()
+            or not (q.is_contiguous() and k_pool.is_contiguous() and v_pool.is_contiguous()
+                    and out.is_contiguous() and ws.is_contiguous())
+            or not (k_pool.get_device() == v_pool.get_device() == out.get_device() == ws.get_device() == device)
+            or not (q.dtype in _BF16 and k_pool.dtype in _BF16 and v_pool.dtype in _BF16 and out.dtype in _BF16)
+            or q.numel() < rows or out.numel() < rows or k_pool.numel() < pool or v_pool.numel() < pool
+            or ws.element_size() != 1):
+        if device < 0:
+            raise ValueError("q is not on a GPU")
+        if device != _current_device():
+            raise ValueError(f"q is on device {device}, not the current one")
+        for name, t, n in (("q", q, rows), ("k_pool", k_pool, pool), ("v_pool", v_pool, pool), ("out", out, rows)):
+            _check_tensor_on(device, name, t, n, _BF16)
+        _check_tensor_on(device, "ws", ws, 0)
     return device
 
 
 def _stream_of(device: int, stream) -> Optional[int]:
-    import torch
-    return _stream(stream) if stream is not None else torch._C._cuda_getCurrentRawStream(device)
+    return _stream(stream) if stream is not None else _raw_stream(device)
 
 
 def _stream(stream) -> Optional[int]:

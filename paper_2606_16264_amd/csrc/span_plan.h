@@ -30,7 +30,7 @@ inline SeenPages seen_pages(int ctx, int n, int window, int sinks) {
 
 // Joining the parts of a row costs a launch, partials written and read: runs are left to
 // their requests where less than this would be read once instead of several times.
-constexpr int64_t kMinSharedBytes = 24 << 20;
+constexpr int64_t kMinSharedBytes = 64 << 20;
 
 struct SpanPlan {
   int64_t min_shared_bytes = kMinSharedBytes;
@@ -59,10 +59,10 @@ struct SpanPlan {
 namespace plan {
 
 constexpr int64_t kSlots = 512;      // workgroups that the chip holds at once
-constexpr int64_t kTileSlots = 256;  // tiles are split to about as many
 constexpr int kMinSplitPages = 16;   // of a stream
-constexpr int kWholePages = 64;      // streams and tiles of up to that many are not split
-constexpr int kMinTilePages = 32;
+constexpr int kWholePages = 64;      // streams of up to that many are not split
+constexpr int kWholeTilePages = 48;  // tiles of up to that many are not split
+constexpr int kMinTilePages = 16;
 constexpr int kExtraTiles = 1024;    // items that splitting tiles adds to a call, at most
 constexpr int kMostSplits = 4096;
 
@@ -130,7 +130,11 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
   const int64_t share = pages[0] * p.nkv / kSlots;  // of a workgroup that the chip holds at once
   const bool whole = longest <= std::max<int64_t>(kWholePages, share + share / 4);
   const int stream_split = whole ? longest : even(std::max<int64_t>(kMinSplitPages, share / 2));
-  const int tile_split = even(std::max<int64_t>(kMinTilePages, (pages[1] * p.nkv + kTileSlots - 1) / kTileSlots));
+  // Tiles are split to as many as the chip holds at once, or one for each CU beside streams
+  // that take a good part of it.
+  const bool mixed = pages[0] * kStreamPage > pages[1] / 4;
+  const int64_t slots = mixed ? kSlots / 2 : kSlots;
+  const int tile_split = even(std::max<int64_t>(mixed ? 2 * kMinTilePages : kMinTilePages, (pages[1] * p.nkv + slots - 1) / slots));
   std::vector<Cost> list[2];
   int64_t extra = kExtraTiles;
   for (size_t i = 0; i < parts.size(); i++) {
@@ -142,7 +146,7 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
       most = std::max(most, seen(r, row, std::min(step, r.n_rows - row)));
     if (!tile) {
       n_split = std::max(1, (most + stream_split / 2) / std::max(1, stream_split));
-    } else if (most > kWholePages || parts[i].partial) {
+    } else if (most > kWholeTilePages || parts[i].partial) {
       n_split = std::max(1, most / tile_split);
       const int64_t tiles = (int64_t)((r.n_rows + step - 1) / step) * p.nkv;
       n_split = (int)std::min<int64_t>(n_split, 1 + extra / tiles);
@@ -237,7 +241,7 @@ inline void plan_window(const mx_batch* b, const mx_attn_shape* s, int window, i
 
 // A prompt whose rows fill tiles by themselves takes its shared keys with its own: the rows
 // that would be saved, times the keys, against partials for all of its rows.
-constexpr int64_t kWholePromptKeys = 1024;
+constexpr int64_t kWholePromptKeys = 2048;
 
 inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
                         const mx_shared_run* runs, SpanPlan& p) {

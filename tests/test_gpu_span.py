@@ -237,7 +237,7 @@ def shared_case(nq, nkv, d, reqs, runs, seed):
 
 
 D, P = 1, 0
-# (runs are taken apart from their requests where that saves 24 MB of reads: `more` decodes
+# (runs are taken apart from their requests where that saves 64 MB of reads: `more` decodes
 # of a run of their own, of as many pages as that takes, go with the requests that follow)
 SHARED = [
     ([(D, 1, 0), (D, 1, 0)], [(0, 2, 1)]),
@@ -261,7 +261,7 @@ SHARED = [
 def test_shared(nq, nkv, d, case, more):
     reqs, runs = SHARED[case]
     if more:
-        pages = -(-(24 << 20) // ((more - 1) * 64 * d * nkv))
+        pages = -(-(64 << 20) // ((more - 1) * 64 * d * nkv))
         runs = runs + [(len(reqs), more, pages)]
         reqs = reqs + [(D, 1, i) for i in range(more)]
     pools, reqs, q = shared_case(nq, nkv, d, reqs, runs, 17 * case + nq)
@@ -289,7 +289,7 @@ def test_shared_not_finite(bad):
     """A value that is no number in a run reaches all of the run's rows; in a chunk's own
     tokens those behind it."""
     reqs, runs = [(D, 1, 20), (P, 30, 0), (D, 1, 4), (D, 1, 9)], [(0, 3, 12), (1, 2, 4)]
-    runs, reqs = runs + [(4, 24, 70)], reqs + [(D, 1, i) for i in range(24)]  # (enough to be taken apart)
+    runs, reqs = runs + [(4, 24, 180)], reqs + [(D, 1, i) for i in range(24)]  # (enough to be taken apart)
     pools, reqs, q = shared_case(8, 2, 128, reqs, runs, 31)
     hk = pools.hv.clone()
     # of request 1: position 100 of the first run (rows of 0, 1, 2), 200 of the second (1, 2)
@@ -322,7 +322,7 @@ def test_rows_behind_stay_and_output_in_place():
     run_window(pools, 8, reqs, buf, 64, 2, out=buf)
     check(buf[:len(q)], out, mag)
     assert (buf[len(q):] == 3).all()
-    reqs, runs = [(D, 1, 20), (P, 30, 0), (P, 400, 7)] + [(D, 1, 3)] * 40, [(0, 43, 80)]
+    reqs, runs = [(D, 1, 20), (P, 30, 0), (P, 400, 7)] + [(D, 1, 3)] * 40, [(0, 43, 200)]
     pools, reqs, q = shared_case(8, 2, 64, reqs, runs, 43)
     out, mag = reference(pools, 8, reqs, q)
     buf = torch.full((len(q) + 5, 8, 64), 3.0, dtype=torch.bfloat16, device="cuda")
@@ -457,8 +457,8 @@ def test_streams_and_threads():
     for i in range(2):
         reqs = [(1, 1, 300 + 100 * i), (0, 60, 40), (1, 1, 1500)]
         pools, reqs, q = window_case(8, 2, 64, reqs, 81 + i, 100, 4)
-        sh, sreqs, sq = shared_case(8, 2, 64, [(D, 1, 9 * k) for k in range(33)], [(0, 33, 100 + i)], 91 + i)
-        cases.append((pools, reqs, q.cuda(), reference(pools, 8, reqs, q, 100, 4), sh, sreqs, [(0, 33, 100 + i)],
+        sh, sreqs, sq = shared_case(8, 2, 64, [(D, 1, 9 * k) for k in range(33)], [(0, 33, 260 + i)], 91 + i)
+        cases.append((pools, reqs, q.cuda(), reference(pools, 8, reqs, q, 100, 4), sh, sreqs, [(0, 33, 260 + i)],
                       sq.cuda(), reference(sh, 8, sreqs, sq)))
     torch.cuda.synchronize()
     errors = []
