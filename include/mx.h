@@ -448,10 +448,11 @@ mx_status mx_debug_gather(const mx_batch* batch, const mx_attn_shape* shape, int
 
 /* Launch timing, for profiling.  When enabled, every kernel launch of
  * mx_layer_step and mx_paged_attn (and those of mx_paged_attn_f8 together, of
- * mx_kv_evict_f8 together) is bracketed by two hipEvents recorded on the
+ * mx_kv_evict_f8, mx_paged_attn_window and mx_paged_attn_shared likewise) is bracketed by two hipEvents recorded on the
  * caller's stream (the launch's own stream), tagged with the step it performs
  * ("token_map+rmsnorm_1", "gemm_qkv", "paged_attn", "gemm_o", "rmsnorm_2",
- * "gemm_gate_up", "gemm_down", "paged_attn_f8", "kv_evict_f8"; a tag covers a split-K GEMM's reduce, the
+ * "gemm_gate_up", "gemm_down", "paged_attn_f8", "kv_evict_f8", "paged_attn_window",
+ * "paged_attn_shared"; a tag covers a split-K GEMM's reduce, the
  * launches of a GEMM whose rows run as two parts, and the attention's split
  * merge, except that when rows of the output projection are split over K their
  * reduce runs fused with the second RMSNorm, timed as "o_reduce+rmsnorm_2"

@@ -1308,6 +1308,14 @@ mx_status check_rows(const mx_batch* b, const mx_attn_shape* s) {
   return MX_OK;
 }
 
+// The rows of a run's requests likewise, all together.
+mx_status check_all_rows(const mx_batch* b, const mx_attn_shape* s, int64_t T) {
+  const mx_status st = check_rows(b, s);
+  if (st == MX_OK && T * (s->n_q_heads / s->n_kv_heads) > INT32_MAX - 4096)
+    return fail(MX_ERR_TOO_LARGE, "%lld new tokens", (long long)T);
+  return st;
+}
+
 // These calls read host staging buffers that later calls write again, so a captured
 // one would read whatever lies there at its replay.
 mx_status check_not_capturing(hipStream_t stream) {
@@ -1951,7 +1959,8 @@ MX_EXPORT size_t mx_workspace_bytes_shared_for(const mx_batch* batch, const mx_a
                                                int32_t num_runs, const mx_shared_run* runs) {
   g_err.clear();
   return no_throw((size_t)0, [&]() -> size_t {
-    if (validate_batch(batch, shape, nullptr) != MX_OK || check_rows(batch, shape) != MX_OK ||
+    int64_t T;
+    if (validate_batch(batch, shape, &T) != MX_OK || check_all_rows(batch, shape, T) != MX_OK ||
         validate_runs(batch, num_runs, runs) != MX_OK)
       return 0;
     SpanPlan p;
@@ -1979,7 +1988,7 @@ MX_EXPORT mx_status mx_paged_attn_shared(const mx_batch* batch, const mx_attn_sh
     if ((st = validate_runs(batch, num_runs, runs)) != MX_OK) return st;
     if (T == 0) return MX_OK;
     if ((st = check_span_tensors(shape, T, q, k_pool, v_pool, out, ws)) != MX_OK) return st;
-    if ((st = check_rows(batch, shape)) != MX_OK) return st;
+    if ((st = check_all_rows(batch, shape, T)) != MX_OK) return st;
     SpanPlan p;
     plan_shared(batch, shape, num_runs, runs, p);
     return span_attn("paged_attn_shared", p, shape, q, k_pool, v_pool, out, ws, ws_bytes, stream);

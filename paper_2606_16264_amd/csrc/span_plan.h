@@ -43,7 +43,7 @@ struct SpanPlan {
   std::vector<SpanItem> items;
   std::vector<SpanSource> sources;
   std::vector<SpanToken> merge_tokens;
-  int64_t n_parts = 0;
+  int64_t n_parts = 0;  // (numbered in 32 bits: the caller refuses a plan with more)
   int most_parts = 0;  // partials of a row
   bool has_tiles = false;
   int heads = 1;  // of a group of span_block
@@ -176,8 +176,8 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
         it.skip_real = pg.skip + r.skip;
         it.page0 = pg.page0;
         it.page1 = pg.page1;
-        it.part = r.part < 0 ? -1 : r.part + s * r.n_rows + row;
-        it.kvh_stride = n_split * r.n_rows;
+        it.part = r.part < 0 ? -1 : (int32_t)(r.part + (int64_t)s * r.n_rows + row);
+        it.kvh_stride = (int32_t)((int64_t)n_split * r.n_rows);
         it.kind = tile;
         it.n_rows = n;
         list[tile].push_back(Cost{it, std::max(1, all.page1 / n_split)});
@@ -203,7 +203,8 @@ inline void plan_merges(SpanPlan& p, const std::vector<RequestSources>& reqs) {
       const SpanRows& r = p.rows[f.first];
       if (r.part < 0) continue;  // the rows went to the output
       n += r.n_split;
-      p.sources.push_back(SpanSource{r.part + f.second * p.group, r.n_split * r.n_rows, r.n_rows, r.n_split});
+      p.sources.push_back(SpanSource{(int32_t)(r.part + (int64_t)f.second * p.group),
+                                     (int32_t)((int64_t)r.n_split * r.n_rows), r.n_rows, r.n_split});
     }
     const int n_src = (int)p.sources.size() - src;
     if (n_src == 0) continue;

@@ -481,3 +481,66 @@ def test_streams_and_threads():
     [t.start() for t in threads]
     [t.join() for t in threads]
     assert not errors, errors
+
+
+def test_captured_streams_are_refused():
+    reqs = [(1, 1, 300), (0, 40, 20)]
+    pools, reqs, q = window_case(8, 2, 64, reqs, 95, 64, 2)
+    q = q.cuda()
+    want, ws = run_window(pools, 8, reqs, q, 64, 2)
+    b, s, out = batch_of([r[:3] + ([max(p, 0) for p in r[3]],) for r in reqs]), pools.shape(8), torch.zeros_like(want)
+    big = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    y = torch.zeros(4, device="cuda")
+    torch.cuda.synchronize()
+    graph, seen = torch.cuda.CUDAGraph(), []
+    with torch.cuda.graph(graph):
+        for call in (lambda: mx.mx_paged_attn_window(b, s, 64, 2, q, pools.k, pools.v, out, big),
+                     lambda: mx.mx_paged_attn_shared(b, s, mx.SharedRuns([]), q, pools.k, pools.v, out, big)):
+            try:
+                call()
+            except mx.MxError as x:
+                seen.append(x.status)
+        y += 1
+    assert seen == [mx.MX_ERR_UNSUPPORTED] * 2
+    graph.replay()
+    torch.cuda.synchronize()
+    assert y.tolist() == [1.0] * 4 and not out.any()
+    assert torch.equal(run_window(pools, 8, reqs, q, 64, 2)[0], want)
+
+
+def test_calls_in_a_row_on_one_workspace():
+    """Calls of different batches on one stream and workspace, without a wait between them: small
+    ones, whose metadata goes with the launch, and large ones, whose metadata is uploaded."""
+    cases = []
+    for i in range(6):
+        n = [3, 40, 1, 90, 5, 60][i]
+        reqs = [(1, 1, 17 * k + 200) for k in range(n)] + [(0, 20 * i + 1, 5 * i)]
+        pools, reqs, q = window_case(8, 2, 64, reqs, 200 + i, 50 + 30 * i, i)
+        cases.append((pools, reqs, q.cuda(), 50 + 30 * i, i, reference(pools, 8, reqs, q, 50 + 30 * i, i)))
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    got = []
+    for _ in range(5):
+        for pools, reqs, q, w, sinks, _ in cases:
+            out = torch.empty_like(q)
+            mx.mx_paged_attn_window(batch_of(reqs), pools.shape(8), w, sinks, q, pools.k, pools.v, out, ws)
+            got.append(out)
+    for i, out in enumerate(got):
+        check(out, *cases[i % 6][5], f"call {i}")
+
+
+def test_binding_refuses_other_tensors():
+    """Strided, of another type, too small, or not on the GPU: refused before anything runs."""
+    reqs = [(1, 1, 90)]
+    pools, reqs, q = window_case(4, 2, 64, reqs, 97, 64, 2)
+    b, s, q = batch_of(reqs), pools.shape(4), q.cuda()
+    out, ws = torch.zeros_like(q), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    good = dict(q=q, k_pool=pools.k, v_pool=pools.v, out=out, ws=ws)
+    for name, t in (("q", q.float()), ("q", q.cpu()), ("q", q.transpose(1, 2)), ("out", out.half()),
+                    ("out", out[:, :3].contiguous()), ("k_pool", pools.k[1:]), ("v_pool", pools.v.transpose(2, 3)),
+                    ("v_pool", pools.v.cpu()), ("ws", ws.view(torch.float32)), ("ws", ws.cpu())):
+        for call in (lambda a: mx.mx_paged_attn_window(b, s, 64, 2, **a),
+                     lambda a: mx.mx_paged_attn_shared(b, s, mx.SharedRuns([]), **a)):
+            with pytest.raises(ValueError, match=f"^{name} "):
+                call(dict(good, **{name: t}))
+    torch.cuda.synchronize()
+    assert not out.any()
