@@ -1875,28 +1875,44 @@ mx_status span_attn(const char* tag, const SpanPlan& p, const mx_attn_shape* s, 
   a.n_items = (int32_t)p.items.size();
   a.heads = p.heads;
   a.group_inv = p.group > 1 ? (uint32_t)((((uint64_t)1 << 32) + p.group - 1) / p.group) : 0;
-  // a small call's metadata goes with the kernels' arguments: no upload (each workgroup reads
-  // it from host memory, so only where there are few)
-  const bool small = L.meta_end <= sizeof(InlineMeta) && p.blocks() <= plan::kSlots;
-  void* meta = small ? nullptr : ws;  // what the pointers into the metadata count from
-  a.items = at<SpanItem>(meta, L.items);
-  a.a.pages = at<int32_t>(meta, L.pages);
-  a.tokens = at<int32_t>(meta, L.tokens);
-  a.merge_tokens = at<SpanToken>(meta, L.merge_tokens);
-  a.sources = at<SpanSource>(meta, L.sources);
-  alignas(16) InlineMeta inlined;
-  if (small) {
-    pack_meta_span(p, L, inlined.b);
-  } else {
-    st = staged(
-        L.meta_end, stream, [&](char* h) { pack_meta_span(p, L, h); },
-        [&](const void* dev) { return launch_upload(dev, ws, L.meta_end, stream); });
-    if (st != MX_OK) return st;
+  // Where the metadata lies: `meta` is what the pointers into it count from.
+  auto place = [&](void* meta) {
+    a.items = at<SpanItem>(meta, L.items);
+    a.a.pages = at<int32_t>(meta, L.pages);
+    a.tokens = at<int32_t>(meta, L.tokens);
+    a.merge_tokens = at<SpanToken>(meta, L.merge_tokens);
+    a.sources = at<SpanSource>(meta, L.sources);
+  };
+  auto launch = [&](const InlineMeta* meta) {
+    return timed(tag, stream, [&] {
+      return launch_span_attn(a, meta, p.has_tiles, (int)p.merge_tokens.size(), p.most_parts,
+                              s->head_dim, stream);
+    });
+  };
+  auto pack = [&](char* h) { pack_meta_span(p, L, h); };
+  // A small call's metadata goes with the kernels' arguments (each workgroup reads it from
+  // host memory, so only where there are few).
+  if (L.meta_end <= sizeof(InlineMeta) && p.blocks() <= plan::kSlots) {
+    alignas(16) InlineMeta meta;
+    pack(meta.b);
+    place(nullptr);
+    const hipError_t e = launch(&meta);
+    return e == hipSuccess ? MX_OK : hip_fail(e, "attention launch");
   }
-  const hipError_t e = timed(tag, stream, [&] {
-    return launch_span_attn(a, small ? &inlined : nullptr, p.has_tiles, (int)p.merge_tokens.size(),
-                            p.most_parts, s->head_dim, stream);
-  });
+  // Whole streams, a page id of which is wanted every microsecond, read theirs from the staging
+  // buffer: 64 decodes through a window of 1024 take 47.7 us, 49.5 with an upload before (its
+  // 4.6 us are the link's latency).  Tiles wait longer for an id than for their keys then (a
+  // prompt's take 2% more), and so do splits, which are short.
+  if (!p.has_tiles && p.merge_tokens.empty())
+    return staged(L.meta_end, stream, pack, [&](const void* dev) {
+      place(const_cast<void*>(dev));
+      return launch(nullptr);
+    });
+  place(ws);
+  st = staged(L.meta_end, stream, pack,
+              [&](const void* dev) { return launch_upload(dev, ws, L.meta_end, stream); });
+  if (st != MX_OK) return st;
+  const hipError_t e = launch(nullptr);
   return e == hipSuccess ? MX_OK : hip_fail(e, "attention launch");
 }
 

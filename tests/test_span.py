@@ -297,7 +297,7 @@ def test_launches(fake_hip):  # noqa: F811
     got = {k: [next(n for n in names if n in x) for x in v] for k, v in r["kernels"].items()}
     assert got == {
         "window": ["small_span_kernel"], "window_mixed": ["small_span_kernel"],
-        "window_many": ["upload", "span_attn"], "window_prompt": ["upload", "span_attn"],
+        "window_many": ["span_attn"], "window_prompt": ["upload", "span_attn"],
         "window_long": ["small_span_kernel", "small_span_merge"],
         "window_late": ["small_span_kernel", "small_span_merge"],
         "shared_few": ["small_span_kernel"], "shared": ["upload", "span_attn", "span_merge"],
