@@ -36,11 +36,11 @@ struct Span {
   __device__ __forceinline__ int first_key(int v) const {  // of page v, as a position
     return 16 * (v < sink_pages ? v : v + skip_real);
   }
-  // pages v and v + 1 are in the item, and all their keys seen from pos
-  __device__ __forceinline__ bool all_seen(int v, int pos) const {
+  // pages v and v + 1 are in the item, and all their keys seen from pos0 .. pos1
+  __device__ __forceinline__ bool all_seen(int v, int pos0, int pos1) const {
     if (v + 1 >= page_end) return false;
     const int first = first_key(v), last = first_key(v + 1) + 15;
-    return last <= pos && (first > pos - window || last < sinks);
+    return last <= pos0 && (first > pos1 - window || last < sinks);
   }
   // some key of the pages may be seen from pos0 .. pos1
   __device__ __forceinline__ bool some_seen(int v, int pos0, int pos1) const {
@@ -309,13 +309,16 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
     }
     return __any(mx1 > r1.thr || mx2 > r2.thr) != 0;
   };
-  auto scores = [&](int c) -> bool {  // of a chunk on its own, masked
+  // (of the wave's rows: fewer chunks need masks than of the tile's)
+  auto whole = [&](int c) { return span.all_seen(first_page + 2 * c, wave_pos0, wave_pos1); };
+  auto scores = [&](int c) -> bool {  // of a chunk on its own
     read_keys(std::integral_constant<int, -1>{}, c);
     lgkm_wait<0>();
     pin(k0);
     pin(k1);
     const f32x4 s1[2] = {score_block<HD>(k0, qf), score_block<HD>(k1, qf)};
     const f32x4 s2[2] = {score_block<HD>(k0, qf2), score_block<HD>(k1, qf2)};
+    if (whole(c)) return take(std::integral_constant<bool, false>{}, s1, s2, c);
     return take(std::integral_constant<bool, true>{}, s1, s2, c);
   };
   const uint32_t no_mask[4] = {};
@@ -335,8 +338,10 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
     pin(v0);
     pin(v1);
     bool some = false;
+    if (!whole(c)) {
 #pragma unroll
-    for (int e = 0; e < ND; e++) some |= some_not_finite(v0[e]) || some_not_finite(v1[e]);
+      for (int e = 0; e < ND; e++) some |= some_not_finite(v0[e]) || some_not_finite(v1[e]);
+    }
     if (__any(some)) {
       left_out = true;
 #pragma unroll
@@ -533,7 +538,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
     const f32x4 s[2] = {score_block<HD>(c.k[0], qf), score_block<HD>(c.k[1], qf)};
     float sv[2][4];
     float mx = take_scores(s, sv);
-    if (!span.all_seen(v, pos)) {
+    if (!span.all_seen(v, pos, pos)) {
       const unsigned seen = seen_keys(span, v, pos, g4);
       mx = mask_scores(s, sv, seen);
       uint32_t keep[4];
