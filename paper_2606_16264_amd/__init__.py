@@ -276,12 +276,20 @@ class EvictBatch:
         return self._reqs
 
 
+def _int32(*values) -> tuple:
+    """The values as they are, if 32 bits hold them (ctypes would cut them)."""
+    for v in values:
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{v} is not a 32-bit number")
+    return values
+
+
 class SharedRuns:
     """Runs of pages that requests of a batch share, in the C layout: (first request,
     requests, pages) each, outer runs first."""
 
     def __init__(self, runs: Sequence[Sequence[int]]):
-        self._runs = (_SharedRun * max(len(runs), 1))(*((int(a), int(n), int(k)) for a, n, k in runs))
+        self._runs = (_SharedRun * max(len(runs), 1))(*(_int32(int(a), int(n), int(k)) for a, n, k in runs))
         self.n = len(runs)
 
     @property
@@ -494,7 +502,7 @@ def mx_kv_evict_f8(batch: EvictBatch, shape: AttnShape, cache: CacheF8, kept, ws
 
 def mx_workspace_bytes_window_for(batch: Batch, shape: AttnShape, window: int, sinks: int = 0) -> int:
     """Workspace of mx_paged_attn_window for this batch."""
-    return _size(_lib.mx_workspace_bytes_window_for(batch.ptr, ctypes.byref(shape), window, sinks))
+    return _size(_lib.mx_workspace_bytes_window_for(batch.ptr, ctypes.byref(shape), *_int32(window, sinks)))
 
 
 def mx_workspace_bytes_window(shape: AttnShape, max_tokens: int, max_reqs: int, max_pages: int) -> int:
@@ -506,7 +514,7 @@ def mx_paged_attn_window(batch: Batch, shape: AttnShape, window: int, sinks: int
     """Attention in which a token sees the last `window` positions up to its own and the
     first `sinks`; table entries of pages that no new token sees are not looked at."""
     device = _check_attn(batch, shape, q, k_pool, v_pool, out, ws)
-    _check(_lib.mx_paged_attn_window(batch.ptr, ctypes.byref(shape), window, sinks, _ptr(q),
+    _check(_lib.mx_paged_attn_window(batch.ptr, ctypes.byref(shape), *_int32(window, sinks), _ptr(q),
                                      _ptr(k_pool), _ptr(v_pool), _ptr(out), _ptr(ws), ws.numel(),
                                      _stream_of(device, stream)))
 

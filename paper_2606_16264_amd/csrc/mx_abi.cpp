@@ -1830,7 +1830,9 @@ mx_status validate_runs(const mx_batch* b, int32_t num_runs, const mx_shared_run
 }
 
 mx_status check_span_plan(const SpanPlan& p) {
-  if (p.n_parts > INT32_MAX || p.pages.size() > (size_t)INT32_MAX || p.blocks() > INT32_MAX / 2)
+  constexpr int64_t kGrid = (1 << 24) - 1;  // workgroups of 256 threads in a launch
+  if (p.n_parts > INT32_MAX || p.pages.size() > (size_t)INT32_MAX || p.blocks() > kGrid / 2 ||
+      (int64_t)p.merge_tokens.size() > kGrid)
     return fail(MX_ERR_TOO_LARGE, "%lld partial rows, %lld work items", (long long)p.n_parts,
                 (long long)p.blocks());
   return MX_OK;

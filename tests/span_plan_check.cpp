@@ -137,8 +137,8 @@ int main(int argc, char** argv) {
     auto in = [&](int a, int b) { return a + (int)(rng() % (unsigned)(b - a + 1)); };
     auto log_in = [&](int hi) { return in(1, 1 << in(0, hi)); };
     Case c;
-    const int shapes[][2] = {{4, 4}, {8, 2}, {8, 1}, {5, 5}, {20, 1}, {36, 2}, {32, 8}, {64, 8}, {150, 1}};
-    const auto& s = shapes[in(0, 8)];
+    const int shapes[][2] = {{4, 4}, {8, 2}, {8, 1}, {5, 5}, {20, 1}, {36, 2}, {32, 8}, {64, 8}, {150, 1}, {20, 10}, {19, 19}};
+    const auto& s = shapes[in(0, 10)];
     c.nq = s[0], c.nkv = s[1];
     const bool window = seed % 2;
     const int R = in(1, window ? 6 : 10);

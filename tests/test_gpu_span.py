@@ -149,6 +149,23 @@ def test_window(nq, nkv, d, window, sinks):
     assert torch.equal(again.view(torch.uint16), got.view(torch.uint16))
 
 
+@pytest.mark.parametrize("nq,nkv,d", [(150, 1, 64), (20, 10, 128), (19, 19, 64), (33, 11, 128)])
+def test_odd_heads(nq, nkv, d):
+    """A group of more rows than a tile has; numbers of KV heads that are no multiple of eight,
+    above it: tiles alone, streams alone, both."""
+    for reqs in ([(1, 1, 100), (1, 1, 17)], [(0, 70, 30), (0, 9, 200)], [(1, 1, 333), (0, 33, 0), (0, 1, 5)]):
+        pools, full, q = window_case(nq, nkv, d, reqs, nq, 60, 7)
+        got, _ = run_window(pools, nq, full, q.cuda(), 60, 7)
+        check(got, *reference(pools, nq, full, q, 60, 7))
+        n = len(reqs)
+        pages = -(-(64 << 20) // (23 * 64 * d * nkv))
+        more = [(1, 1, i) for i in range(24)]
+        runs = [(0, n, 3), (n, 24, pages)]
+        pools, full, q = shared_case(nq, nkv, d, reqs + more, runs, nq + 1)
+        got, _ = run_shared(pools, nq, full, runs, q.cuda())
+        check(got, *reference(pools, nq, full, q))
+
+
 @pytest.mark.parametrize("kind", ["decode", "prefill"])
 @pytest.mark.parametrize("nq,nkv,d,window,sinks", [
     (8, 2, 128, 4000, 100), (32, 32, 128, 1000, 4), (4, 4, 64, 3333, 0), (16, 1, 64, 5000, 600)])

@@ -211,6 +211,16 @@ def test_workspace_bounds_cover_batches(seed):
         assert 0 < mx.mx_workspace_bytes_shared_for(b, s, runs) <= mx.mx_workspace_bytes_shared(s, T, R, pages, depth)
 
 
+def test_binding_refuses_numbers_that_32_bits_do_not_hold():
+    b, s = one(), shape()
+    for w, sinks in ((2 ** 32 + 8, 0), (8, 2 ** 32 + 1), (2 ** 31, 0), (8, -2 ** 31 - 1)):
+        with pytest.raises(ValueError):
+            mx.mx_workspace_bytes_window_for(b, s, w, sinks)
+    for run_ in ((2 ** 32, 1, 1), (0, 2 ** 32 + 1, 1), (0, 1, 2 ** 32 + 1)):
+        with pytest.raises(ValueError):
+            mx.SharedRuns([run_])
+
+
 class OnGpu:
     """Stands for a tensor on a device."""
 
