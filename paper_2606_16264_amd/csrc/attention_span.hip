@@ -49,16 +49,19 @@ struct Span {
   }
 };
 
-// Which of the lane group's eight keys of pages v0 and v0 + 1 (all of one page) the row at
-// pos sees, as bits.
-__device__ __forceinline__ unsigned seen_keys(const Span& s, int v0, int pos, int g4) {
+// Which of the lane group's eight keys of pages v0 and v0 + 1 (all of one page) are seen from
+// some position of pos0 .. pos1, as bits.
+__device__ __forceinline__ unsigned seen_keys(const Span& s, int v0, int pos0, int pos1, int g4) {
   const int v = v0 + (g4 >> 1);
   const int j0 = s.first_key(v) + 8 * (g4 & 1);
   auto below = [](int n) { return (1u << min(max(n, 0), 8)) - 1; };  // keys j0 .. j0 + n - 1
-  // (unsigned: a window of 2^31 - 1 and a position before j0 pass the 32 bits, and see nothing)
-  const int low = (int)((unsigned)pos - (unsigned)s.window + 1u - (unsigned)j0);
-  const unsigned m = below(pos - j0 + 1) & (~below(low) | below(s.sinks - j0));
+  // (the max first: a window of 2^31 - 1 and keys behind pos0 would pass the 32 bits)
+  const int hidden = max(pos0 - s.window + 1, j0) - j0;
+  const unsigned m = below(pos1 - j0 + 1) & (~below(hidden) | below(s.sinks - j0));
   return v < s.page_end ? m : 0;
+}
+__device__ __forceinline__ unsigned seen_keys(const Span& s, int v0, int pos, int g4) {
+  return seen_keys(s, v0, pos, pos, g4);
 }
 // The scores of these keys, -inf where the row does not see one (its bit as a word of its
 // own, and a select by it), and their max.
@@ -168,6 +171,17 @@ __device__ __forceinline__ RowAt row_at(const SpanParams& p, const SpanItem& it,
 // The partial of the item's first row.
 __device__ __forceinline__ int64_t part_of(const SpanItem& it, int kvh) {
   return it.part + (int64_t)kvh * it.kvh_stride;
+}
+
+// The values of pages v and v + 1 from memory, once more, as a value product takes them: put(e,
+// the lane's eight of dim row 16 e + col).
+template <int HD, typename Put>
+__device__ __forceinline__ void put_back(const SpanParams& p, const Span& span, int kvh, const int32_t* ptab,
+                                         int v, int col, int g4, Put&& put) {
+  const int64_t page = ptab[span.entry(min(v + (g4 >> 1), span.page_end - 1))];
+  const uint16_t* at = p.a.v_pool + (page * p.a.nkv + kvh) * (16 * HD) + col * 16 + 8 * (g4 & 1);
+#pragma unroll
+  for (int e = 0; e < HD / 16; e++) put(e, *reinterpret_cast<const u32x4*>(at + e * 256));
 }
 
 static_assert(kSpanTileRows == 4 * 32, "four waves of two 16-row blocks");
@@ -468,14 +482,10 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
       const int v0 = first_page + 2 * c;
       const bf16x8 ones1 = seen_ones(seen_keys(span, v0, pos, g4));
       const bf16x8 ones2 = seen_ones(seen_keys(span, v0, pos2, g4));
-      const int64_t page = p.a.pages[it.pages + span.entry(min(v0 + (g4 >> 1), page_end - 1))];
-      const uint16_t* at = p.a.v_pool + (page * p.a.nkv + kvh) * (16 * HD) + col * 16 + 8 * (g4 & 1);
-#pragma unroll
-      for (int e = 0; e < HD / 16; e++) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(at + e * 256);
-        put_not_finite(v, ones1, o[e]);
-        put_not_finite(v, ones2, o2[e]);
-      }
+      put_back<HD>(p, span, kvh, p.a.pages + it.pages, v0, col, g4, [&](int e, const u32x4& x) {
+        put_not_finite(x, ones1, o[e]);
+        put_not_finite(x, ones2, o2[e]);
+      });
     }
   }
 
@@ -507,10 +517,11 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
   store(row0 + 16 + col, l2, r2, o2);
 }
 
-// Stream: up to 16 rows of one position (a decode's q heads; or rows that see a whole run);
-// its waves stride over the item's 32-key chunks, keys and values straight to
-// registers, and combine through LDS.  Keys that the rows do not see are taken out by
-// select, scores and values, so what their slots hold stays out.
+// Stream: up to 16 rows (a decode's q heads, a few tokens of a prompt, rows that see a whole
+// run); its waves stride over the item's 32-key chunks, keys and values straight to
+// registers, and combine through LDS.  Values that no row sees are taken out by select, so
+// what their slots hold stays out; those that are no numbers and that some rows see only
+// come back at the end, as in a tile.
 template <int HD, bool NT, int WAVES>
 __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem& it, int kvh, char* smem) {
   const int lane = threadIdx.x & 63;
@@ -520,7 +531,8 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
   const int page_end = it.page1;
   const Span span(p, it);
   const RowAt at = row_at(p, it, kvh, min(col, it.n_rows - 1));
-  const int pos = it.pos;  // of every row
+  const int pos0 = it.pos, pos1 = it.list ? it.pos : it.pos + ItemRows(p, it).token(it.n_rows - 1);
+  bool left_out = false;
   RowState r = span_row_start();
   const float scale = p.a.scale_log2, inv_scale = 1.f / scale;
   f32x4 o[HD / 16];
@@ -538,15 +550,22 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
     const f32x4 s[2] = {score_block<HD>(c.k[0], qf), score_block<HD>(c.k[1], qf)};
     float sv[2][4];
     float mx = take_scores(s, sv);
-    if (!span.all_seen(v, pos, pos)) {
-      const unsigned seen = seen_keys(span, v, pos, g4);
-      mx = mask_scores(s, sv, seen);
+    if (!span.all_seen(v, pos0, pos1)) {
+      mx = mask_scores(s, sv, seen_keys(span, v, at.pos, g4));
       uint32_t keep[4];
-      value_mask(seen, keep);
+      value_mask(seen_keys(span, v, pos0, pos1, g4), keep);
+      bool some = false;
 #pragma unroll
-      for (int db = 0; db < HD / 16; db++)
+      for (int db = 0; db < HD / 16; db++) {
 #pragma unroll
         for (int h = 0; h < 4; h++) c.v[db][h] &= keep[h];
+        some |= some_not_finite(c.v[db]);
+      }
+      if (pos0 != pos1 && __any(some)) {
+        left_out = true;
+#pragma unroll
+        for (int db = 0; db < HD / 16; db++) drop_not_finite(c.v[db]);
+      }
     }
     if (__any(mx > r.thr)) raise_max(r, mx, scale, inv_scale, o);
     const bf16x8 pb = probs(sv, r, scale);
@@ -588,6 +607,12 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
     }
   }
 
+  if (left_out)  // (of the wave) their values once more
+    for (int v = it.page0 + 2 * wave; v < page_end; v += STEP)
+      if (!span.all_seen(v, pos0, pos1))
+        put_back<HD>(p, span, kvh, ptab, v, col, g4, [&](int e, const u32x4& x) {
+          put_not_finite(x, seen_ones(seen_keys(span, v, at.pos, g4)), o[e]);
+        });
   // (a row's output in SEGS threads of EL dims each)
   constexpr int SEGS = WAVES * 4, EL = HD / SEGS;
   float(*s_o)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(smem);

@@ -60,7 +60,7 @@ inline SpanPages span_split(SpanPages s, int split, int n_split) {
 }
 
 // A work item, of each KV head a workgroup: `n_rows` rows of a record, over some of its pages.
-//   kind 0 (stream): up to kSpanStreamRows rows of one position
+//   kind 0 (stream): up to kSpanStreamRows rows
 //   kind 1 (tile):   up to kSpanTileRows rows
 // All that a workgroup has to know before its first loads stands here: each record read on the
 // way to them costs it most of a microsecond.

@@ -72,6 +72,15 @@ struct Part {
   bool partial;  // its rows have other parts
 };
 
+// Whether a record's rows run as streams: a decode's, and so few that a stream holds them, which
+// has four waves share the keys where a tile would have one wave with rows and three without
+// (chunks of 2 to 4 tokens behind 2000 to 8000 keys take 11-15 us
+// alone, 20 in a batch of 16, as tiles 14-19 and 25).  17 to 64 rows as streams of 16 read their keys again for each: up to
+// a quarter less where a few requests are alone, up to half more in other batches, so not.
+inline bool is_stream(const SpanRows& r, int group) {
+  return r.n_rows <= kSpanStreamRows || (!r.list && r.n_rows == group);
+}
+
 // The launch order, both kinds longest first.  Streams are bound by HBM, tiles by the matrix
 // cores, and interleaved they share a CU; but all tiles have to start early enough to end
 // with the rest, so they are dealt out over the first part of the list, the share of it that
@@ -232,7 +241,7 @@ inline void plan_window(const mx_batch* b, const mx_attn_shape* s, int window, i
     const int at = p.add_table(q.pages, seen.sink_pages);
     p.add_table(q.pages + seen.sink_pages + seen.skip, seen.entries() - seen.sink_pages);
     p.rows.push_back(SpanRows{tok, q.n_new * p.group, q.ctx_len, 0, at, seen.entries(), seen.sink_pages, seen.skip, 1, -1});
-    parts.push_back(plan::Part{q.n_new == 1, false});
+    parts.push_back(plan::Part{plan::is_stream(p.rows.back(), p.group), false});
     reqs.push_back(RequestSources{tok, q.n_new, {{r, 0}}});
     tok += q.n_new;
   }
@@ -298,7 +307,7 @@ inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
     }
     const int pages = p.add_table(b->reqs[leader].pages + first, run.n_pages);
     p.rows.push_back(SpanRows{list, n_tok * p.group, INT32_MAX / 2, 1, pages, run.n_pages, 0, 0, 1, -1});
-    parts.push_back(plan::Part{n_tok * p.group <= kSpanStreamRows, true});
+    parts.push_back(plan::Part{plan::is_stream(p.rows.back(), p.group), true});
   }
   for (int r = 0; r < R; r++) {
     const mx_request& q = b->reqs[r];
@@ -306,7 +315,7 @@ inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
     reqs[r].from.push_back({(int)p.rows.size(), 0});
     const int pages = p.add_table(q.pages + own[r], end - own[r]);
     p.rows.push_back(SpanRows{reqs[r].tok, q.n_new * p.group, q.ctx_len, 0, pages, end - own[r], 0, own[r], 1, -1});
-    parts.push_back(plan::Part{q.n_new == 1, own[r] > 0});
+    parts.push_back(plan::Part{plan::is_stream(p.rows.back(), p.group), own[r] > 0});
   }
   plan_items(p, parts);
   plan_merges(p, reqs);

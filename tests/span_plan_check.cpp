@@ -55,7 +55,6 @@ static void walk(const Case& c, const SpanPlan& p) {
     CHECK(it.n_rows <= (it.kind ? kSpanTileRows : kSpanStreamRows), "rows of an item");
     CHECK(it.page0 % 2 == 0 && it.page0 >= 0, "page0 %d", it.page0);
     if (it.page0 >= it.page1) CHECK(it.part >= 0, "an empty item without partials");
-    if (it.kind == 0 && !it.list) CHECK(it.rest + it.n_rows <= group, "a stream's rows are of one position");
     std::vector<std::pair<int, int>> keys;
     for (int v = it.page0; v < it.page1; v++) {
       const int t = v < it.sink_pages ? v : v + it.skip_table;

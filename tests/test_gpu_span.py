@@ -231,6 +231,35 @@ def test_window_not_finite(nq, nkv, d, what, bad):
 
 
 # ----------------------------------------------------------------------- shared runs
+@pytest.mark.parametrize("bad", [0.0, math.nan, math.inf])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (2, 1), (5, 0), (40, 6), (700, 20), (ALL, 0)])
+@pytest.mark.parametrize("nq,nkv,d", [(4, 4, 64), (8, 2, 128), (16, 2, 128)])
+def test_few_tokens(nq, nkv, d, window, sinks, bad):
+    """Chunks of a few tokens, whose rows see different keys of the same pages: values that are
+    no numbers at both edges of the window, in the first token's sight and the last's."""
+    reqs = [(0, n, c) for n, c in [(2, 0), (3, 62), (4, 300), (2, 1000), (16, 31), (9, 2000), (2, 47), (1, 90), (5, 3000)]]
+    pools, reqs, q = window_case(nq, nkv, d, reqs, 10, window, sinks)
+    start = np.cumsum([0] + [r[1] for r in reqs])
+    clean = pools.hv.clone()
+    hit = torch.zeros(len(q), dtype=torch.bool)
+    for r, (_, n, ctx, table) in enumerate(reqs):
+        see = seen(n, ctx, window, sinks)
+        for j in {ctx + n - 1, max(0, ctx - window + 1), ctx} if bad else ():
+            if see[:, j].any():
+                pools.hv[table[j // 16], :, j % 16, 7] = bad
+                hit[start[r]:start[r + 1]] |= torch.from_numpy(see[:, j])
+    pools.upload()
+    got, _ = run_window(pools, nq, reqs, q.cuda(), window, sinks)
+    got, pools.hv = got.cpu(), clean
+    out, mag = reference(pools, nq, reqs, q, window, sinks)
+    if not hit.all():
+        check(got[~hit], out[~hit.numpy()], mag[~hit.numpy()])
+    rest = torch.arange(d) != 7
+    check(got[..., rest], out[..., rest.numpy()], mag[..., rest.numpy()])
+    at = got[hit][..., 7]
+    assert torch.isnan(at).all() if math.isnan(bad) else (at == bad).all()
+
+
 def shared_case(nq, nkv, d, reqs, runs, seed):
     """Requests of (decode, n_new, own cached tokens); runs of (first, requests, pages)."""
     rng = np.random.default_rng(seed)
