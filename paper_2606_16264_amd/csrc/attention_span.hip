@@ -10,7 +10,13 @@
 // softmax in the four lanes that hold it.
 //
 // Rows with several items (split keys; shared and own keys) leave unnormalised outputs,
-// maxima and sums in fp32, which a second launch joins in a fixed order.
+// maxima and sums in fp32, which a second launch joins in a fixed order.  (Joined by the last
+// of them to end instead, behind fences or with partials written through to memory, a call
+// takes 8 to 250 us more; the launch takes 4 to 6.)
+//
+// Probabilities are rounded to bf16 for the value product, up to 2^-9 of each; the row sums
+// are those of the rounded ones, so that the errors of numerator and denominator go together.
+// Scores, maxima, sums and outputs stay in fp32 up to the one rounding of the result.
 //
 // Masked scores are -inf and a row's running maximum starts at the lowest finite number, so
 // that a row without a key in an item's chunk, or in the whole item, adds exactly 0.
@@ -23,14 +29,15 @@ namespace mx {
 
 namespace {
 
+constexpr int kWaves = 4;  // of a workgroup
 constexpr float kLowest = -3.402823466e38f, kInf = __builtin_inff();
 __device__ __forceinline__ RowState span_row_start() { return RowState{kLowest, -kInf, 0.f}; }
 
 // Where an item's pages lie, and what a position sees of them.
 struct Span {
-  int sink_pages, skip_table, skip_real, page0, page_end, window, sinks;
+  int sink_pages, skip_table, skip_real, page_end, window, sinks;
   __device__ __forceinline__ Span(const SpanParams& p, const SpanItem& it)
-      : sink_pages(it.sink_pages), skip_table(it.skip_table), skip_real(it.skip_real), page0(it.page0),
+      : sink_pages(it.sink_pages), skip_table(it.skip_table), skip_real(it.skip_real),
         page_end(it.page1), window(p.window), sinks(p.sinks) {}
   __device__ __forceinline__ int entry(int v) const { return v < sink_pages ? v : v + skip_table; }
   __device__ __forceinline__ int first_key(int v) const {  // of page v, as a position
@@ -190,6 +197,15 @@ static_assert(kSpanTileRows == 4 * 32, "four waves of two 16-row blocks");
 // how the copies run three chunks ahead).  Chunks that all rows of the tile see whole, from
 // first_whole to end_whole, take no masks; those before (the window's low edge, sinks) and
 // behind (the diagonal, the end) do, and a wave leaves out those that none of its rows sees.
+//
+// Bound by the matrix cores and the vector instructions of the softmax beside them, at the
+// clock that the power limit leaves: a chunk takes 0.87 us with two workgroups on a CU (0.52
+// to 0.66 with one), 1.25 with masks, the start 3.5 and the end 2.2.  2048 tokens of 64 q
+// heads through a window of 4096 take 246 us, 1.13 PFLOP/s of what the rows see; a prompt of
+// 8191 on 32 heads through 1024 takes 175, 0.74 of what they see, as each tile of 128 tokens
+// takes 9 chunks of 37 with masks.  128 rows: twice as many in a workgroup would leave one of
+// them on a CU, and half as many copy twice as much.  The 32x32x16 instruction takes half the
+// issue slots and 290 us where this takes 255: the clock falls.
 template <int HD>
 __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& it, int kvh, char* smem) {
   using SC = SharedChunk<HD>;
@@ -522,7 +538,12 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
 // registers, and combine through LDS.  Values that no row sees are taken out by select, so
 // what their slots hold stays out; those that are no numbers and that some rows see only
 // come back at the end, as in a tile.
-template <int HD, bool NT, int WAVES>
+//
+// Bound by HBM: 128 decodes of 8 KV heads through a window of 4096 read 2.1 GB in 317 us, 6.7
+// TB/s; 64 through 1024 their 267 MB in 44, of which some 4 are the first chain of loads (item,
+// page id, keys).  With few items that chain is the time: 4 us.  (Eight waves to a workgroup
+// where streams are alone in up to 256: nothing gained over batches drawn at random.)
+template <int HD, bool NT>
 __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem& it, int kvh, char* smem) {
   const int lane = threadIdx.x & 63;
   const int wave = threadIdx.x >> 6;
@@ -574,7 +595,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
   };
   // two chunk buffers in turn, a chunk's loads issued only where it exists (decode_item of
   // the bf16 attention tells why)
-  constexpr int STEP = 2 * WAVES;
+  constexpr int STEP = 2 * kWaves;
   Chunk<HD> ca, cb;
   int v = it.page0 + 2 * wave;
   if (v < page_end) {
@@ -614,10 +635,10 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
           put_not_finite(x, seen_ones(seen_keys(span, v, at.pos, g4)), o[e]);
         });
   // (a row's output in SEGS threads of EL dims each)
-  constexpr int SEGS = WAVES * 4, EL = HD / SEGS;
+  constexpr int SEGS = kWaves * 4, EL = HD / SEGS;
   float(*s_o)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(smem);
-  float(*s_m)[16] = reinterpret_cast<float(*)[16]>(smem + WAVES * 16 * (HD + 4) * 4);
-  float(*s_l)[16] = s_m + WAVES;
+  float(*s_m)[16] = reinterpret_cast<float(*)[16]>(smem + kWaves * 16 * (HD + 4) * 4);
+  float(*s_l)[16] = s_m + kWaves;
 #pragma unroll
   for (int db = 0; db < HD / 16; db++)
     *reinterpret_cast<f32x4*>(&s_o[wave][col][db * 16 + 4 * g4]) = o[db];
@@ -632,10 +653,10 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
   if (row >= it.n_rows) return;
   float M = kLowest;
 #pragma unroll
-  for (int w = 0; w < WAVES; w++) M = fmaxf(M, s_m[w][row]);
-  float wt[WAVES], L = 0.f;
+  for (int w = 0; w < kWaves; w++) M = fmaxf(M, s_m[w][row]);
+  float wt[kWaves], L = 0.f;
 #pragma unroll
-  for (int w = 0; w < WAVES; w++) {
+  for (int w = 0; w < kWaves; w++) {
     wt[w] = exp2f(s_m[w][row] - M);
     L += s_l[w][row] * wt[w];
   }
@@ -644,7 +665,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
   for (int e = 0; e < EL; e++) {
     float a = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; w++) a += s_o[w][row][dseg + e] * wt[w];
+    for (int w = 0; w < kWaves; w++) a += s_o[w][row][dseg + e] * wt[w];
     acc[e] = a;
   }
   if (it.part < 0) {
@@ -689,15 +710,15 @@ __device__ __forceinline__ SpanParams inline_params(const SmallSpan& s) {
   return p;
 }
 
-template <int HD, int WAVES>
+template <int HD>
 constexpr int combine_bytes() {
-  return (WAVES * 16 * (HD + 4) + 2 * WAVES * 16) * 4;
+  return (kWaves * 16 * (HD + 4) + 2 * kWaves * 16) * 4;
 }
-template <int HD, bool TILES, int WAVES>
+template <int HD, bool TILES>
 constexpr int span_smem() {
-  return TILES ? smem_bytes<HD>() : combine_bytes<HD, WAVES>();
+  return TILES ? smem_bytes<HD>() : combine_bytes<HD>();
 }
-template <int HD, bool TILES, int WAVES>
+template <int HD, bool TILES>
 __device__ __forceinline__ void span_item(const SpanParams& p, char* smem) {
   const SpanBlock b = span_block(blockIdx.x, p.n_items, p.a.nkv, p.heads);
   const SpanItem it = p.items[b.item];
@@ -705,26 +726,29 @@ __device__ __forceinline__ void span_item(const SpanParams& p, char* smem) {
     empty_item<HD>(p, it, part_of(it, b.kvh));
   } else if constexpr (TILES) {
     if (it.kind == 1) tile_item<HD>(p, it, b.kvh, smem);
-    else stream_item<HD, false, WAVES>(p, it, b.kvh, smem);
+    else stream_item<HD, false>(p, it, b.kvh, smem);
   } else {
-    stream_item<HD, true, WAVES>(p, it, b.kvh, smem);
+    stream_item<HD, true>(p, it, b.kvh, smem);
   }
 }
-template <int HD, bool TILES, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void span_attn_kernel(
+template <int HD, bool TILES>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void span_attn_kernel(
     SpanParams p) {
-  __shared__ __attribute__((aligned(16))) char smem[span_smem<HD, TILES, WAVES>()];
-  span_item<HD, TILES, WAVES>(p, smem);
+  __shared__ __attribute__((aligned(16))) char smem[span_smem<HD, TILES>()];
+  span_item<HD, TILES>(p, smem);
 }
-template <int HD, bool TILES, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void small_span_kernel(
+template <int HD, bool TILES>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void small_span_kernel(
     SmallSpan s) {
-  __shared__ __attribute__((aligned(16))) char smem[span_smem<HD, TILES, WAVES>()];
-  span_item<HD, TILES, WAVES>(inline_params(s), smem);
+  __shared__ __attribute__((aligned(16))) char smem[span_smem<HD, TILES>()];
+  span_item<HD, TILES>(inline_params(s), smem);
 }
 
 // The merge: HD / 4 threads hold a row; a workgroup takes 8 (HD = 128) or 16 q heads of a
-// token, or (WIDE) one q head, whose partials its groups of threads read side by side.
+// token, or (WIDE) one q head, whose partials its groups of threads read side by side: with
+// more than eight partials a row, read one behind another, their latency is the time (from
+// four on: a prompt of 3314 tokens 38.6 us a call for 31.5; from 25 on: three decodes of a run
+// of 361 pages 34.8 for 31.1).  Bound by latency: 4 us, up to 6 for 128 tokens of 64 q heads.
 template <int HD, bool WIDE>
 __device__ __forceinline__ void span_merge(const SpanParams& p) {
   constexpr int TPR = HD / 4, G = kMergeThreads / TPR;
@@ -792,8 +816,6 @@ __global__ __launch_bounds__(kMergeThreads) void small_span_merge_kernel(SmallSp
   span_merge<HD, WIDE>(inline_params(s));
 }
 
-// Streams alone in few workgroups: eight waves each, so that a wave takes half the keys.
-constexpr int kCUs = 256;
 template <int HD>
 hipError_t launch(const SpanParams& p, const InlineMeta* meta, bool tiles, int n_merge, int most_parts,
                   hipStream_t stream) {
@@ -801,13 +823,11 @@ hipError_t launch(const SpanParams& p, const InlineMeta* meta, bool tiles, int n
   if (n == 0) return hipSuccess;
   if (meta) {
     const SmallSpan s{p, *meta};
-    if (tiles) small_span_kernel<HD, true, 4><<<n, 256, 0, stream>>>(s);
-    else if (n <= kCUs) small_span_kernel<HD, false, 8><<<n, 512, 0, stream>>>(s);
-    else small_span_kernel<HD, false, 4><<<n, 256, 0, stream>>>(s);
+    if (tiles) small_span_kernel<HD, true><<<n, 64 * kWaves, 0, stream>>>(s);
+    else small_span_kernel<HD, false><<<n, 64 * kWaves, 0, stream>>>(s);
   } else {
-    if (tiles) span_attn_kernel<HD, true, 4><<<n, 256, 0, stream>>>(p);
-    else if (n <= kCUs) span_attn_kernel<HD, false, 8><<<n, 512, 0, stream>>>(p);
-    else span_attn_kernel<HD, false, 4><<<n, 256, 0, stream>>>(p);
+    if (tiles) span_attn_kernel<HD, true><<<n, 64 * kWaves, 0, stream>>>(p);
+    else span_attn_kernel<HD, false><<<n, 64 * kWaves, 0, stream>>>(p);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || n_merge == 0) return e;

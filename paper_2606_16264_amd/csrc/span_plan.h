@@ -29,7 +29,9 @@ inline SeenPages seen_pages(int ctx, int n, int window, int sinks) {
 }
 
 // Joining the parts of a row costs a launch, partials written and read: runs are left to
-// their requests where less than this would be read once instead of several times.
+// their requests where less than this would be read once instead of several times.  (Over
+// batches drawn at random from 24 MB takes 0.4 to 1.3% more than from 64; with sharing
+// wherever it saves this much, none took 1.23 times what it takes without.)
 constexpr int64_t kMinSharedBytes = 64 << 20;
 
 struct SpanPlan {
@@ -58,11 +60,18 @@ struct SpanPlan {
 
 namespace plan {
 
+// (Both sides of each, over batches drawn at random.  Splits of streams of 16 pages instead of
+// 32: 1% more, the metadata of 4 decodes through 1500 keys on 32 heads no longer goes with the
+// arguments and they take 25.2 us for 20.4; of 48: up to a quarter more for a few decodes.
+// Whole streams of up to 32 pages only: 2% more; up to 128: nothing gained.  Whole tiles of up
+// to 16 pages only: 250 tokens in three prompts behind a run take 24.1 for 20.6; up to 96:
+// nothing.  Splits of tiles of 32 pages where they are alone: 1 to 3% more.)
 constexpr int64_t kSlots = 512;      // workgroups that the chip holds at once
-constexpr int kMinSplitPages = 16;   // of a stream
+constexpr int kMinSplitPages = 32;   // of a stream's split
 constexpr int kWholePages = 64;      // streams of up to that many are not split
 constexpr int kWholeTilePages = 48;  // tiles of up to that many are not split
-constexpr int kMinTilePages = 16;
+constexpr int kMinTilePages = 16;    // of a tile's split
+constexpr int kFullPages = 16;       // streams of so many for each workgroup fill the chip
 constexpr int kExtraTiles = 1024;    // items that splitting tiles adds to a call, at most
 constexpr int kMostSplits = 4096;
 
@@ -73,10 +82,10 @@ struct Part {
 };
 
 // Whether a record's rows run as streams: a decode's, and so few that a stream holds them, which
-// has four waves share the keys where a tile would have one wave with rows and three without
-// (chunks of 2 to 4 tokens behind 2000 to 8000 keys take 11-15 us
-// alone, 20 in a batch of 16, as tiles 14-19 and 25).  17 to 64 rows as streams of 16 read their keys again for each: up to
-// a quarter less where a few requests are alone, up to half more in other batches, so not.
+// has four waves share the keys where a tile would have one wave with rows and three without:
+// chunks of 2 to 4 tokens behind 2000 to 8000 keys take 11 to 15 us, as tiles 14 to 19, and 16
+// of them on 32 KV heads 20 and 25.  17 to 64 rows as streams of 16 would read their keys again
+// for each: up to a quarter less where a few requests are alone, half more in other batches.
 inline bool is_stream(const SpanRows& r, int group) {
   return r.n_rows <= kSpanStreamRows || (!r.list && r.n_rows == group);
 }
@@ -84,7 +93,9 @@ inline bool is_stream(const SpanRows& r, int group) {
 // The launch order, both kinds longest first.  Streams are bound by HBM, tiles by the matrix
 // cores, and interleaved they share a CU; but all tiles have to start early enough to end
 // with the rest, so they are dealt out over the first part of the list, the share of it that
-// is left of the whole when one tile's time is taken off its end.
+// is left of the whole when one tile's time is taken off its end.  (1024 tokens beside 64
+// decodes: 79.8 us, all tiles first 84.7; dealt evenly to the end, 128 decodes of one document
+// of 16384 tokens take 145 for 123.)
 struct Cost {
   SpanItem item;
   int64_t cost;
@@ -121,7 +132,7 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
     return span_seen(r, row / p.group, (row + n - 1) / p.group, p.window).page1;
   };
   // how much there is to do, in pages of one head
-  int64_t pages[2] = {}, n_items[2] = {};
+  int64_t pages[2] = {};
   int longest = 0;
   for (size_t i = 0; i < parts.size(); i++) {
     const SpanRows& r = p.rows[i];
@@ -129,7 +140,6 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
     for (int row = 0; row < r.n_rows; row += step) {
       const int n = seen(r, row, std::min(step, r.n_rows - row));
       pages[tile] += n;
-      n_items[tile]++;
       if (!tile) longest = std::max(longest, n);
     }
   }
@@ -140,10 +150,16 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
   const bool whole = longest <= std::max<int64_t>(kWholePages, share + share / 4);
   const int stream_split = whole ? longest : even(std::max<int64_t>(kMinSplitPages, share / 2));
   // Tiles are split to as many as the chip holds at once, or one for each CU beside streams
-  // that take a good part of it.
+  // that take a good part of the time.  (Alone for each CU only: a prompt of 7659 tokens on 4
+  // heads takes 80 us for 58, 371 tokens in 12 prompts on 40 heads 86 for 61.  Beside streams
+  // as many as fit: 1024 tokens of 64 q heads beside 64 decodes 80 for 72.)  Where the streams
+  // fill the chip as well, with splits of 32 pages, so that there is less to join: 32 decodes
+  // of one prompt of 2000 take 43.6 us, with splits of 16 45.8; a tree 67.7 and 70.8.  Where
+  // they do not the longest tile is the time: 45 decodes below six runs 25 us, 33 with 32.
   const bool mixed = pages[0] * kStreamPage > pages[1] / 4;
   const int64_t slots = mixed ? kSlots / 2 : kSlots;
-  const int tile_split = even(std::max<int64_t>(mixed ? 2 * kMinTilePages : kMinTilePages, (pages[1] * p.nkv + slots - 1) / slots));
+  const int min_tile = mixed && pages[0] * p.nkv >= kFullPages * kSlots ? 2 * kMinTilePages : kMinTilePages;
+  const int tile_split = even(std::max<int64_t>(min_tile, (pages[1] * p.nkv + slots - 1) / slots));
   std::vector<Cost> list[2];
   int64_t extra = kExtraTiles;
   for (size_t i = 0; i < parts.size(); i++) {
@@ -250,7 +266,9 @@ inline void plan_window(const mx_batch* b, const mx_attn_shape* s, int window, i
 }
 
 // A prompt whose rows fill tiles by themselves takes its shared keys with its own: the rows
-// that would be saved, times the keys, against partials for all of its rows.
+// that would be saved, times the keys, against partials for all of its rows.  (With 512: 1500
+// tokens in 12 prompts about one document beside 24 decodes of it take 218 us for 210; with
+// 8192: nothing gained.)
 constexpr int64_t kWholePromptKeys = 2048;
 
 inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
