@@ -537,13 +537,16 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
 // run); its waves stride over the item's 32-key chunks, keys and values straight to
 // registers, and combine through LDS.  Values that no row sees are taken out by select, so
 // what their slots hold stays out; those that are no numbers and that some rows see only
-// come back at the end, as in a tile.
+// come back at the end, as in a tile.  Keys and values are loaded non-temporally, also beside
+// tiles: a call reads them once, and with the cache full of a layer's other data, which they
+// would have to push out, 74 decodes beside a shared run take 98 us so and 140 otherwise, a
+// prompt of 1024 tokens beside 64 decodes 78 and 90.
 //
 // Bound by HBM: 128 decodes of 8 KV heads through a window of 4096 read 2.1 GB in 317 us, 6.7
 // TB/s; 64 through 1024 their 267 MB in 44, of which some 4 are the first chain of loads (item,
 // page id, keys).  With few items that chain is the time: 4 us.  (Eight waves to a workgroup
 // where streams are alone in up to 256: nothing gained over batches drawn at random.)
-template <int HD, bool NT>
+template <int HD>
 __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem& it, int kvh, char* smem) {
   const int lane = threadIdx.x & 63;
   const int wave = threadIdx.x >> 6;
@@ -600,7 +603,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
   int v = it.page0 + 2 * wave;
   if (v < page_end) {
     int n0 = pid(v + STEP), n1 = pid(v + STEP + 1);
-    load_chunk<HD, NT>(ca, p.a, kvh, pid(v), pid(v + 1), 0, col, g4);
+    load_chunk<HD, true>(ca, p.a, kvh, pid(v), pid(v + 1), 0, col, g4);
     while (true) {
       int vn = v + STEP;
       if (vn >= page_end) {
@@ -608,7 +611,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
         break;
       }
       int m0 = pid(vn + STEP), m1 = pid(vn + STEP + 1);
-      load_chunk<HD, NT>(cb, p.a, kvh, n0, n1, 0, col, g4);
+      load_chunk<HD, true>(cb, p.a, kvh, n0, n1, 0, col, g4);
       proc(ca, v);
       v = vn;
       n0 = m0;
@@ -620,7 +623,7 @@ __device__ __forceinline__ void stream_item(const SpanParams& p, const SpanItem&
       }
       m0 = pid(vn + STEP);
       m1 = pid(vn + STEP + 1);
-      load_chunk<HD, NT>(ca, p.a, kvh, n0, n1, 0, col, g4);
+      load_chunk<HD, true>(ca, p.a, kvh, n0, n1, 0, col, g4);
       proc(cb, v);
       v = vn;
       n0 = m0;
@@ -726,9 +729,9 @@ __device__ __forceinline__ void span_item(const SpanParams& p, char* smem) {
     empty_item<HD>(p, it, part_of(it, b.kvh));
   } else if constexpr (TILES) {
     if (it.kind == 1) tile_item<HD>(p, it, b.kvh, smem);
-    else stream_item<HD, false>(p, it, b.kvh, smem);
+    else stream_item<HD>(p, it, b.kvh, smem);
   } else {
-    stream_item<HD, true>(p, it, b.kvh, smem);
+    stream_item<HD>(p, it, b.kvh, smem);
   }
 }
 template <int HD, bool TILES>
