@@ -94,12 +94,13 @@ inline bool is_stream(const SpanRows& r, int group) {
 // cores, and interleaved they share a CU; but all tiles have to start early enough to end
 // with the rest, so they are dealt out over the first part of the list, the share of it that
 // is left of the whole when one tile's time is taken off its end.  (1024 tokens beside 64
-// decodes: 79.8 us, all tiles first 84.7; dealt evenly to the end, 128 decodes of one document
-// of 16384 tokens take 145 for 123.)
+// decodes: 68 us, all tiles first 75; dealt evenly to the end those take 64, but 128 decodes
+// of one document of 16384 tokens 136 for 110.)
 struct Cost {
   SpanItem item;
   int64_t cost;
 };
+// (1.0: those 1024 tokens take 74 us, the tree as long; 2.4: 70, the tree 63 for 62.)
 constexpr double kStreamPage = 1.6;  // time of a stream's page, in tile pages
 inline void order_items(std::vector<Cost>& tiles, std::vector<Cost>& streams, int nkv,
                         std::vector<SpanItem>& out) {
@@ -152,9 +153,9 @@ inline void plan_items(SpanPlan& p, const std::vector<plan::Part>& parts) {
   // Tiles are split to as many as the chip holds at once, or one for each CU beside streams
   // that take a good part of the time.  (Alone for each CU only: a prompt of 7659 tokens on 4
   // heads takes 80 us for 58, 371 tokens in 12 prompts on 40 heads 86 for 61.  Beside streams
-  // as many as fit: 1024 tokens of 64 q heads beside 64 decodes 80 for 72.)  Where the streams
+  // as many as fit: 1024 tokens of 64 q heads beside 64 decodes 72.6 for 68.1.)  Where the streams
   // fill the chip as well, with splits of 32 pages, so that there is less to join: 32 decodes
-  // of one prompt of 2000 take 43.6 us, with splits of 16 45.8; a tree 67.7 and 70.8.  Where
+  // of one prompt of 2000 take 44.4 us, with splits of 16 46.2; a tree 62.0 and 65.1.  Where
   // they do not the longest tile is the time: 45 decodes below six runs 25 us, 33 with 32.
   const bool mixed = pages[0] * kStreamPage > pages[1] / 4;
   const int64_t slots = mixed ? kSlots / 2 : kSlots;
@@ -267,7 +268,7 @@ inline void plan_window(const mx_batch* b, const mx_attn_shape* s, int window, i
 
 // A prompt whose rows fill tiles by themselves takes its shared keys with its own: the rows
 // that would be saved, times the keys, against partials for all of its rows.  (With 512: 1500
-// tokens in 12 prompts about one document beside 24 decodes of it take 218 us for 210; with
+// tokens in 12 prompts about one document beside 24 decodes of it take 219 us for 215; with
 // 8192: nothing gained.)
 constexpr int64_t kWholePromptKeys = 2048;
 
