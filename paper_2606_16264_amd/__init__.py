@@ -506,7 +506,7 @@ def mx_workspace_bytes_window_for(batch: Batch, shape: AttnShape, window: int, s
 
 
 def mx_workspace_bytes_window(shape: AttnShape, max_tokens: int, max_reqs: int, max_pages: int) -> int:
-    return _size(_lib.mx_workspace_bytes_window(ctypes.byref(shape), max_tokens, max_reqs, max_pages))
+    return _size(_lib.mx_workspace_bytes_window(ctypes.byref(shape), *_int32(max_tokens, max_reqs), max_pages))
 
 
 def mx_paged_attn_window(batch: Batch, shape: AttnShape, window: int, sinks: int, q, k_pool, v_pool,
@@ -526,8 +526,8 @@ def mx_workspace_bytes_shared_for(batch: Batch, shape: AttnShape, runs: SharedRu
 
 def mx_workspace_bytes_shared(shape: AttnShape, max_tokens: int, max_reqs: int, max_pages: int,
                               max_depth: int) -> int:
-    return _size(_lib.mx_workspace_bytes_shared(ctypes.byref(shape), max_tokens, max_reqs, max_pages,
-                                                max_depth))
+    return _size(_lib.mx_workspace_bytes_shared(ctypes.byref(shape), *_int32(max_tokens, max_reqs),
+                                                max_pages, *_int32(max_depth)))
 
 
 def mx_paged_attn_shared(batch: Batch, shape: AttnShape, runs: SharedRuns, q, k_pool, v_pool, out, ws,

@@ -1783,15 +1783,17 @@ size_t span_bound(const mx_attn_shape* s, int32_t max_tokens, int32_t max_reqs, 
     return 0;
   }
   const int64_t nkv = s->n_kv_heads, group = s->n_q_heads / nkv;
-  const int64_t parts = (int64_t)max_reqs * (depth + 1), tokens = (int64_t)max_tokens * (depth + 1);
+  // (what does not fit 32 bits is refused by the calls)
+  auto most = [](__int128 n) { return (int64_t)std::min<__int128>(n, INT32_MAX); };
+  const int64_t parts = most((int64_t)max_reqs * ((int64_t)depth + 1));
+  const int64_t tokens = most((int64_t)max_tokens * ((int64_t)depth + 1));
+  max_pages = most(max_pages);
   const int64_t streams = max_pages / plan::kMinSplitPages + parts;
-  const int64_t items = streams * ceil_div(group, kSpanStreamRows) +
-                        ceil_div(tokens * group, kSpanTileRows) + parts + plan::kExtraTiles;
-  return make_layout_span(items, max_pages, tokens, max_tokens, parts,
-                          streams * nkv * std::max<int64_t>(kSpanStreamRows, group) +
-                              tokens * s->n_q_heads + (int64_t)plan::kExtraTiles * kSpanTileRows,
-                          s->head_dim)
-      .total;
+  const int64_t items = most(streams * ceil_div(group, kSpanStreamRows) +
+                             ceil_div(tokens * group, kSpanTileRows) + parts + plan::kExtraTiles);
+  const int64_t partials = most((__int128)streams * nkv * std::max<int64_t>(kSpanStreamRows, group) +
+                                tokens * s->n_q_heads + (int64_t)plan::kExtraTiles * kSpanTileRows);
+  return make_layout_span(items, max_pages, tokens, max_tokens, parts, partials, s->head_dim).total;
 }
 
 mx_status validate_window(int32_t window, int32_t sinks) {

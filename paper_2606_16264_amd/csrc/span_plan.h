@@ -325,7 +325,8 @@ inline void plan_shared(const mx_batch* b, const mx_attn_shape* s, int num_runs,
       own[r] = start[r];
     }
     const int pages = p.add_table(b->reqs[leader].pages + first, run.n_pages);
-    p.rows.push_back(SpanRows{list, n_tok * p.group, INT32_MAX / 2, 1, pages, run.n_pages, 0, 0, 1, -1});
+    // (a position behind every key)
+    p.rows.push_back(SpanRows{list, n_tok * p.group, INT32_MAX - 16, 1, pages, run.n_pages, 0, 0, 1, -1});
     parts.push_back(plan::Part{plan::is_stream(p.rows.back(), p.group), true});
   }
   for (int r = 0; r < R; r++) {

@@ -66,7 +66,7 @@ static void walk(const Case& c, const SpanPlan& p) {
       const int tk = (it.rest + i) / group, h = at_b.kvh * group + (it.rest + i) % group;
       const int tok = it.list ? p.tokens.at(it.tok + tk) : it.tok + tk;
       CHECK(tok >= 0 && tok < T, "token %d", tok);
-      CHECK(it.list || it.pos + tk == tok_pos[tok], "position");
+      CHECK(it.list ? it.pos >= INT32_MAX - 16 : it.pos + tk == tok_pos[tok], "position");
       if (it.part >= 0) {
         const int at = it.part + at_b.kvh * it.kvh_stride + i;
         CHECK(at < p.n_parts, "partial %d of %lld", at, (long long)p.n_parts);

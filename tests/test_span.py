@@ -200,7 +200,7 @@ def test_workspace_bounds_cover_batches(seed):
         dec = rng.random(R) < 0.6
         depth, k = int(rng.integers(0, 4)), int(rng.choice([1, 30, 800]))
         ctx = rng.integers(1, rng.choice([20, 300, 40000]), R) + 16 * depth * k
-        new = np.where(dec, 1, rng.integers(1, 400, R))
+        new = np.where(dec, 1, rng.integers(1, rng.choice([6, 400]), R))
         need = -(-(ctx + new) // 16)
         at = np.cumsum(np.concatenate([[depth * k], need - depth * k]))
         b = mx.Batch(dec.astype(int), new, ctx, [np.r_[np.arange(depth * k), np.arange(at[r], at[r + 1])] for r in range(R)])
@@ -211,8 +211,28 @@ def test_workspace_bounds_cover_batches(seed):
         assert 0 < mx.mx_workspace_bytes_shared_for(b, s, runs) <= mx.mx_workspace_bytes_shared(s, T, R, pages, depth)
 
 
+def test_workspace_bounds_of_large_numbers():
+    """Bounds grow with what they bound, up to the largest numbers."""
+    big = 2 ** 31 - 1
+    for heads in ((32, 8, 128), (32767, 1, 64), (32767, 32767, 128)):
+        s = shape(*heads, 1 << 40)
+        last = 0
+        for n in (1, 100, 10 ** 4, 10 ** 6, 10 ** 8, big):
+            now = mx.mx_workspace_bytes_window(s, n, n, n * n)
+            deep = mx.mx_workspace_bytes_shared(s, n, n, n * n, n)
+            assert last <= now <= deep < 2 ** 42
+            last = now
+
+
 def test_binding_refuses_numbers_that_32_bits_do_not_hold():
     b, s = one(), shape()
+    for n in (2 ** 31, 2 ** 32 + 1, -2 ** 31 - 1):
+        for tokens, reqs, depth in ((n, 1, 1), (1, n, 1), (1, 1, n)):
+            with pytest.raises(ValueError):
+                mx.mx_workspace_bytes_shared(s, tokens, reqs, 1, depth)
+            if depth == 1:
+                with pytest.raises(ValueError):
+                    mx.mx_workspace_bytes_window(s, tokens, reqs, 1)
     for w, sinks in ((2 ** 32 + 8, 0), (8, 2 ** 32 + 1), (2 ** 31, 0), (8, -2 ** 31 - 1)):
         with pytest.raises(ValueError):
             mx.mx_workspace_bytes_window_for(b, s, w, sinks)
