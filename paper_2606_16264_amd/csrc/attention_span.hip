@@ -14,7 +14,7 @@
 // of them to end instead, behind fences or with partials written through to memory, a call
 // takes 8 to 250 us more; the launch takes 4 to 6.)
 //
-// Probabilities are rounded to bf16 for the value product, up to 2^-9 of each; the row sums
+// Probabilities are rounded to bf16 for the value product, by up to 2^-8 of each; the row sums
 // are those of the rounded ones, so that the errors of numerator and denominator go together.
 // Scores, maxima, sums and outputs stay in fp32 up to the one rounding of the result.
 //
