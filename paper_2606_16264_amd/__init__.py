@@ -156,7 +156,9 @@ import torch  # noqa: E402  (loaded already, before the library)
 
 # what the calls on tensors ask of torch every time
 _BF16 = (torch.bfloat16, torch.uint16)  # uint16: the bits of bf16
-_current_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+_current_device = torch.cuda.current_device
+# (None in a torch built without a GPU, where no tensor comes as far as to need it)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def lib() -> ctypes.CDLL:
