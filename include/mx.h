@@ -281,10 +281,13 @@ mx_status mx_paged_attn_window(const mx_batch* batch, const mx_attn_shape* shape
  * caches.  A run says that requests first_req .. first_req + num_reqs - 1 hold the same
  * n_pages pages, behind the pages of the runs before it that they belong to: the first
  * run of a request starts at its page 0, its next one where that ends, and so on (a system
- * prompt shared by all, examples shared by some).  The keys and values of a run are read
- * once for all of its requests (a prompt chunk that fills its tiles by itself reads them
- * for its own rows).  The result is mx_paged_attn's up to the order of sums and the
- * rounding of the probabilities.
+ * prompt shared by all, examples shared by some).  Runs say what may be read once.  Where
+ * all runs of the call together save at least 64 MiB of reads, the keys and values of each
+ * are read once for its requests (a prompt chunk that nearly fills its tiles by itself reads
+ * them for its own rows); where they save less, every request reads its pages by itself, as
+ * joining the parts of a row costs a launch.  Which of the two follows from the batch, the
+ * shape and the runs, and the order of sums with it, so the last bits of a result too.  The
+ * result is mx_paged_attn's up to that order and the rounding of the probabilities.
  * MX_ERR_INVALID where a run has no request or no page, names a request that is not there,
  * has requests that differ in where it starts or in the pages' ids, or reaches past the
  * cached tokens of one (16 * pages <= ctx_len).

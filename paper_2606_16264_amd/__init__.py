@@ -534,7 +534,8 @@ def mx_workspace_bytes_shared(shape: AttnShape, max_tokens: int, max_reqs: int, 
 
 def mx_paged_attn_shared(batch: Batch, shape: AttnShape, runs: SharedRuns, q, k_pool, v_pool, out, ws,
                          stream=None) -> None:
-    """mx_paged_attn where requests share runs of pages, whose keys are read once."""
+    """mx_paged_attn where requests share runs of pages, whose keys are read once for them if
+    all runs of the call together save 64 MiB of reads or more."""
     device = _check_attn(batch, shape, q, k_pool, v_pool, out, ws)
     _check(_lib.mx_paged_attn_shared(batch.ptr, ctypes.byref(shape), runs.n, runs.ptr, _ptr(q),
                                      _ptr(k_pool), _ptr(v_pool), _ptr(out), _ptr(ws), ws.numel(),

@@ -28,10 +28,11 @@ inline SeenPages seen_pages(int ctx, int n, int window, int sinks) {
   return s;
 }
 
-// Joining the parts of a row costs a launch, partials written and read: runs are left to
-// their requests where less than this would be read once instead of several times.  (Over
-// batches drawn at random from 24 MB takes 0.4 to 1.3% more than from 64; with sharing
-// wherever it saves this much, none took 1.23 times what it takes without.)
+// Joining the parts of a row costs a launch, partials written and read: all runs of a call are
+// left to their requests where less than this, in sum, would be read once instead of several
+// times.  (Over batches drawn at random a limit of 24 MB takes 0.4 to 1.3% more than one of
+// 64.  Once a call is above it all of its runs are joined, the short ones too: not measured
+// against joining some of them.)
 constexpr int64_t kMinSharedBytes = 64 << 20;
 
 struct SpanPlan {

@@ -42,3 +42,36 @@ def test_gpu_batches_are_taken_apart(planner, name):
     heads, reqs, runs = CASES[name]
     got, = planner([(heads, tables(reqs, runs, itertools.count()), runs, -1)])
     assert tuple(got[:2]) == JOINED[name]
+
+
+def decodes(n, nkv, runs, d=128):
+    """Decodes of a few own tokens below runs; the heads, requests and runs of a planner's batch."""
+    return (nkv, nkv, d), tables([(1, 1, 3 + i) for i in range(n)], runs, itertools.count()), runs
+
+
+@pytest.mark.parametrize("d,nkv,pages", [(128, 8, 64), (64, 8, 128), (128, 1, 512)])
+def test_runs_are_joined_from_64_mib_on(planner, d, nkv, pages):
+    """17 requests, for 16 of which a run of `pages` pages is not read again: 64 MiB."""
+    assert 16 * pages * nkv * 16 * 2 * 2 * d == 64 << 20
+    batches = [decodes(n, nkv, [(0, n, pages - k)], d) for n, k in ((17, 0), (17, 1), (16, 0), (18, 1))]
+    got = planner([b + (-1,) for b in batches])
+    assert [g[0] for g in got] == [1, 0, 0, 1]
+
+
+def test_runs_are_joined_all_or_none(planner):
+    """What counts is what all runs of a call save together: then the shortest of them is joined too."""
+    half = [(0, 17, 32), (17, 16, 33)]
+    alone, both, more = planner([decodes(33, 8, half[:1]) + (-1,), decodes(33, 8, half) + (-1,),
+                                 decodes(36, 8, half + [(33, 3, 1)]) + (-1,)])
+    assert 16 * 32 + 15 * 33 < 1024 <= 16 * 32 + 15 * 33 + 2 * 9
+    assert alone[0] == both[0] == 0
+    assert more[0] == 0
+    assert planner([decodes(36, 8, half + [(33, 3, 9)]) + (-1,)])[0][0] == 3
+    assert planner([decodes(36, 8, [(0, 17, 64), (17, 2, 1)]) + (-1,)])[0][0] == 2
+
+
+def test_prompts_that_fill_their_tiles_read_runs_by_themselves(planner):
+    """Long prompts take no part in a run; the rest of its requests does."""
+    reqs, runs = [(1, 1, 5)] * 20 + [(0, 1024, 3), (0, 9, 0)], [(0, 22, 64)]
+    got, = planner([((8, 8, 128), tables(reqs, runs, itertools.count()), runs, -1)])
+    assert got[:2] == [1, 29]
