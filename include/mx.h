@@ -123,7 +123,7 @@ uint32_t mx_version(void);
 
 /*
  * Host-only check of a batch against a shape (the rules every entry point
- * applies first): R >= 0; phase in {PREFILL, DECODE}; n_new >= 1; a decode has
+ * applies first; mx_paged_attn_window looks at the ids of fewer pages): R >= 0; phase in {PREFILL, DECODE}; n_new >= 1; a decode has
  * n_new == 1 and ctx_len >= 1; ctx_len >= 0; n_pages >= ceil((ctx_len + n_new)/16)
  * (else MX_ERR_NO_SPACE); page ids in [0, pool_pages); the slots written by the
  * new tokens are distinct across the batch (cached prefix pages may be shared
@@ -262,7 +262,9 @@ mx_status mx_layer_step(const mx_batch* batch, const mx_layer_cfg* cfg, const vo
  * window >= 1 and sinks >= 0, else MX_ERR_INVALID; with window > p every key is seen.  Page
  * table entries of pages in which no new token of the call sees a position are neither
  * checked nor read (they may hold anything: pages that have left the window can be freed and
- * used again); the table's length is as for mx_paged_attn.
+ * used again); the table's length is as for mx_paged_attn.  The other calls check every id:
+ * mx_kv_append gets such a request with valid ids in those places, any ones, as it writes
+ * to the pages of new tokens alone.
  * Workspace: mx_workspace_bytes_window_for, and for any batch of at most max_tokens new
  * tokens, max_reqs requests and max_pages page-table entries in total
  * mx_workspace_bytes_window.
