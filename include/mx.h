@@ -255,6 +255,9 @@ mx_status mx_layer_step(const mx_batch* batch, const mx_layer_cfg* cfg, const vo
  * that is being captured into a graph (MX_ERR_UNSUPPORTED).  out may be q itself; any other
  * overlap of the two is refused (MX_ERR_INVALID).  A key or value reaches the rows that see
  * its token, and no other: what masked slots hold (NaN and infinities among it) stays out.
+ * Probabilities and sums are fp32 and sums are divided last, so that an infinite value whose
+ * probability underflows (some 90 below the row's largest score) may arrive as NaN, and
+ * finite values beyond 2^120 / (the keys that the row sees) may overflow.
  *
  * mx_paged_attn_window: a sliding window and sinks.  The token at position p sees the
  * positions j <= p with j > p - window or j < sinks:
