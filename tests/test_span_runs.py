@@ -75,3 +75,54 @@ def test_prompts_that_fill_their_tiles_read_runs_by_themselves(planner):
     reqs, runs = [(1, 1, 5)] * 20 + [(0, 1024, 3), (0, 9, 0)], [(0, 22, 64)]
     got, = planner([((8, 8, 128), tables(reqs, runs, itertools.count()), runs, -1)])
     assert got[:2] == [1, 29]
+
+
+def size_of(plan, d):
+    """The workspace of a plan's arrays: the metadata, each array from a multiple of 16 bytes on,
+    then the partial rows' outputs in fp32 and their maxima and sums, from multiples of 256."""
+    items, pages, listed, merged, sources, partials = plan[2:]
+    up = lambda n, k: -(-n // k) * k  # noqa: E731
+    n = 0
+    for count, size in ((items, 64), (pages, 4), (listed, 4), (merged, 16), (sources, 16)):
+        n = up(n + count * size, 16)
+    n = up(n, 256)
+    for size in (4 * d, 8):
+        n = up(n + partials * size, 256)
+    return max(n, 256)
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_workspace_bound_covers_every_plan(planner, seed):
+    """Random batches, below runs of any length, are taken apart whatever that saves: the bound for
+    batches of their size covers what their plans need.  As the library takes them apart, this is
+    the size that it names."""
+    rng = np.random.default_rng(400 + seed)
+    batches, bounds, sizes, joined = [], [], [], 0
+    for _ in range(40):
+        nkv = int(rng.choice([1, 2, 8, 19]))
+        heads = nkv * int(rng.choice([1, 4, 16, 17, 40])), nkv, int(rng.choice([64, 128]))
+        R = int(rng.integers(1, 14))
+        dec = rng.random(R) < rng.choice([0.2, 0.7, 1.0])
+        new = np.where(dec, 1, rng.integers(1, rng.choice([6, 40, 400]), R))
+        own = rng.integers(1, rng.choice([20, 300, 20000]), R)
+        runs, depth, start = [], np.zeros(R, int), np.zeros(R, int)
+        for _ in range(int(rng.integers(0, 6))):
+            a = int(rng.integers(0, R))
+            n = int(rng.integers(1, R - a + 1))
+            if (start[a:a + n] == start[a]).all():
+                k = int(rng.choice([1, 2, 30, 400]))
+                runs.append((a, n, k))
+                start[a:a + n] += k
+                depth[a:a + n] += 1
+        reqs = tables([(d, int(n), int(c)) for d, n, c in zip(dec, new, own)], runs, itertools.count())
+        s = mx.attn_shape(*heads, 1 << 30)
+        b = mx.Batch(dec.astype(int), new, [c for _, c, _ in reqs], [t for _, _, t in reqs])
+        bounds.append(mx.mx_workspace_bytes_shared(s, b.T, b.R, sum(len(t) for _, _, t in reqs), int(depth.max())))
+        sizes.append(mx.mx_workspace_bytes_shared_for(b, s, mx.SharedRuns(runs)))
+        batches.append((heads, reqs, runs))
+    for plan, b, n, bound in zip(planner([x + (-1,) for x in batches]), batches, sizes, bounds):
+        assert size_of(plan, b[0][2]) == n <= bound
+    for plan, b, bound in zip(planner([x + (0,) for x in batches]), batches, bounds):
+        assert size_of(plan, b[0][2]) <= bound, b[0]
+        joined += plan[0] > 0
+    assert joined > 10
