@@ -46,7 +46,8 @@ constexpr float kLazyMax = 8.0f;
 // is bit-identical in the four lanes of a row.
 // (The max as compare and select: fmaxf cannot tell that the swapped bits are
 // canonical and quiets both operands first, three instructions instead of two.
-// Scores are never NaN here: masked keys carry -1e30.)
+// The maxima are never NaN here: they start at a number, fmaxf takes no NaN score
+// over it, and masked keys carry -1e30 or -inf.)
 __device__ __forceinline__ float max_pair(float a, float b) { return a > b ? a : b; }
 __device__ __forceinline__ float lane_groups_max(float x) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -72,8 +73,12 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 // Called by the whole wave when some lane holds a score above its row's
 // threshold: each row takes its max over its four lane groups and raises m to
 // it if that exceeds m by more than kLazyMax, rescaling its output and sum.
-// The first step of every row comes here (thr starts at kNegBig and every row
-// has a key in its first step).
+// Masked scores are finite (kNegBig) where every row has a key in its first step:
+// states start with m = thr = kNegBig, and that step comes here for each of them.
+// Attention over parts of the keys masks with -inf and starts with the lowest
+// finite m and thr = -inf: the first score that a row sees comes here, and a row
+// that sees no key of a step, or of a whole item, is not raised by the others'
+// calls (its max is -inf) and keeps a sum of 0.
 template <int NO>
 __device__ __forceinline__ void raise_max(RowState& r, float mx, float scale_log2, float inv_scale,
                                           f32x4 (&o)[NO]) {
