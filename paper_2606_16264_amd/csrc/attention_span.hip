@@ -198,14 +198,16 @@ static_assert(kSpanTileRows == 4 * 32, "four waves of two 16-row blocks");
 // first_whole to end_whole, take no masks; those before (the window's low edge, sinks) and
 // behind (the diagonal, the end) do, and a wave leaves out those that none of its rows sees.
 //
-// Bound by the matrix cores and the vector instructions of the softmax beside them, at the
-// clock that the power limit leaves: a chunk takes 0.87 us with two workgroups on a CU (0.52
-// to 0.66 with one), 1.25 with masks, the start 3.5 and the end 2.2.  2048 tokens of 64 q
-// heads through a window of 4096 take 246 us, 1.13 PFLOP/s of what the rows see; a prompt of
-// 8191 on 32 heads through 1024 takes 175, 0.74 of what they see, as each tile of 128 tokens
-// takes 9 chunks of 37 with masks.  128 rows: twice as many in a workgroup would leave one of
+// Bound by the matrix cores and the vector instructions of the softmax beside them.  A whole
+// chunk takes 0.7 to 0.8 us with two workgroups on a CU and 0.59 with one, a chunk with masks
+// 1.0 to 1.3 at the diagonal and 1.6 to 1.9 at the window's low edge, the start 4 to 5 and the
+// end 2.2.  2048 tokens of 64 q heads through a window of 4096 take 247 us, 1.13 PFLOP/s of
+// what the rows see, with the matrix cores busy 56% of the time at 1.94 GHz, which the power
+// limit leaves.  A prompt of 8191 on 32 heads through 1024 takes 175, 0.74 PFLOP/s of what
+// they see, with them busy 33% at 2.26 GHz: half of a tile's 39 us is its start, its end and
+// nine chunks of 36 with masks.  128 rows: twice as many in a workgroup would leave one of
 // them on a CU, and half as many copy twice as much.  The 32x32x16 instruction takes half the
-// issue slots and 290 us where this takes 255: the clock falls.
+// issue slots and 290 us where this took 255: the clock falls.
 template <int HD>
 __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& it, int kvh, char* smem) {
   using SC = SharedChunk<HD>;
@@ -542,8 +544,8 @@ __device__ __forceinline__ void tile_item(const SpanParams& p, const SpanItem& i
 // would have to push out, 74 decodes beside a shared run take 98 us so and 140 otherwise, a
 // prompt of 1024 tokens beside 64 decodes 78 and 90.
 //
-// Bound by HBM: 128 decodes of 8 KV heads through a window of 4096 read 2.1 GB in 317 us, 6.7
-// TB/s; 64 through 1024 their 267 MB in 44, of which some 4 are the first chain of loads (item,
+// Bound by HBM: 128 decodes of 8 KV heads through a window of 4096 read 2.1 GB in 320 us, 6.6
+// TB/s; 64 through 1024 their 267 MB in 45, of which some 4 are the first chain of loads (item,
 // page id, keys).  With few items that chain is the time: 4 us.  (Eight waves to a workgroup
 // where streams are alone in up to 256: nothing gained over batches drawn at random.)
 template <int HD>

@@ -86,8 +86,11 @@ struct Part {
 // Whether a record's rows run as streams: a decode's, and so few that a stream holds them, which
 // has four waves share the keys where a tile would have one wave with rows and three without:
 // chunks of 2 to 4 tokens behind 2000 to 8000 keys take 11 to 15 us, as tiles 14 to 19, and 16
-// of them on 32 KV heads 20 and 25.  17 to 64 rows as streams of 16 would read their keys again
-// for each: up to a quarter less where a few requests are alone, half more in other batches.
+// of them on 32 KV heads 20 and 25.  17 to 64 rows of several tokens as streams of 16 would read
+// their keys again for each: up to a quarter less where a few requests are alone, half more in
+// other batches.  A lone token's group of more than 16 q heads does run so, as in mx_paged_attn:
+// 64 decodes behind 8000 keys take 99 us with 20 q heads on a KV head and 183 with 64 on two, 96
+// and 184 there, 2.7 and 2.9 TB/s of what they have to read; as tiles they were not measured.
 inline bool is_stream(const SpanRows& r, int group) {
   return r.n_rows <= kSpanStreamRows || (!r.list && r.n_rows == group);
 }
