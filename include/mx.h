@@ -456,7 +456,9 @@ mx_status mx_debug_gather(const mx_batch* batch, const mx_attn_shape* shape, int
 
 /* Launch timing, for profiling.  When enabled, every kernel launch of
  * mx_layer_step and mx_paged_attn (and those of mx_paged_attn_f8 together, of
- * mx_kv_evict_f8, mx_paged_attn_window and mx_paged_attn_shared likewise) is bracketed by two hipEvents recorded on the
+ * mx_kv_evict_f8, mx_paged_attn_window and mx_paged_attn_shared likewise), but for
+ * the upload of a call's metadata where that is a launch of its own, is bracketed
+ * by two hipEvents recorded on the
  * caller's stream (the launch's own stream), tagged with the step it performs
  * ("token_map+rmsnorm_1", "gemm_qkv", "paged_attn", "gemm_o", "rmsnorm_2",
  * "gemm_gate_up", "gemm_down", "paged_attn_f8", "kv_evict_f8", "paged_attn_window",

@@ -8,7 +8,7 @@ import pytest
 
 import paper_2606_16264_amd as mx
 from span_batches import CASES, D, P
-from test_gpu_span import Pools, bf16, check, reference, run_shared, shared_case
+from test_gpu_span import Pools, bf16, check, reference, run_shared, run_window, shared_case, window_case
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -113,3 +113,25 @@ def test_append_then_attention():
         check(out, *reference(pools, nq, reqs, q), f"step {step}")
 
 
+
+
+def test_launch_timing():
+    """Each call counts once under its tag, whichever way its metadata takes, and its results are
+    those without timing."""
+    window = [window_case(8, 2, 64, [(D, 1, 90 + i) for i in range(n)] + [(P, p, 9)] * (p > 0), 149, 33, 2)
+              for n, p in ((3, 0), (300, 0), (2, 900))]
+    nq, runs, pools, reqs, q = case_of("in place", 150)
+    calls = [lambda c=c: run_window(c[0], 8, c[1], c[2].cuda(), 33, 2)[0] for c in window]
+    calls.append(lambda: run_shared(pools, nq, reqs, runs, q.cuda())[0])
+    plain = [f() for f in calls]
+    mx.mx_profile_read()
+    mx.mx_profile_enable(True)
+    try:
+        timed = [f() for f in calls]
+        got = mx.mx_profile_read()
+    finally:
+        mx.mx_profile_enable(False)
+    for a, b in zip(plain, timed):
+        assert torch.equal(a.view(torch.uint16), b.view(torch.uint16))
+    assert {k: v[1] for k, v in got.items()} == {"paged_attn_window": 3, "paged_attn_shared": 1}
+    assert all(v[0] > 0 for v in got.values())
